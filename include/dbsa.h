@@ -146,6 +146,36 @@ int dbsa_layout_build_append(const dbsa_pool_desc* pool, int32_t first_group, in
                              int32_t flags, void* stream, dbsa_layout** out);
 
 /*
+ * Layout of the chunk attention (dbsa_chunk_attn): several new tokens per question, whose own keys lie in pages.
+ * pool and sel as for a query-stage layout, sel->cu_qlens packing the NEW tokens (n_split is ignored); the heads are those of
+ * the calls, because the plan deals blocks of rows (tokens x query heads of a KV head) to workgroups.
+ *   own_tokens : host [B], each question's own keys at the call, its new tokens included (NULL: no older ones).  Only the
+ *                balance of the launch goes by it; the keys attended are those that self_len counts at the call, so that
+ *                one layout serves all layers, and later steps that bring as many new tokens.
+ * Such a layout goes with dbsa_chunk_attn, dbsa_chunk_attn_kv8, dbsa_workspace_bytes (0 for another n_q_heads) and
+ * dbsa_layout_export_chunk; every other call takes it for a layout of the wrong stage.
+ * Errors as dbsa_layout_build; UNSUPPORTED unless n_q_heads is a multiple of n_kv_heads, at most 32 times as many.
+ */
+int dbsa_layout_build_chunk(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t n_q_heads, int32_t n_kv_heads,
+                            const int32_t* own_tokens, int32_t flags, void* stream, dbsa_layout** out);
+
+/*
+ * The plan of a chunk layout (plumbing; INVALID_ARG for any other).
+ *   rows       : rows of a workgroup (tokens x query heads of a KV head).
+ *   worker_ptr : int32 [n_workers + 1]: worker c of every KV head takes records worker_ptr[c] .. worker_ptr[c+1]-1.
+ *   records    : int32 [n_records][12] = (first token in tokens, tokens, first tile in tiles, pool tiles, question whose own
+ *                keys follow or -1, first own tile, own tile behind the last, own tiles expected, first partial row or -1,
+ *                first new token and new tokens of that question, 0).  Own tiles are 64 keys; the device scales the
+ *                range from the tiles expected to those that self_len gives.
+ *   tokens     : int32: new tokens of the records' blocks.     tiles : int32 [][2], encoding as list_ent, kinds FULL.
+ *   part_ptr   : int32 [sum T + 1] into parts: partial rows of a token (none: its record finishes its rows).
+ * The arrays belong to the layout; any output pointer may be NULL.
+ */
+int dbsa_layout_export_chunk(const dbsa_layout* layout, int32_t* rows, const int32_t** worker_ptr, int32_t* n_workers,
+                             const int32_t** records, const int32_t** tokens, const int32_t** tiles, const int32_t** part_ptr,
+                             const int32_t** parts);
+
+/*
  * Host views of the lists, valid until the layout is destroyed.
  *   qtile_tab : int32 [n_qtiles][4] = (q_start, q_len, owner, 0); owner is -1 for
  *               the sink segment, else the group (pre-encode) or query index.
@@ -502,6 +532,95 @@ int dbsa_decode_attn_kv8_rope(const dbsa_layout* layout, dbsa_tensor q_step, dbs
                               dbsa_tensor o, const float* rope_table, int32_t rope_n_pos, int32_t n_q_heads,
                               int32_t n_kv_heads, int32_t head_dim, float softmax_scale, void* workspace,
                               size_t workspace_bytes, void* stream);
+
+/*
+ * ---- chunks of new tokens over paged caches ---------------------------------------------------
+ * Own keys of the questions in pages: key j of question u is row j % page_tokens of page
+ * table[u * table_stride + j / page_tokens].  A question's table row thus holds table_stride * page_tokens keys at most.
+ * (Contiguous caches [B, Tmax, Hkv, D] are pages of Tmax tokens with table[u] = u.)
+ */
+typedef struct {
+  dbsa_tensor k, v;      /* first page; element strides between tokens and heads of a page */
+  int64_t stride_page;   /* elements between pages (k and v); a multiple like the other strides */
+  const int32_t* table;  /* device int32 [B][table_stride] */
+  int32_t table_stride;  /* >= 1 */
+  int32_t page_tokens;   /* a power of two, at least 16 */
+  int32_t n_pages;       /* pages there are; a table entry outside [0, n_pages) is a page that is not there: no row
+                            sees its keys, and nothing is read for it */
+} dbsa_pages;
+
+/*
+ * Stage 2 for a chunk of T_u >= 1 new tokens per question (a follow-up turn, a long prompt piece by piece, several
+ * proposed tokens checked at once, one generated token): new token a attends the sink, every key of u's selected
+ * groups, and u's own keys 0 .. self_len[u] - T_u + a; one softmax over the union.  The caller puts the new tokens' K/V into
+ * the pages before the call and counts them in self_len, as for dbsa_decode_attn; all tensors are post-RoPE.
+ *
+ *   layout     : of dbsa_layout_build_chunk, with these heads, on the device.
+ *   q, o       : [sum T, n_q_heads, D], new tokens packed by the layout's cu_qlens; rows behind the last are left alone.
+ *   k_pool, v_pool : [N, n_kv_heads, D] (or the arena the layout's page_start names).
+ *   self_len   : device int32 [B], taken as at least 0 and at most the table row's keys.  A token whose own index
+ *                self_len[u] - T_u + a is negative has no own keys (left padding); a row without any key gives
+ *                zeros, and lse -inf.
+ *   lse        : optional device float [n_q_heads][sum T]: natural-log softmax denominator.
+ *   dtype      : DBSA_BF16 or DBSA_F32, of every tensor; head_dim in {64, 128}.
+ *   workspace  : device memory of >= dbsa_workspace_bytes() bytes, 16-byte aligned (none where that is 0); two calls that
+ *                overlap need one each.
+ * The call only launches kernels, whose number and shape are the layout's: it may be recorded into a HIP graph, and
+ * self_len, the table and the caches may change between replays.  Results do not depend on what runs beside it.
+ * A non-finite VALUE under a mask (a later token of the chunk) does not reach the rows that do not see it.
+ * Errors: INVALID_ARG, UNSUPPORTED (also pages of more than 2^31 rows), WORKSPACE, HIP.
+ */
+int dbsa_chunk_attn(const dbsa_layout* layout, dbsa_tensor q, dbsa_tensor k_pool, dbsa_tensor v_pool, const dbsa_pages* own,
+                    const int32_t* self_len, dbsa_tensor o, float* lse, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads,
+                    int32_t head_dim, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * dbsa_chunk_attn over 8-bit caches: pool AND pages are e4m3 bytes (strides in bytes, multiples of 16) with the value
+ * byte * k_scale[kv head] (v_scale likewise; device float [n_kv_heads]), as dbsa_kv8_write leaves them; q and o are bf16.
+ * The result is defined on the de-quantised values.  (dbsa_decode_attn_kv8 keeps the own cache in bf16.)
+ */
+int dbsa_chunk_attn_kv8(const dbsa_layout* layout, dbsa_tensor q, dbsa_tensor k_pool8, dbsa_tensor v_pool8,
+                        const dbsa_pages* own8, const int32_t* self_len, const float* k_scale, const float* v_scale,
+                        dbsa_tensor o, float* lse, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                        float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- 8-bit caches: what dbsa_decode_attn_kv8 and dbsa_chunk_attn_kv8 read -----------------------
+ * Scales of n_tokens rows of K and V: the largest finite magnitude of a KV head over 448, the largest value of the format
+ * (a head of zeros gets 0).  running != 0: the scales in k_scale / v_scale (>= 0) stay where they are larger.
+ *   k, v       : [n_tokens, n_kv_heads, D], dtype DBSA_BF16 or DBSA_F32, D in {64, 128}.
+ *   rope_table : NULL, or as written by dbsa_rope_table: K is taken rotated at positions[t] (device int32 [n_tokens], clamped to
+ *                the table), or at first_id + t when positions is NULL (INVALID_ARG unless inside the table), in
+ *                fp32; the rotated keys are not written anywhere.
+ *   k_scale, v_scale : device float [n_kv_heads], written.
+ * The result does not depend on the order in which the rows are visited.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+int dbsa_kv8_scales(dbsa_tensor k, dbsa_tensor v, int32_t n_tokens, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                    const int32_t* positions, int32_t first_id, const float* rope_table, int32_t rope_n_pos, int32_t running,
+                    float* k_scale, float* v_scale, void* stream);
+
+/*
+ * Quantises rows as they enter a cache: cache row rows[t] (device int32 [n_tokens]; or first_row + t when rows is NULL) of
+ * k_cache8 / v_cache8 (e4m3 bytes [n_rows, n_kv_heads, D], strides in bytes, multiples of 16) receives the nearest
+ * e4m3 values, ties to even, of k[t] * (1 / k_scale) and v[t] * (1 / v_scale), both operations in fp32; what lies beyond the
+ * format becomes +-448, NaN stays NaN, and under a scale whose inverse is not finite (0) every finite element becomes 0.
+ * K is rotated first as in dbsa_kv8_scales.  A token whose row is outside [0, n_rows) is not written (padding); rows the call
+ * does not name stay as they are.  Rows have to differ: one named twice ends up with 16-byte pieces of either token.
+ * With rows == NULL: INVALID_ARG unless first_row >= 0 and first_row + n_tokens <= n_rows.  Errors as dbsa_kv8_scales.
+ */
+int dbsa_kv8_write(dbsa_tensor k, dbsa_tensor v, int32_t n_tokens, const int32_t* rows, int64_t first_row, dbsa_tensor k_cache8,
+                   dbsa_tensor v_cache8, int64_t n_rows, const float* k_scale, const float* v_scale, int32_t n_kv_heads,
+                   int32_t head_dim, int32_t dtype, const int32_t* positions, int32_t first_id, const float* rope_table,
+                   int32_t rope_n_pos, void* stream);
+
+/*
+ * Reads cache rows back: k[t] = byte * k_scale of cache row rows[t] (or first_row + t), v likewise, rounded once to
+ * dtype.  A row outside [0, n_rows) gives zeros; the same row may be named any number of times.  Arguments and errors as
+ * dbsa_kv8_write.
+ */
+int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, const int32_t* rows, int64_t first_row,
+                  int32_t n_tokens, const float* k_scale, const float* v_scale, dbsa_tensor k, dbsa_tensor v,
+                  int32_t n_kv_heads, int32_t head_dim, int32_t dtype, void* stream);
 
 #ifdef __cplusplus
 }

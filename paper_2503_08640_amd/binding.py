@@ -46,6 +46,8 @@ EXPORTED_SYMBOLS = (
     "dbsa_decode_attn_rope", "dbsa_decode_attn_kv8", "dbsa_decode_attn_kv8_rope", "dbsa_decode_attn_static", "dbsa_pooled_list_blocks", "dbsa_layout_export_matrix_records",
     "dbsa_layout_export_matrix_plan",
     "dbsa_layout_export_schedule", "dbsa_layout_export_cut_schedule",
+    "dbsa_layout_build_chunk", "dbsa_layout_export_chunk", "dbsa_chunk_attn", "dbsa_chunk_attn_kv8", "dbsa_kv8_scales",
+    "dbsa_kv8_write", "dbsa_kv8_read",
 )
 DBSA_STATIC_SCRATCH_BYTES = 32 << 20
 
@@ -68,6 +70,11 @@ class SelectDesc(C.Structure):
 
 class Tensor(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("stride_tok", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class Pages(C.Structure):
+    _fields_ = [("k", Tensor), ("v", Tensor), ("stride_page", C.c_int64), ("table", C.c_void_p), ("table_stride", C.c_int32),
+                ("page_tokens", C.c_int32), ("n_pages", C.c_int32)]
 
 
 _lib = None
@@ -155,6 +162,26 @@ def lib() -> C.CDLL:
     L.dbsa_decode_attn_kv8_rope.argtypes = [C.c_void_p, Tensor, Tensor, Tensor, C.c_void_p, C.c_int64, Tensor, Tensor,
                                             C.c_void_p, C.c_void_p, Tensor, C.c_void_p, C.c_int32, C.c_int32,
                                             C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.dbsa_layout_build_chunk.restype = C.c_int
+    L.dbsa_layout_build_chunk.argtypes = [C.POINTER(PoolDesc), C.POINTER(SelectDesc), C.c_int32, C.c_int32,
+                                          C.POINTER(C.c_int32), C.c_int32, C.c_void_p, C.POINTER(C.c_void_p)]
+    ints = C.POINTER(C.POINTER(C.c_int32))
+    L.dbsa_layout_export_chunk.restype = C.c_int
+    L.dbsa_layout_export_chunk.argtypes = [C.c_void_p, C.POINTER(C.c_int32), ints, C.POINTER(C.c_int32)] + [ints] * 5
+    L.dbsa_chunk_attn.restype = C.c_int
+    L.dbsa_chunk_attn.argtypes = [C.c_void_p, Tensor, Tensor, Tensor, C.POINTER(Pages), C.c_void_p, Tensor, C.c_void_p] + tail
+    L.dbsa_chunk_attn_kv8.restype = C.c_int
+    L.dbsa_chunk_attn_kv8.argtypes = [C.c_void_p, Tensor, Tensor, Tensor, C.POINTER(Pages), C.c_void_p, C.c_void_p, C.c_void_p,
+                                      Tensor, C.c_void_p] + tail[1:]
+    rope = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int32]
+    L.dbsa_kv8_scales.restype = C.c_int
+    L.dbsa_kv8_scales.argtypes = [Tensor, Tensor] + [C.c_int32] * 4 + rope + [C.c_int32] + [C.c_void_p] * 3
+    L.dbsa_kv8_write.restype = C.c_int
+    L.dbsa_kv8_write.argtypes = [Tensor, Tensor, C.c_int32, C.c_void_p, C.c_int64, Tensor, Tensor, C.c_int64, C.c_void_p,
+                                 C.c_void_p] + [C.c_int32] * 3 + rope + [C.c_void_p]
+    L.dbsa_kv8_read.restype = C.c_int
+    L.dbsa_kv8_read.argtypes = [Tensor, Tensor, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, Tensor,
+                                Tensor] + [C.c_int32] * 3 + [C.c_void_p]
     _lib = L
     return L
 
@@ -300,6 +327,21 @@ class Layout:
         n = int(ptr[-1])
         return bool(worth.value), ptr, arr(rc, n, 4), arr(pr, n), arr(ct, n_cut.value, 4)
 
+    def export_chunk(self, n_tokens: int):
+        """-> dict(rows, worker_ptr [W+1], records [n, 12], tokens, tiles [m, 2], part_ptr [n_tokens+1], parts) int32 copies."""
+        rows, nw = C.c_int32(), C.c_int32()
+        wp, rc, tk, tl, pp, pt = (C.POINTER(C.c_int32)() for _ in range(6))
+        _check(lib().dbsa_layout_export_chunk(self.handle, C.byref(rows), C.byref(wp), C.byref(nw), C.byref(rc), C.byref(tk),
+                                              C.byref(tl), C.byref(pp), C.byref(pt)), "dbsa_layout_export_chunk")
+
+        def arr(p, *shape):
+            return np.ctypeslib.as_array(p, shape=shape).copy() if shape[0] else np.zeros(shape, np.int32)
+        worker_ptr, part_ptr = arr(wp, nw.value + 1), arr(pp, n_tokens + 1)
+        rec = arr(rc, int(worker_ptr[-1]), 12)
+        return dict(rows=rows.value, worker_ptr=worker_ptr, records=rec, part_ptr=part_ptr, parts=arr(pt, int(part_ptr[-1])),
+                    tokens=arr(tk, int((rec[:, 0] + rec[:, 1]).max())),
+                    tiles=arr(tl, int((rec[:, 2] + rec[:, 3]).max()), 2))
+
     def workspace_bytes(self, n_q_heads: int, head_dim: int) -> int:
         return int(lib().dbsa_workspace_bytes(self.handle, n_q_heads, head_dim))
 
@@ -337,6 +379,25 @@ def dbsa_layout_build_append(sink_len: int, demo_offsets, group_demo_offsets, pr
                                         DBSA_LAYOUT_HOST_ONLY if host_only else 0, C.c_void_p(stream), C.byref(out))
     _check(rc, "dbsa_layout_build_append")
     return Layout(out.value, False, int(block_m), int(block_n))
+
+
+def dbsa_layout_build_chunk(sink_len: int, demo_offsets, group_demo_offsets, *, cu_qlens, sel_ptr, sel_idx=None,
+                            n_q_heads: int, n_kv_heads: int, own_tokens=None, page_start=None, host_only: bool = False,
+                            stream: int = 0) -> Layout:
+    """Layout of the chunk attention: cu_qlens packs the new tokens, own_tokens [B] counts each question's own keys (new
+    tokens included) for the balance of the launch."""
+    do, gdo, cu, sp = _i32(demo_offsets), _i32(group_demo_offsets), _i32(cu_qlens), _i32(sel_ptr)
+    si = _i32(sel_idx if sel_idx is not None else [])
+    own = _i32(own_tokens) if own_tokens is not None else None
+    assert own is None or len(own) == len(cu) - 1, "own_tokens: one number per question"
+    ps = _i32(page_start) if page_start is not None else None
+    pool = PoolDesc(int(sink_len), len(do) - 1, _p32(do), len(gdo) - 1, _p32(gdo), 0)
+    sel = SelectDesc(len(cu) - 1, _p32(cu), _p32(sp), _p32(si), 0, _p32(ps))
+    out = C.c_void_p()
+    rc = lib().dbsa_layout_build_chunk(C.byref(pool), C.byref(sel), int(n_q_heads), int(n_kv_heads), _p32(own),
+                                       DBSA_LAYOUT_HOST_ONLY if host_only else 0, C.c_void_p(stream), C.byref(out))
+    _check(rc, "dbsa_layout_build_chunk")
+    return Layout(out.value, False, 0, 64)
 
 
 # ---------------------------------------------------------------------------
@@ -537,3 +598,143 @@ def dbsa_decode_attn_kv8(layout: Layout, q_step, k_cache, v_cache, self_len, k_p
     _check(rc, "dbsa_decode_attn_kv8")
     return o
 
+
+
+# ---------------------------------------------------------------------------
+# chunks of new tokens over paged caches, 8-bit caches
+# ---------------------------------------------------------------------------
+
+def _here(*tensors) -> None:
+    """These calls launch on the current device's current stream: every tensor has to be on that device."""
+    device = _stream_calls()[0]()
+    for t in tensors:
+        assert t is None or t.device.index == device, "expected tensors on the current device"
+
+
+def _pages(k_pages, v_pages, page_table):
+    """[pages, page tokens, heads, D] device tensors and an int32 [B, pages of a question] table."""
+    s = k_pages.stride()
+    assert k_pages.dim() == 4 and s[3] == 1 and v_pages.stride() == s and v_pages.shape == k_pages.shape
+    assert page_table.dim() == 2 and page_table.element_size() == 4 and not page_table.is_floating_point()
+    assert page_table.is_contiguous(), "expected a contiguous page table"
+    return Pages(_cache(k_pages), _cache(v_pages), s[0], page_table.data_ptr(), page_table.shape[1], k_pages.shape[1],
+                 k_pages.shape[0])
+
+
+def _chunk_args(layout: Layout, q, k_pages, page_table, self_len, k_pool, out, lse, workspace):
+    import torch
+    assert self_len.element_size() == 4 and not self_len.is_floating_point() and self_len.is_contiguous()
+    assert self_len.shape[0] == page_table.shape[0] and k_pool.shape[1:] == k_pages.shape[2:]
+    o = torch.empty_like(q) if out is None else out
+    assert o.shape == q.shape and o.dtype == q.dtype
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous())
+    _here(q, k_pages, page_table, self_len, k_pool, o, lse)
+    ws, ws_ptr, ws_bytes = _workspace(layout, q, workspace)
+    _here(ws)
+    return o, ws, ws_ptr, ws_bytes
+
+
+def dbsa_chunk_attn(layout: Layout, q, k_pool, v_pool, k_pages, v_pages, page_table, self_len, scale: float, out=None, lse=None,
+                    workspace=None):
+    """Stage 2 for the new tokens q [sum T, Hq, D] of every question: pool part as the layout lists it, own keys (older ones
+    and the new tokens', self_len int32 [B] on the device) in pages k_pages / v_pages [pages, page tokens, Hkv, D] by page_table
+    int32 [B, pages of a question].  Returns O [sum T, Hq, D]."""
+    o, ws, ws_ptr, ws_bytes = _chunk_args(layout, q, k_pages, page_table, self_len, k_pool, out, lse, workspace)
+    assert q.dtype == k_pool.dtype == v_pool.dtype == k_pages.dtype == v_pages.dtype
+    pages = _pages(k_pages, v_pages, page_table)
+    rc = lib().dbsa_chunk_attn(layout.handle, _tensor(q), _tensor(k_pool), _tensor(v_pool), C.byref(pages),
+                               C.c_void_p(self_len.data_ptr()), _tensor(o), C.c_void_p(lse.data_ptr() if lse is not None else None),
+                               _dtype_code(q), q.shape[1], k_pool.shape[1], q.shape[2], float(scale), ws_ptr, ws_bytes,
+                               C.c_void_p(_stream()))
+    _check(rc, "dbsa_chunk_attn")
+    return o
+
+
+def dbsa_chunk_attn_kv8(layout: Layout, q, k_pool8, v_pool8, k_pages8, v_pages8, page_table, self_len, k_scale, v_scale,
+                        scale: float, out=None, lse=None, workspace=None):
+    """dbsa_chunk_attn over an 8-bit pool and 8-bit pages (float8_e4m3fn or uint8 tensors) with float32 scales [Hkv] on the
+    device, as dbsa_kv8_write leaves them; q and the result are bf16."""
+    import torch
+    o, ws, ws_ptr, ws_bytes = _chunk_args(layout, q, k_pages8, page_table, self_len, k_pool8, out, lse, workspace)
+    assert q.dtype == torch.bfloat16 and all(t.element_size() == 1 for t in (k_pool8, v_pool8, k_pages8, v_pages8))
+    _scales(k_scale, v_scale, k_pool8.shape[1])
+    pages = _pages(k_pages8, v_pages8, page_table)
+    rc = lib().dbsa_chunk_attn_kv8(layout.handle, _tensor(q), _tensor(k_pool8), _tensor(v_pool8), C.byref(pages),
+                                   C.c_void_p(self_len.data_ptr()), C.c_void_p(k_scale.data_ptr()), C.c_void_p(v_scale.data_ptr()),
+                                   _tensor(o), C.c_void_p(lse.data_ptr() if lse is not None else None), q.shape[1],
+                                   k_pool8.shape[1], q.shape[2], float(scale), ws_ptr, ws_bytes, C.c_void_p(_stream()))
+    _check(rc, "dbsa_chunk_attn_kv8")
+    return o
+
+
+def _scales(k_scale, v_scale, n_kv_heads: int) -> None:
+    import torch
+    for s in (k_scale, v_scale):
+        assert s.dtype == torch.float32 and s.numel() == n_kv_heads and s.is_contiguous(), "expected float32 scales, one per KV head"
+    _here(k_scale, v_scale)
+
+
+def _rope_args(table, positions, first_id, n_tokens):
+    if positions is not None:
+        assert positions.element_size() == 4 and positions.is_contiguous() and positions.numel() == n_tokens
+    _here(table, positions)
+    return (C.c_void_p(positions.data_ptr() if positions is not None else None), int(first_id),
+            C.c_void_p(table.data_ptr() if table is not None else None), table.shape[0] if table is not None else 0)
+
+
+def dbsa_kv8_scales(k, v, k_scale=None, v_scale=None, running: bool = False, table=None, positions=None, first_id: int = 0):
+    """-> (k_scale, v_scale) float32 [Hkv]: largest magnitude of k / v [T, Hkv, D] over 448, k rotated by ``table`` if given.
+    ``running`` keeps given scales where they are larger."""
+    import torch
+    assert k.shape == v.shape and k.dtype == v.dtype and not (running and (k_scale is None or v_scale is None))
+    if k_scale is None:
+        k_scale = torch.empty(k.shape[1], dtype=torch.float32, device=k.device)
+    if v_scale is None:
+        v_scale = torch.empty(k.shape[1], dtype=torch.float32, device=k.device)
+    _scales(k_scale, v_scale, k.shape[1])
+    _here(k, v)
+    rc = lib().dbsa_kv8_scales(_tensor(k), _tensor(v), k.shape[0], k.shape[1], k.shape[2], _dtype_code(k),
+                               *_rope_args(table, positions, first_id, k.shape[0]), int(running), C.c_void_p(k_scale.data_ptr()),
+                               C.c_void_p(v_scale.data_ptr()), C.c_void_p(_stream()))
+    _check(rc, "dbsa_kv8_scales")
+    return k_scale, v_scale
+
+
+def _cache_rows(k8, v8, rows, n_tokens):
+    assert k8.shape == v8.shape and k8.element_size() == 1 and v8.element_size() == 1
+    assert rows is None or (rows.element_size() == 4 and not rows.is_floating_point() and rows.is_contiguous() and rows.numel() == n_tokens)
+    _here(k8, v8, rows)
+    return C.c_void_p(rows.data_ptr() if rows is not None else None)
+
+
+def dbsa_kv8_write(k, v, k8, v8, k_scale, v_scale, rows=None, first_row: int = 0, table=None, positions=None, first_id: int = 0):
+    """Quantises k, v [T, Hkv, D] into rows ``rows`` (int32 [T] on the device; outside the cache = not written) or first_row + t
+    of the 8-bit caches k8, v8 [rows, Hkv, D]; k is rotated by ``table`` at ``positions`` or first_id + t if one is given."""
+    assert k.shape == v.shape and k.dtype == v.dtype and k.shape[1:] == k8.shape[1:]
+    _scales(k_scale, v_scale, k.shape[1])
+    _here(k, v)
+    rows_ptr = _cache_rows(k8, v8, rows, k.shape[0])
+    rc = lib().dbsa_kv8_write(_tensor(k), _tensor(v), k.shape[0], rows_ptr, int(first_row), _tensor(k8), _tensor(v8), k8.shape[0],
+                              C.c_void_p(k_scale.data_ptr()), C.c_void_p(v_scale.data_ptr()), k.shape[1], k.shape[2],
+                              _dtype_code(k), *_rope_args(table, positions, first_id, k.shape[0]), C.c_void_p(_stream()))
+    _check(rc, "dbsa_kv8_write")
+
+
+def dbsa_kv8_read(k8, v8, k_scale, v_scale, rows=None, first_row: int = 0, n_tokens: Optional[int] = None, dtype=None, k_out=None,
+                  v_out=None):
+    """-> (k, v) [T, Hkv, D]: rows ``rows`` (int32 [T]) or first_row .. first_row + n_tokens - 1 of an 8-bit cache, in ``dtype``
+    (bf16 unless given) or in the type of ``k_out``."""
+    import torch
+    n = rows.numel() if rows is not None else k8.shape[0] - first_row if n_tokens is None else n_tokens
+    shape = (n, k8.shape[1], k8.shape[2])
+    k = torch.empty(shape, dtype=dtype or torch.bfloat16, device=k8.device) if k_out is None else k_out
+    v = torch.empty(shape, dtype=k.dtype, device=k8.device) if v_out is None else v_out
+    assert tuple(k.shape) == shape and tuple(v.shape) == shape and k.dtype == v.dtype
+    _scales(k_scale, v_scale, k8.shape[1])
+    _here(k, v)
+    rows_ptr = _cache_rows(k8, v8, rows, n)
+    rc = lib().dbsa_kv8_read(_tensor(k8), _tensor(v8), k8.shape[0], rows_ptr, int(first_row), n, C.c_void_p(k_scale.data_ptr()),
+                             C.c_void_p(v_scale.data_ptr()), _tensor(k), _tensor(v), k8.shape[1], k8.shape[2], _dtype_code(k),
+                             C.c_void_p(_stream()))
+    _check(rc, "dbsa_kv8_read")
+    return k, v

@@ -4,9 +4,11 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
+#include <functional>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -175,13 +177,18 @@ hipError_t upload_lists(dbsa_layout* L, hipStream_t stream) {
                b_srec = L->qtile_tab.size() * sizeof(int32_t), b_sptr = (kMaxSchedClasses + 1) * sizeof(int32_t),
                b_mrec = L->mx_rec.size() * sizeof(int32_t), b_dsh = L->dec_shift.size() * sizeof(int32_t),
                b_gqs = L->gm_qshift.size() * sizeof(int32_t), b_mqr = L->mx_qrefs.size() * sizeof(int32_t),
-               b_mqs = L->mx_qshift.size() * sizeof(int32_t), b_msp = L->mx_slot_ptr.size() * sizeof(int64_t);
+               b_mqs = L->mx_qshift.size() * sizeof(int32_t), b_msp = L->mx_slot_ptr.size() * sizeof(int64_t),
+               b_crec = L->ck_rec.size() * sizeof(int32_t), b_cptr = L->ck_ptr.size() * sizeof(int32_t),
+               b_ctok = L->ck_toks.size() * sizeof(int32_t), b_cent = L->ck_ent.size() * sizeof(int32_t),
+               b_ctp = L->ck_tok_ptr.size() * sizeof(int32_t), b_ctq = L->ck_tok_part.size() * sizeof(int32_t);
   const size_t o_tab = 0, o_ptr = o_tab + pad(b_tab), o_ent = o_ptr + pad(b_ptr), o_ord = o_ent + pad(b_ent),
                o_dec = o_ord + pad(b_ord), o_spl = o_dec + pad(b_dec), o_gsp = o_spl + pad(b_spl),
                o_lsh = o_gsp + pad(b_gsp), o_gir = o_lsh + pad(b_lsh), o_grp = o_gir + pad(b_gir),
                o_grw = o_grp + pad(b_grp), o_gse = o_grw + pad(b_grw), o_gqr = o_gse + pad(b_gse),
                o_dsh = o_gqr + pad(b_gqr), o_gqs = o_dsh + pad(b_dsh), o_mqr = o_gqs + pad(b_gqs), o_mqs = o_mqr + pad(b_mqr), o_msp = o_mqs + pad(b_mqs),
-               o_cut = o_msp + pad(b_msp), o_srec = o_cut + pad(cut_room_bytes(L)), o_sptr = o_srec + pad(b_srec),
+               o_crec = o_msp + pad(b_msp), o_cptr = o_crec + pad(b_crec), o_ctok = o_cptr + pad(b_cptr),
+               o_cent = o_ctok + pad(b_ctok), o_ctp = o_cent + pad(b_cent), o_ctq = o_ctp + pad(b_ctp),
+               o_cut = o_ctq + pad(b_ctq), o_srec = o_cut + pad(cut_room_bytes(L)), o_sptr = o_srec + pad(b_srec),
                o_mrec = o_sptr + pad(b_sptr), o_mptr = o_mrec + pad(b_mrec), total = o_mptr + pad(b_sptr) + 256;
   ListBlock blk{};
   hipError_t e = acquire_block(total, &blk);
@@ -208,6 +215,12 @@ hipError_t upload_lists(dbsa_layout* L, hipStream_t stream) {
   put(o_mqr, L->mx_qrefs.data(), b_mqr);
   put(o_mqs, L->mx_qshift.data(), b_mqs);
   put(o_msp, L->mx_slot_ptr.data(), b_msp);
+  put(o_crec, L->ck_rec.data(), b_crec);
+  put(o_cptr, L->ck_ptr.data(), b_cptr);
+  put(o_ctok, L->ck_toks.data(), b_ctok);
+  put(o_cent, L->ck_ent.data(), b_cent);
+  put(o_ctp, L->ck_tok_ptr.data(), b_ctp);
+  put(o_ctq, L->ck_tok_part.data(), b_ctq);
   L->dev.cut_room = static_cast<unsigned char*>(blk.dev) + o_cut;
   // the staging twin stays with the block, so nothing has to wait for the copy here; calls on
   // other streams are ordered behind it through the event
@@ -251,6 +264,12 @@ hipError_t upload_lists(dbsa_layout* L, hipStream_t stream) {
   L->dev.mx_qrefs = reinterpret_cast<int32_t*>(b + o_mqr);
   L->dev.mx_qshift = reinterpret_cast<int32_t*>(b + o_mqs);
   L->dev.mx_slot_ptr = reinterpret_cast<int64_t*>(b + o_msp);
+  L->dev.ck_rec = reinterpret_cast<int32_t*>(b + o_crec);
+  L->dev.ck_ptr = reinterpret_cast<int32_t*>(b + o_cptr);
+  L->dev.ck_toks = reinterpret_cast<int32_t*>(b + o_ctok);
+  L->dev.ck_ent = reinterpret_cast<int32_t*>(b + o_cent);
+  L->dev.ck_tok_ptr = reinterpret_cast<int32_t*>(b + o_ctp);
+  L->dev.ck_tok_part = reinterpret_cast<int32_t*>(b + o_ctq);
   L->dev.sched_rec = reinterpret_cast<int32_t*>(b + o_srec);
   L->dev.sched_ptr = reinterpret_cast<int32_t*>(b + o_sptr);
   L->dev.mx_sched_rec = reinterpret_cast<int32_t*>(b + o_mrec);
@@ -675,7 +694,7 @@ int prefill_common(const dbsa_layout* L, bool want_query_stage, dbsa_tensor q, d
                    dbsa_tensor k_pool, dbsa_tensor v_pool, dbsa_tensor o, float* lse, int32_t dtype, int32_t hq,
                    int32_t hkv, int32_t d, float scale, void* stream, const float* rope_table = nullptr,
                    int32_t rope_n_pos = 0, void* workspace = nullptr, size_t workspace_bytes = 0) {
-  if (!L || !L->on_device || L->query_stage != want_query_stage) return DBSA_ERR_INVALID_ARG;
+  if (!L || !L->on_device || L->chunk_stage || L->query_stage != want_query_stage) return DBSA_ERR_INVALID_ARG;
   if (int rc = check_shapes(dtype, hq, hkv, d, scale)) return rc;
   if (!tensor_ok(q, dtype) || !tensor_ok(k_pool, dtype) || !tensor_ok(v_pool, dtype) || !tensor_ok(o, dtype))
     return DBSA_ERR_INVALID_ARG;
@@ -788,8 +807,8 @@ const char* dbsa_strerror(int code) {
 }
 
 namespace {
-int build_layout(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t first_group, int32_t block_m,
-                 int32_t block_n, int32_t flags, void* stream, dbsa_layout** out) {
+// build_lists(L): fills the host lists, returns a DBSA_* code
+int build_layout_with(int32_t flags, void* stream, dbsa_layout** out, const std::function<int(dbsa_layout*)>& build_lists) {
   if (!out || (flags & ~DBSA_LAYOUT_HOST_ONLY)) return DBSA_ERR_INVALID_ARG;
   dbsa_layout* L = new (std::nothrow) dbsa_layout();
   if (!L) return DBSA_ERR_INVALID_ARG;
@@ -797,7 +816,7 @@ int build_layout(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_
   // the decode chunking and the split / persistent prefill launches are sized for the current device
   if (!(flags & DBSA_LAYOUT_HOST_ONLY)) L->compute_units = device_compute_units();
   try {
-    rc = dbsa_build_host_lists(pool, sel, first_group, block_m, block_n, L);
+    rc = build_lists(L);
   } catch (...) {
     rc = DBSA_ERR_INVALID_ARG;
   }
@@ -816,6 +835,13 @@ int build_layout(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_
   *out = L;
   return DBSA_OK;
 }
+
+int build_layout(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t first_group, int32_t block_m,
+                 int32_t block_n, int32_t flags, void* stream, dbsa_layout** out) {
+  return build_layout_with(flags, stream, out, [&](dbsa_layout* L) {
+    return dbsa_build_host_lists(pool, sel, first_group, block_m, block_n, L);
+  });
+}
 }  // namespace
 
 int dbsa_layout_build(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t block_m, int32_t block_n,
@@ -827,6 +853,28 @@ int dbsa_layout_build_append(const dbsa_pool_desc* pool, int32_t first_group, in
                              int32_t flags, void* stream, dbsa_layout** out) {
   if (first_group < 0) return DBSA_ERR_INVALID_ARG;
   return build_layout(pool, nullptr, first_group, block_m, block_n, flags, stream, out);
+}
+
+int dbsa_layout_build_chunk(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t n_q_heads, int32_t n_kv_heads,
+                            const int32_t* own_tokens, int32_t flags, void* stream, dbsa_layout** out) {
+  return build_layout_with(flags, stream, out, [&](dbsa_layout* L) {
+    return dbsa_build_chunk_lists(pool, sel, n_q_heads, n_kv_heads, own_tokens, L);
+  });
+}
+
+int dbsa_layout_export_chunk(const dbsa_layout* L, int32_t* rows, const int32_t** worker_ptr, int32_t* n_workers,
+                             const int32_t** records, const int32_t** tokens, const int32_t** tiles, const int32_t** part_ptr,
+                             const int32_t** parts) {
+  if (!L || !L->chunk_stage) return DBSA_ERR_INVALID_ARG;
+  if (rows) *rows = L->ck_rows;
+  if (worker_ptr) *worker_ptr = L->ck_ptr.data();
+  if (n_workers) *n_workers = L->ck_workers;
+  if (records) *records = L->ck_rec.data();
+  if (tokens) *tokens = L->ck_toks.data();
+  if (tiles) *tiles = L->ck_ent.data();
+  if (part_ptr) *part_ptr = L->ck_tok_ptr.data();
+  if (parts) *parts = L->ck_tok_part.data();
+  return DBSA_OK;
 }
 
 int dbsa_layout_export(const dbsa_layout* L, const int32_t** qtile_tab, int64_t* n_qtiles, const int64_t** list_ptr,
@@ -886,7 +934,7 @@ int dbsa_layout_export_order(const dbsa_layout* L, const int32_t** order, int64_
 
 int dbsa_layout_export_schedule(const dbsa_layout* L, int32_t n_classes, const int32_t** class_ptr,
                                 const int32_t** records) {
-  if (!L || n_classes < 1 || n_classes > kMaxSchedClasses) return DBSA_ERR_INVALID_ARG;
+  if (!L || L->chunk_stage || n_classes < 1 || n_classes > kMaxSchedClasses) return DBSA_ERR_INVALID_ARG;
   std::lock_guard<std::mutex> lock(L->sched_mutex);
   if (L->sched_classes != 0 && L->sched_classes != n_classes) return DBSA_ERR_INVALID_ARG;
   if (L->sched_classes == 0) {
@@ -951,6 +999,10 @@ void dbsa_layout_destroy(dbsa_layout* L) {
 }
 
 size_t dbsa_workspace_bytes(const dbsa_layout* L, int32_t n_q_heads, int32_t head_dim) {
+  if (L && L->chunk_stage)
+    return n_q_heads == L->ck_q_heads && head_dim > 0
+               ? static_cast<size_t>(L->ck_part_rows) * n_q_heads * (head_dim + kPartialPad) * sizeof(float)
+               : 0;
   if (!L || !L->query_stage || n_q_heads <= 0 || head_dim <= 0) return 0;
   return std::max(decode_workspace_bytes(L, n_q_heads, head_dim),
                   query_prefill_states(L, n_q_heads, head_dim) * (head_dim + kPartialPad) * sizeof(float));
@@ -1113,6 +1165,158 @@ int dbsa_decode_attn_rope(const dbsa_layout* L, dbsa_tensor q_step, dbsa_tensor 
   return decode_common(L, q_step, k_selfcache, v_selfcache, self_len, stride_query, k_pool, v_pool, o, dtype,
                        n_q_heads, n_kv_heads, head_dim, softmax_scale, workspace, workspace_bytes, stream, rope_table,
                        rope_n_pos);
+}
+
+namespace {
+// what the 8-bit cache takes: rows of bytes in 16-byte pieces
+bool cache_ok(const dbsa_tensor& t) {
+  return t.ptr != nullptr && reinterpret_cast<uintptr_t>(t.ptr) % 16 == 0 && t.stride_tok > 0 && t.stride_head > 0 &&
+         t.stride_tok % 16 == 0 && t.stride_head % 16 == 0;
+}
+
+int chunk_common(const dbsa_layout* L, dbsa_tensor q, dbsa_tensor k_pool, dbsa_tensor v_pool, const dbsa_pages* own,
+                 const int32_t* self_len, const float* k_scale, const float* v_scale, dbsa_tensor o, float* lse,
+                 ChunkKind kind, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float softmax_scale,
+                 void* workspace, size_t workspace_bytes, void* stream) {
+  if (!L || !L->chunk_stage || !own || !own->table || !self_len) return DBSA_ERR_INVALID_ARG;
+  const int dtype = kind == ChunkKind::kF32 ? DBSA_F32 : DBSA_BF16;
+  if (int rc = check_shapes(dtype, n_q_heads, n_kv_heads, head_dim, softmax_scale)) return rc;
+  if (n_q_heads != L->ck_q_heads || n_kv_heads != L->ck_kv_heads) return DBSA_ERR_INVALID_ARG;
+  if (!tensor_ok(q, dtype) || !tensor_ok(o, dtype)) return DBSA_ERR_INVALID_ARG;
+  const bool bytes = kind == ChunkKind::kE4m3;
+  if (bytes && (!k_scale || !v_scale)) return DBSA_ERR_INVALID_ARG;
+  for (const dbsa_tensor& t : {k_pool, v_pool, own->k, own->v})
+    if (!(bytes ? cache_ok(t) : tensor_ok(t, dtype))) return DBSA_ERR_INVALID_ARG;
+  const int64_t piece = bytes ? 16 : dtype == DBSA_BF16 ? 8 : 4;
+  if (own->stride_page <= 0 || own->stride_page % piece != 0 || own->n_pages < 1 || own->table_stride < 1) return DBSA_ERR_INVALID_ARG;
+  if (own->page_tokens < 16 || (own->page_tokens & (own->page_tokens - 1)) != 0) return DBSA_ERR_UNSUPPORTED;
+  // rows of the pages and own keys are counted in 32 bits
+  if (int64_t{own->n_pages} * own->page_tokens > INT32_MAX - 2 * kChunkTile) return DBSA_ERR_UNSUPPORTED;
+  ChunkParams p{};
+  p.page_log2 = __builtin_ctz(static_cast<unsigned>(own->page_tokens));
+  p.own_capacity = static_cast<int32_t>(std::min<int64_t>(int64_t{own->table_stride} * own->page_tokens, INT32_MAX - 2 * kChunkTile));
+  p.merge = L->ck_part_rows > 0 ? 1 : 0;
+  const size_t need = static_cast<size_t>(L->ck_part_rows) * n_q_heads * (head_dim + kPartialPad) * sizeof(float);
+  if (need > 0 && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
+    return DBSA_ERR_WORKSPACE;
+  if (!L->on_device) return DBSA_ERR_INVALID_ARG;
+  p.rec = L->dev.ck_rec;
+  p.ptr = L->dev.ck_ptr;
+  p.toks = L->dev.ck_toks;
+  p.ent = L->dev.ck_ent;
+  p.tok_ptr = L->dev.ck_tok_ptr;
+  p.tok_part = L->dev.ck_tok_part;
+  p.q = view(q);
+  p.o = view(o);
+  p.k_pool = view(k_pool);
+  p.v_pool = view(v_pool);
+  p.k_own = view(own->k);
+  p.v_own = view(own->v);
+  p.stride_page = own->stride_page;
+  p.page_table = own->table;
+  p.table_stride = own->table_stride;
+  p.n_pages = own->n_pages;
+  p.self_len = self_len;
+  p.k_scale = bytes ? k_scale : nullptr;
+  p.v_scale = bytes ? v_scale : nullptr;
+  p.lse = lse;
+  p.partial = static_cast<float*>(workspace);
+  p.n_rows = L->n_query_tokens;
+  p.n_q_heads = n_q_heads;
+  p.n_kv_heads = n_kv_heads;
+  p.n_workers = L->ck_workers;
+  p.rows = L->ck_rows;
+  p.scale_log2e = softmax_scale * 1.4426950408889634f;
+  if (order_behind_upload(L, static_cast<hipStream_t>(stream)) != hipSuccess) return DBSA_ERR_HIP;
+  return launch_chunk_attn(p, head_dim, kind, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
+}
+
+// The checks the three calls on 8-bit caches share.  writes / reads: the call touches cache rows.
+int kv8_common(Kv8Params& p, dbsa_tensor k, dbsa_tensor v, const dbsa_tensor* k8, const dbsa_tensor* v8, int32_t n_tokens,
+               const int32_t* rows, int64_t first_row, int64_t n_rows, const float* k_scale, const float* v_scale,
+               int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const int32_t* positions, int32_t first_id,
+               const float* table, int32_t n_pos) {
+  if (dtype != DBSA_BF16 && dtype != DBSA_F32) return DBSA_ERR_UNSUPPORTED;
+  if (head_dim != 64 && head_dim != 128) return DBSA_ERR_UNSUPPORTED;
+  if (n_tokens < 0 || n_kv_heads < 1 || !k_scale || !v_scale) return DBSA_ERR_INVALID_ARG;
+  // (a launch counts its threads, at most 8 per token and head, in workgroups of 256)
+  if (int64_t{n_tokens} * n_kv_heads > (int64_t{1} << 34)) return DBSA_ERR_UNSUPPORTED;
+  if (n_tokens > 0 && (!tensor_ok(k, dtype) || !tensor_ok(v, dtype))) return DBSA_ERR_INVALID_ARG;
+  if (k8) {
+    if (!cache_ok(*k8) || !cache_ok(*v8) || n_rows < 1) return DBSA_ERR_INVALID_ARG;
+    if (!rows && (first_row < 0 || first_row > n_rows - n_tokens)) return DBSA_ERR_INVALID_ARG;
+    p.k8 = view(*k8);
+    p.v8 = view(*v8);
+  }
+  if (table) {
+    if (n_pos < 1 || reinterpret_cast<uintptr_t>(table) % 16 != 0) return DBSA_ERR_INVALID_ARG;
+    // ids the host can see must lie inside the table (ids read from `positions` are clamped by the kernels)
+    if (!positions && (first_id < 0 || int64_t{first_id} + n_tokens > n_pos)) return DBSA_ERR_INVALID_ARG;
+  }
+  p.k = view(k);
+  p.v = view(v);
+  p.k_scale = const_cast<float*>(k_scale);
+  p.v_scale = const_cast<float*>(v_scale);
+  p.rows = rows;
+  p.first_row = first_row;
+  p.n_cache_rows = n_rows;
+  p.table = table;
+  p.positions = positions;
+  p.first_id = first_id;
+  p.n_pos = n_pos;
+  p.n_tokens = n_tokens;
+  p.n_kv_heads = n_kv_heads;
+  p.head_dim = head_dim;
+  return DBSA_OK;
+}
+}  // namespace
+
+int dbsa_chunk_attn(const dbsa_layout* layout, dbsa_tensor q, dbsa_tensor k_pool, dbsa_tensor v_pool, const dbsa_pages* own,
+                    const int32_t* self_len, dbsa_tensor o, float* lse, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads,
+                    int32_t head_dim, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream) {
+  if (dtype != DBSA_BF16 && dtype != DBSA_F32) return DBSA_ERR_UNSUPPORTED;
+  return chunk_common(layout, q, k_pool, v_pool, own, self_len, nullptr, nullptr, o, lse,
+                      dtype == DBSA_F32 ? ChunkKind::kF32 : ChunkKind::kBf16, n_q_heads, n_kv_heads, head_dim, softmax_scale,
+                      workspace, workspace_bytes, stream);
+}
+
+int dbsa_chunk_attn_kv8(const dbsa_layout* layout, dbsa_tensor q, dbsa_tensor k_pool8, dbsa_tensor v_pool8,
+                        const dbsa_pages* own8, const int32_t* self_len, const float* k_scale, const float* v_scale,
+                        dbsa_tensor o, float* lse, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                        float softmax_scale, void* workspace, size_t workspace_bytes, void* stream) {
+  return chunk_common(layout, q, k_pool8, v_pool8, own8, self_len, k_scale, v_scale, o, lse, ChunkKind::kE4m3, n_q_heads,
+                      n_kv_heads, head_dim, softmax_scale, workspace, workspace_bytes, stream);
+}
+
+int dbsa_kv8_scales(dbsa_tensor k, dbsa_tensor v, int32_t n_tokens, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                    const int32_t* positions, int32_t first_id, const float* rope_table, int32_t rope_n_pos, int32_t running,
+                    float* k_scale, float* v_scale, void* stream) {
+  Kv8Params p{};
+  if (int rc = kv8_common(p, k, v, nullptr, nullptr, n_tokens, nullptr, 0, 0, k_scale, v_scale, n_kv_heads, head_dim, dtype,
+                          positions, first_id, rope_table, rope_n_pos))
+    return rc;
+  return launch_kv8_scales(p, dtype == DBSA_BF16, running != 0, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
+}
+
+int dbsa_kv8_write(dbsa_tensor k, dbsa_tensor v, int32_t n_tokens, const int32_t* rows, int64_t first_row, dbsa_tensor k_cache8,
+                   dbsa_tensor v_cache8, int64_t n_rows, const float* k_scale, const float* v_scale, int32_t n_kv_heads,
+                   int32_t head_dim, int32_t dtype, const int32_t* positions, int32_t first_id, const float* rope_table,
+                   int32_t rope_n_pos, void* stream) {
+  Kv8Params p{};
+  if (int rc = kv8_common(p, k, v, &k_cache8, &v_cache8, n_tokens, rows, first_row, n_rows, k_scale, v_scale, n_kv_heads,
+                          head_dim, dtype, positions, first_id, rope_table, rope_n_pos))
+    return rc;
+  return launch_kv8_write(p, dtype == DBSA_BF16, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
+}
+
+int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, const int32_t* rows, int64_t first_row,
+                  int32_t n_tokens, const float* k_scale, const float* v_scale, dbsa_tensor k, dbsa_tensor v,
+                  int32_t n_kv_heads, int32_t head_dim, int32_t dtype, void* stream) {
+  Kv8Params p{};
+  if (int rc = kv8_common(p, k, v, &k_cache8, &v_cache8, n_tokens, rows, first_row, n_rows, k_scale, v_scale, n_kv_heads,
+                          head_dim, dtype, nullptr, 0, nullptr, 0))
+    return rc;
+  return launch_kv8_read(p, dtype == DBSA_BF16, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
 }
 
 }  // extern "C"

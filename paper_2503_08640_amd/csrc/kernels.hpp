@@ -122,3 +122,42 @@ hipError_t launch_rope_apply(const TensorView& x, const TensorView& out, int n_t
 // fp32-arithmetic kernel for fp32 or bf16 storage (attn_plain.hip); compute_units: of the device the layout was built for
 hipError_t launch_prefill_plain(const AttnParams& p, int head_dim, bool bf16_storage, int compute_units, hipStream_t stream);
 hipError_t launch_decode_plain(const AttnParams& p, int head_dim, bool bf16_storage, int compute_units, hipStream_t stream);
+
+// Chunk attention (chunk_attn.hip) over the plan of a chunk layout (layout.hpp: ck_*).
+struct ChunkParams {
+  const int32_t *rec, *ptr, *toks, *ent, *tok_ptr, *tok_part;  // device
+  TensorView q, o;            // [new tokens, Hq, D]
+  TensorView k_pool, v_pool;  // [rows, Hkv, D]
+  TensorView k_own, v_own;    // a page: [page tokens, Hkv, D]; pages stride_page elements apart
+  int64_t stride_page;
+  const int32_t* page_table;  // device [B][table_stride]
+  int32_t table_stride, n_pages, page_log2;
+  int32_t own_capacity;       // most own keys a question's table row reaches
+  const int32_t* self_len;    // device [B]
+  const float *k_scale, *v_scale;  // 8-bit caches: device [Hkv]; else null
+  float* lse;                 // optional [Hq][n_rows]
+  float* partial;             // [partial row][Hq][D + kPartialPad]
+  int32_t n_rows;             // new tokens
+  int32_t n_q_heads, n_kv_heads, n_workers, rows;
+  int32_t merge;              // 1: some records leave partial states
+  float scale_log2e;
+};
+enum class ChunkKind { kBf16, kF32, kE4m3 };
+hipError_t launch_chunk_attn(const ChunkParams& p, int head_dim, ChunkKind kind, hipStream_t stream);
+
+// 8-bit caches (kv8.hip).  rows: device row of each token, or null for first_row + token; a null table leaves the keys as
+// they are, else token t is rotated at positions[t], or at first_id + t.
+struct Kv8Params {
+  TensorView k, v;    // [tokens, Hkv, D] bf16 or fp32
+  TensorView k8, v8;  // [cache rows, Hkv, D] e4m3 bytes
+  float *k_scale, *v_scale;
+  const int32_t* rows;
+  int64_t first_row, n_cache_rows;
+  const float* table;
+  const int32_t* positions;
+  int32_t first_id, n_pos;
+  int32_t n_tokens, n_kv_heads, head_dim;
+};
+hipError_t launch_kv8_scales(const Kv8Params& p, bool bf16, bool running, hipStream_t stream);
+hipError_t launch_kv8_write(const Kv8Params& p, bool bf16, hipStream_t stream);
+hipError_t launch_kv8_read(const Kv8Params& p, bool bf16, hipStream_t stream);

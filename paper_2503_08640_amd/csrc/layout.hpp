@@ -56,6 +56,13 @@ struct dbsa_device_lists {
   void* mx_uploaded = nullptr;
   void* mx_stream = nullptr;
   bool mx_landed = false;
+  // chunk attention (dbsa_layout::ck_*)
+  int32_t* ck_rec = nullptr;      // [n_records][12]
+  int32_t* ck_ptr = nullptr;      // [ck_workers + 1]
+  int32_t* ck_toks = nullptr;
+  int32_t* ck_ent = nullptr;      // [n_ent][2]
+  int32_t* ck_tok_ptr = nullptr;  // [n_query_tokens + 1]
+  int32_t* ck_tok_part = nullptr;
   // ordering of the asynchronous upload against the calls that read the lists (HIP handles kept
   // as plain pointers so that host-only code can include this header)
   void* upload_stream = nullptr;  // stream the lists were copied on
@@ -64,6 +71,7 @@ struct dbsa_device_lists {
 
 struct dbsa_layout {
   bool query_stage = false;
+  bool chunk_stage = false;  // built by dbsa_layout_build_chunk: the ck_* members alone
   bool on_device = false;
   int32_t block_m = 0, block_n = 0;
   int32_t sink_len = 0, n_tokens = 0, n_groups = 0, prev_window = 0;
@@ -134,6 +142,17 @@ struct dbsa_layout {
   // compute units of the device the launches are sized for (set before the host lists are built;
   // 256 when the layout is built without a device)
   int32_t compute_units = 256;
+
+  // Plan of the chunk attention (chunk_plan.cpp) for ck_q_heads / ck_kv_heads heads and workgroups of ck_rows rows.
+  // Worker c of a KV head takes records ck_ptr[c] .. ck_ptr[c+1]-1 of ck_rec, twelve words each:
+  //   0 first token in ck_toks, 1 tokens, 2 first pool tile in ck_ent, 3 pool tiles,
+  //   4 question whose own keys follow (-1: none), 5 / 6 first tile of them and the one behind the last, out of 7 expected
+  //   tiles (the device scales them to the tiles there are), 8 first partial row (-1: the record finishes its rows),
+  //   9 / 10 first new token and new tokens of that question
+  // Partial row p + i of a record is its token i's.  Token t's partial rows: ck_tok_part[ck_tok_ptr[t] ..].
+  int32_t ck_q_heads = 0, ck_kv_heads = 0, ck_rows = 0, ck_workers = 0;
+  int64_t ck_part_rows = 0;
+  std::vector<int32_t> ck_rec, ck_ptr, ck_toks, ck_ent, ck_tok_ptr, ck_tok_part;
 
   // Schedule of a persistent prefill-shaped launch for n_classes workers (dbsa_balance_schedule),
   // computed by the first call that needs one and kept: class c walks records
@@ -216,3 +235,13 @@ bool dbsa_crowd_worth(const dbsa_layout* L, int64_t classes, bool cuts);
 // first_group < 0: every segment; >= 0 (pre-encode only): Q tiles of groups first_group.. alone
 int dbsa_build_host_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t first_group, int32_t block_m, int32_t block_n,
                           dbsa_layout* L);
+
+// Chunk attention: keys of a tile, rows of a workgroup and workgroups a compute unit holds for a number of rows wanted,
+// and the plan (fills the ck_* members; own_tokens: expected own keys per question or null).
+constexpr int32_t kChunkTile = 64, kChunkWords = 12;
+struct ChunkShape {
+  int32_t rows, per_cu;
+};
+ChunkShape dbsa_chunk_shape(int32_t rows);
+int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t n_q_heads, int32_t n_kv_heads,
+                           const int32_t* own_tokens, dbsa_layout* L);
