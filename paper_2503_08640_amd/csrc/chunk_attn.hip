@@ -97,12 +97,14 @@ struct Chunk {
   static constexpr int kRowBytes = kD * Kind<T>::kBytes, kTileBytes = kBN * kRowBytes;  // as staged
   static constexpr int kSlots = kRowBytes / 16;                                         // 16-byte places of a staged row
   static constexpr int kPieces = kD * Kind<T>::kStoredBytes / 16;                       // 16-byte pieces of a stored row
-  static constexpr int kLoads = kBN * kPieces / kThreads;                               // pieces per thread and operand
+  static constexpr int kOperand = kBN * kPieces;                                        // pieces of K, and of V, of a step
+  static constexpr int kLoads = 2 * kOperand / kThreads;                                // pieces per thread
+  static constexpr bool kApart = kOperand < kThreads;                                   // half the waves fetch K, half V
   static constexpr int kKeyBlocks = kBN / 32, kChBlocks = kD / 32;
   static constexpr int kStages = 2;
   static constexpr int kLds = kStages * (2 * kTileBytes + kNW * 8);  // tiles, and each wave's mask of poisoned rows
   static_assert(kPieces <= 32 && 64 % kPieces == 0, "a stored row is fetched by neighbouring lanes of one wave");
-  static_assert(kBN * kPieces % kThreads == 0, "whole pieces per thread");
+  static_assert(kApart ? kOperand * 2 == kThreads : kOperand % kThreads == 0, "whole pieces per thread");
   // K places: xor by row, so that the 16 rows a quarter wave reads of one column lie on different banks; V rows of 16-bit
   // elements are read transposed, four rows at a time (as in attn_prefill64.hip), V rows of fp32 element by element, the two
   // half-waves four rows apart.
@@ -114,7 +116,7 @@ struct Chunk {
 };
 
 template <typename T, int kD, int kNW, int kRB, int kBN>
-__global__ __launch_bounds__(64 * kNW, 1) void chunk_attn_kernel(ChunkParams p) {
+__global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) {
   typedef Chunk<T, kD, kNW, kRB, kBN> C;
   typedef typename C::Q Q;
   constexpr bool kF32 = Kind<T>::kBytes == 4;
@@ -137,6 +139,11 @@ __global__ __launch_bounds__(64 * kNW, 1) void chunk_attn_kernel(ChunkParams p) 
   const unsigned char* const vpool = static_cast<const unsigned char*>(p.v_pool.ptr) + hk * p.v_pool.stride_head * Kind<T>::kStoredBytes;
   const unsigned char* const kown = static_cast<const unsigned char*>(p.k_own.ptr) + hk * p.k_own.stride_head * Kind<T>::kStoredBytes;
   const unsigned char* const vown = static_cast<const unsigned char*>(p.v_own.ptr) + hk * p.v_own.stride_head * Kind<T>::kStoredBytes;
+
+  const int64_t kpool_stride = p.k_pool.stride_tok * Kind<T>::kStoredBytes, vpool_stride = p.v_pool.stride_tok * Kind<T>::kStoredBytes;
+  // this thread's first piece of a whole step
+  const int64_t k_lane = (tid % C::kOperand / C::kPieces) * kpool_stride + (tid % C::kPieces) * 16;
+  const int64_t v_lane = (tid % C::kOperand / C::kPieces) * vpool_stride + (tid % C::kPieces) * 16;
 
   int stage = 0;
   const int rec_end = p.ptr[worker + 1];
@@ -185,11 +192,11 @@ __global__ __launch_bounds__(64 * kNW, 1) void chunk_attn_kernel(ChunkParams p) 
 
     // ---- the stream of steps ----
     // raw: what a step hangs off (its list entry, or the page of this lane's key), requested two steps ahead
-    struct Raw {
+    struct Ahead {
       int start, len, page;
     };
     auto fetch = [&](int s) DBSA_INLINE {
-      Raw x{0, 0, -1};
+      Ahead x{0, 0, -1};
       if (s < pool_steps) {
         const int32_t* const e = p.ent + 2 * static_cast<int64_t>(ent_begin + s / (kChunkTile / kBN));
         x.start = e[0];
@@ -206,7 +213,7 @@ __global__ __launch_bounds__(64 * kNW, 1) void chunk_attn_kernel(ChunkParams p) 
       bool own, whole;  // whole: every row sees all kBN keys
       int first, len;   // pool: keys; own: index of the first key
     };
-    auto place = [&](int s, const Raw& x) DBSA_INLINE {
+    auto place = [&](int s, const Ahead& x) DBSA_INLINE {
       Keys k;
       k.own = s >= pool_steps;
       if (!k.own) {
@@ -224,24 +231,33 @@ __global__ __launch_bounds__(64 * kNW, 1) void chunk_attn_kernel(ChunkParams p) 
       }
       return k;
     };
-    uintx4 kreg[C::kLoads], vreg[C::kLoads];
+    // This thread's pieces of a step: piece tid + i threads of K, then of V; the operand of piece i is the wave's.
+    uintx4 raw[C::kLoads];
+    auto is_v = [&](int i) DBSA_INLINE { return C::kApart ? wave >= kNW / 2 : i >= C::kLoads / 2; };
+    auto piece_row = [&](int i) DBSA_INLINE { return (tid + i * C::kThreads) % C::kOperand / C::kPieces; };
     auto load = [&](const Keys& k) DBSA_INLINE {
-      const unsigned char* const kb = k.own ? kown : kpool;
-      const unsigned char* const vb = k.own ? vown : vpool;
-      const int64_t ks = (k.own ? p.k_own.stride_tok : p.k_pool.stride_tok) * Kind<T>::kStoredBytes;
-      const int64_t vs = (k.own ? p.v_own.stride_tok : p.v_pool.stride_tok) * Kind<T>::kStoredBytes;
+      if (!k.own && k.whole) {
+        const int64_t first = __builtin_amdgcn_readfirstlane(k.row);
+#pragma unroll
+        for (int i = 0; i < C::kLoads; ++i) {
+          const unsigned char* const base = is_v(i) ? vpool : kpool;
+          const int64_t stride = is_v(i) ? vpool_stride : kpool_stride;
+          const int row0 = i * C::kThreads % C::kOperand / C::kPieces;  // (whole rows per pass of the threads)
+          raw[i] = *reinterpret_cast<const uintx4*>(base + (first + row0) * stride + (is_v(i) ? v_lane : k_lane));
+        }
+        return;
+      }
       const int shift = k.own ? p.page_log2 : 31;
-      const int64_t page_bytes = p.stride_page * Kind<T>::kStoredBytes;
 #pragma unroll
       for (int i = 0; i < C::kLoads; ++i) {
-        const int piece = tid + i * C::kThreads;
-        const int row = __shfl(k.row, piece / C::kPieces);
-        const int at = (piece % C::kPieces) * 16;
-        kreg[i] = vreg[i] = uintx4{0, 0, 0, 0};
+        const unsigned char* const base = k.own ? (is_v(i) ? vown : kown) : (is_v(i) ? vpool : kpool);
+        const int64_t stride = k.own ? (is_v(i) ? p.v_own.stride_tok : p.k_own.stride_tok) * Kind<T>::kStoredBytes
+                                     : (is_v(i) ? vpool_stride : kpool_stride);
+        const int row = __shfl(k.row, piece_row(i));
+        raw[i] = uintx4{0, 0, 0, 0};
         if (row >= 0) {
-          const int64_t page = row >> shift, in = row - (static_cast<int64_t>(page) << shift);
-          kreg[i] = *reinterpret_cast<const uintx4*>(kb + page * page_bytes + in * ks + at);
-          vreg[i] = *reinterpret_cast<const uintx4*>(vb + page * page_bytes + in * vs + at);
+          const int64_t page = row >> shift, in = row - (page << shift);
+          raw[i] = *reinterpret_cast<const uintx4*>(base + page * p.stride_page * Kind<T>::kStoredBytes + in * stride + (tid % C::kPieces) * 16);
         }
       }
     };
@@ -250,37 +266,32 @@ __global__ __launch_bounds__(64 * kNW, 1) void chunk_attn_kernel(ChunkParams p) 
     uint64_t* const poison = reinterpret_cast<uint64_t*>(smem + C::kStages * 2 * C::kTileBytes);
     auto take_poison = [&](int st) DBSA_INLINE {
       uint64_t mask = 0;
+      constexpr uint64_t kRowLanes = (1ull << C::kPieces) - 1;
 #pragma unroll
       for (int i = 0; i < C::kLoads; ++i) {
-        const uint64_t bad = __builtin_amdgcn_ballot_w64(not_finite<T>(vreg[i]));
+        if (!is_v(i)) continue;
+        const uint64_t bad = __builtin_amdgcn_ballot_w64(not_finite<T>(raw[i]));
         if (bad == 0) continue;
-        const uint64_t row_lanes = C::kPieces == 64 ? ~0ull : (1ull << C::kPieces) - 1;
+        const int row0 = (64 * wave + i * C::kThreads) % C::kOperand / C::kPieces;
         for (int rr = 0; rr < 64 / C::kPieces; ++rr)
-          if ((bad >> (rr * C::kPieces)) & row_lanes) mask |= 1ull << ((64 * wave + i * C::kThreads) / C::kPieces + rr);
-        if ((bad >> (lane / C::kPieces * C::kPieces)) & row_lanes) vreg[i] = uintx4{0, 0, 0, 0};
+          if ((bad >> (rr * C::kPieces)) & kRowLanes) mask |= 1ull << (row0 + rr);
+        if ((bad >> (lane / C::kPieces * C::kPieces)) & kRowLanes) raw[i] = uintx4{0, 0, 0, 0};
       }
       if (lane == 0) poison[st * kNW + wave] = mask;
     };
     auto store = [&](int st) DBSA_INLINE {
-      unsigned char* const kt = smem + st * 2 * C::kTileBytes;
-      unsigned char* const vt = kt + C::kTileBytes;
 #pragma unroll
       for (int i = 0; i < C::kLoads; ++i) {
-        const int piece = tid + i * C::kThreads;
-        const int row = piece / C::kPieces, col = piece % C::kPieces;
-        unsigned char* const kr = kt + row * C::kRowBytes;
-        unsigned char* const vr = vt + row * C::kRowBytes;
+        const int row = piece_row(i), col = tid % C::kPieces;
+        unsigned char* const at = smem + (2 * st + (is_v(i) ? 1 : 0)) * C::kTileBytes + row * C::kRowBytes;
+        const int swizzle = is_v(i) ? C::v_swizzle(row) : C::k_swizzle(row);
         if constexpr (Kind<T>::kStoredBytes == 1) {
           uintx4 lo, hi;
-          widen16(kreg[i], lo, hi);
-          *reinterpret_cast<uintx4*>(kr + ((2 * col) ^ C::k_swizzle(row)) * 16) = lo;
-          *reinterpret_cast<uintx4*>(kr + ((2 * col + 1) ^ C::k_swizzle(row)) * 16) = hi;
-          widen16(vreg[i], lo, hi);
-          *reinterpret_cast<uintx4*>(vr + ((2 * col) ^ C::v_swizzle(row)) * 16) = lo;
-          *reinterpret_cast<uintx4*>(vr + ((2 * col + 1) ^ C::v_swizzle(row)) * 16) = hi;
+          widen16(raw[i], lo, hi);
+          *reinterpret_cast<uintx4*>(at + ((2 * col) ^ swizzle) * 16) = lo;
+          *reinterpret_cast<uintx4*>(at + ((2 * col + 1) ^ swizzle) * 16) = hi;
         } else {
-          *reinterpret_cast<uintx4*>(kr + (col ^ C::k_swizzle(row)) * 16) = kreg[i];
-          *reinterpret_cast<uintx4*>(vr + (col ^ C::v_swizzle(row)) * 16) = vreg[i];
+          *reinterpret_cast<uintx4*>(at + (col ^ swizzle) * 16) = raw[i];
         }
       }
     };
@@ -456,7 +467,7 @@ __global__ __launch_bounds__(64 * kNW, 1) void chunk_attn_kernel(ChunkParams p) 
       }
     };
 
-    Raw next{};
+    Ahead next{};
     Keys cur{}, ahead{};
     if (steps > 0) {
       ahead = place(0, fetch(0));
@@ -580,7 +591,7 @@ hipError_t launch_kind(const ChunkParams& p, hipStream_t stream) {
   if (p.rows == 32) e = launch_shape<T, kD, 1, 1, 32>(p, stream);
   else if (p.rows == 64) e = launch_shape<T, kD, 2, 1, 32>(p, stream);
   else if (p.rows == 128) e = launch_shape<T, kD, 4, 1, kWide>(p, stream);
-  else if (p.rows == 256) e = launch_shape<T, kD, 4, 2, kWide>(p, stream);
+  else if (p.rows == 256) e = launch_shape<T, kD, 8, 1, kWide>(p, stream);
   if (e != hipSuccess || !p.merge) return e;
   const int64_t pairs = static_cast<int64_t>(p.n_rows) * p.n_q_heads;
   chunk_merge_kernel<typename Kind<T>::Q, kD><<<dim3(static_cast<unsigned>((pairs + 3) / 4)), dim3(256), 0, stream>>>(p);
