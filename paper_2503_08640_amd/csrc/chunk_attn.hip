@@ -89,11 +89,22 @@ __device__ DBSA_INLINE float stored_value(const unsigned char* row, int ch) {
   else return reinterpret_cast<const float*>(row)[ch];
 }
 
-// kBN keys per step (a 64-key tile is one or two steps), kNW waves of kRB blocks of 32 rows.
-template <typename T, int kD, int kNW, int kRB, int kBN>
+// kBN keys per step (a 64-key tile is one or two steps), kNW waves of 32 rows.
+//
+// kPingPong (eight waves, two to a SIMD): the waves form two groups half a step apart.  While one group multiplies
+// (O += V(t-1) P(t-1), then S(t) = K(t) Q: 32 matrix instructions), the other turns its scores into probabilities and
+// fills the stages, so that each SIMD's matrix pipe and vector ALU work at the same time on one wave each; a barrier ends
+// every phase.  Phases of group 0: M(0) S(0) M(1) S(1) ...; group 1 one phase later:
+//     phase 2t    : group 0 multiplies K(t), V(t-1); group 1 is at S(t-1) and stores its pieces of K(t+1), V(t+1)
+//     phase 2t + 1: group 1 multiplies K(t), V(t-1); group 0 is at S(t)   and stores its pieces of K(t+1), V(t+1)
+// K(t+1) takes the place of K(t-1), last read in phase 2t - 1; V(t+1) that of V(t-2), last read in phase 2t - 1: two stages of
+// K, three of V.
+template <typename T, int kD, int kNW, int kBN>
 struct Chunk {
   typedef typename Kind<T>::Q Q;
-  static constexpr int kThreads = 64 * kNW, kRows = 32 * kRB * kNW;
+  static constexpr bool kF32 = Kind<T>::kBytes == 4;
+  static constexpr bool kPingPong = kNW == 8 && !kF32;
+  static constexpr int kThreads = 64 * kNW, kRows = 32 * kNW;
   static constexpr int kRowBytes = kD * Kind<T>::kBytes, kTileBytes = kBN * kRowBytes;  // as staged
   static constexpr int kSlots = kRowBytes / 16;                                         // 16-byte places of a staged row
   static constexpr int kPieces = kD * Kind<T>::kStoredBytes / 16;                       // 16-byte pieces of a stored row
@@ -101,8 +112,9 @@ struct Chunk {
   static constexpr int kLoads = 2 * kOperand / kThreads;                                // pieces per thread
   static constexpr bool kApart = kOperand < kThreads;                                   // half the waves fetch K, half V
   static constexpr int kKeyBlocks = kBN / 32, kChBlocks = kD / 32;
-  static constexpr int kStages = 2;
-  static constexpr int kLds = kStages * (2 * kTileBytes + kNW * 8);  // tiles, and each wave's mask of poisoned rows
+  static constexpr int kKStages = 2, kVStages = kPingPong ? 3 : 2;
+  static constexpr int kPoisonAt = (kKStages + kVStages) * kTileBytes;  // each wave's mask of poisoned rows, per stage of V
+  static constexpr int kLds = kPoisonAt + kVStages * kNW * 8;
   static_assert(kPieces <= 32 && 64 % kPieces == 0, "a stored row is fetched by neighbouring lanes of one wave");
   static_assert(kApart ? kOperand * 2 == kThreads : kOperand % kThreads == 0, "whole pieces per thread");
   // K places: xor by row, so that the 16 rows a quarter wave reads of one column lie on different banks; V rows of 16-bit
@@ -110,17 +122,27 @@ struct Chunk {
   // half-waves four rows apart.
   __device__ static DBSA_INLINE int k_swizzle(int row) { return kSlots >= 16 ? row % 16 : (row / 2) % 8; }
   __device__ static DBSA_INLINE int v_swizzle(int row) {
-    if (Kind<T>::kBytes == 4) return 8 * ((row / 4) % 2);
+    if (kF32) return 8 * ((row / 4) % 2);
     return kSlots >= 16 ? 4 * (row % 4) : 4 * ((row / 2) % 2);
   }
 };
 
-template <typename T, int kD, int kNW, int kRB, int kBN>
+// The lane index counted anew, for rare blocks of the step loop: what they derive from it is then not kept in registers
+// through the loop.
+__device__ DBSA_INLINE int lane_here() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+  return x;
+}
+
+template <typename T, int kD, int kNW, int kBN>
 __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) {
-  typedef Chunk<T, kD, kNW, kRB, kBN> C;
+  typedef Chunk<T, kD, kNW, kBN> C;
   typedef typename C::Q Q;
-  constexpr bool kF32 = Kind<T>::kBytes == 4;
-  constexpr int kB = C::kKeyBlocks, kO = C::kChBlocks;
+  constexpr bool kF32 = C::kF32;
+  constexpr int kB = C::kKeyBlocks, kO = C::kChBlocks, kC = C::kSlots / 2;
+  constexpr int kSteps = kChunkTile / kBN;  // steps of a tile
+  constexpr int kEs = Kind<T>::kStoredBytes;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
 
   const int tid = threadIdx.x, lane = tid % 64, l32 = lane % 32, half = lane / 32;
@@ -133,72 +155,66 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
   if (p.k_scale) c2 *= p.k_scale[hk];
   const bool negate = c2 < 0.f;
   c2 = fmaxf(fabsf(c2), 1e-30f);
-  const float v_scale = p.v_scale ? p.v_scale[hk] : 1.f;
 
-  const unsigned char* const kpool = static_cast<const unsigned char*>(p.k_pool.ptr) + hk * p.k_pool.stride_head * Kind<T>::kStoredBytes;
-  const unsigned char* const vpool = static_cast<const unsigned char*>(p.v_pool.ptr) + hk * p.v_pool.stride_head * Kind<T>::kStoredBytes;
-  const unsigned char* const kown = static_cast<const unsigned char*>(p.k_own.ptr) + hk * p.k_own.stride_head * Kind<T>::kStoredBytes;
-  const unsigned char* const vown = static_cast<const unsigned char*>(p.v_own.ptr) + hk * p.v_own.stride_head * Kind<T>::kStoredBytes;
-
-  const int64_t kpool_stride = p.k_pool.stride_tok * Kind<T>::kStoredBytes, vpool_stride = p.v_pool.stride_tok * Kind<T>::kStoredBytes;
+  const unsigned char* const kpool = static_cast<const unsigned char*>(p.k_pool.ptr) + hk * p.k_pool.stride_head * kEs;
+  const unsigned char* const vpool = static_cast<const unsigned char*>(p.v_pool.ptr) + hk * p.v_pool.stride_head * kEs;
+  const int64_t kpool_stride = p.k_pool.stride_tok * kEs, vpool_stride = p.v_pool.stride_tok * kEs;
   // this thread's first piece of a whole step
   const int64_t k_lane = (tid % C::kOperand / C::kPieces) * kpool_stride + (tid % C::kPieces) * 16;
   const int64_t v_lane = (tid % C::kOperand / C::kPieces) * vpool_stride + (tid % C::kPieces) * 16;
+  // LDS addresses of fragments: K fragment (kb, c) is row 32 kb + l32, place 2 c + half; V fragment (16-bit: kb, ch, ob) keys
+  // 32 kb + 16 ch + 4 half + {0..3, 8..11}, the order the probabilities lie in, read transposed: lane j of 16 fetches four
+  // channels of one key and gets four keys of one channel.  (A place is xor-ed: base ^ (32 c), base ^ (64 ob).)
+  const int k_at = l32 * C::kRowBytes + ((half ^ C::k_swizzle(l32)) * 16);
+  const int v_at = (4 * half + (lane % 16) / 4) * C::kRowBytes +
+                   (((2 * (l32 / 16) + (lane % 4) / 2) ^ C::v_swizzle((lane % 16) / 4)) * 16) + (lane % 2) * 8;
 
-  int stage = 0;
+  int n_stored = 0;  // steps staged so far, over all records: their stages
   const int rec_end = p.ptr[worker + 1];
   for (int rec = p.ptr[worker]; rec < rec_end; ++rec) {
     const int32_t* const w = p.rec + rec * kChunkWords;
     const int tok_begin = w[0], n_tok = w[1], ent_begin = w[2], n_ent = w[3], own_u = w[4], part_base = w[8];
     const int cu = w[9], t_new = w[10];
 
-    // ---- rows ----
-    int row_tok[kRB], row_head[kRB], row_pos[kRB];
-    bool row_ok[kRB];
+    // ---- the row of this lane (both half-waves hold it) ----
     int own_n = 0;  // own keys there are
     if (own_u >= 0) own_n = min(max(p.self_len[own_u], 0), p.own_capacity);
-#pragma unroll
-    for (int rb = 0; rb < kRB; ++rb) {
-      const int i = (wave * kRB + rb) * 32 + l32;
-      const int t = i / r;
-      row_ok[rb] = t < n_tok;
-      row_tok[rb] = min(t, n_tok - 1);
-      row_head[rb] = hk * r + i % r;
-    }
+    const int row_index = wave * 32 + l32;
+    const bool row_ok = row_index / r < n_tok;
+    const int row_in = min(row_index / r, n_tok - 1);
+    const int row_tok = p.toks[tok_begin + row_in];
+    const int row_pos = own_n - t_new + (row_tok - cu);  // the row's own index: it sees own keys 0 .. row_pos
     typedef typename std::conditional<kF32, floatx4, bf16x8>::type Piece;
-    Piece qf[kRB][C::kSlots / 2];
+    Piece qf[kC];
+    {
+      const Q* const qp = static_cast<const Q*>(p.q.ptr) + row_tok * p.q.stride_tok + (hk * r + row_index % r) * p.q.stride_head;
 #pragma unroll
-    for (int rb = 0; rb < kRB; ++rb) {
-      const int tok = p.toks[tok_begin + row_tok[rb]];
-      row_pos[rb] = own_n - t_new + (tok - cu);  // the row's own index: it sees own keys 0 .. row_pos
-      const Q* const qp = static_cast<const Q*>(p.q.ptr) + tok * p.q.stride_tok + row_head[rb] * p.q.stride_head;
-#pragma unroll
-      for (int c = 0; c < C::kSlots / 2; ++c) {
-        qf[rb][c] = *reinterpret_cast<const Piece*>(qp + (2 * c + half) * (16 / static_cast<int>(sizeof(Q))));
-        if (negate) qf[rb][c] = -qf[rb][c];
+      for (int c = 0; c < kC; ++c) {
+        qf[c] = *reinterpret_cast<const Piece*>(qp + (2 * c + half) * (16 / static_cast<int>(sizeof(Q))));
+        if (negate) qf[c] = -qf[c];
       }
     }
     // own tiles of this record: its share of those up to the last token's own key
     int own_first = 0, own_steps = 0;
+    const int first_pos = own_n - t_new + (p.toks[tok_begin] - cu);  // (tokens of a question ascend)
     if (own_u >= 0) {
       const int last = own_n - t_new + (p.toks[tok_begin + n_tok - 1] - cu);
       const int64_t tiles = max(0, (last + kChunkTile) / kChunkTile);
       const int lo = static_cast<int>(w[5] * tiles / w[7]), hi = static_cast<int>(w[6] * tiles / w[7]);
       own_first = lo * kChunkTile;
-      own_steps = (hi - lo) * (kChunkTile / kBN);
+      own_steps = (hi - lo) * kSteps;
     }
-    const int first_pos = own_n - t_new + (p.toks[tok_begin] - cu);  // (tokens of a question ascend)
-    const int pool_steps = n_ent * (kChunkTile / kBN), steps = pool_steps + own_steps;
+    const int pool_steps = n_ent * kSteps, steps = pool_steps + own_steps;
 
     // ---- the stream of steps ----
-    // raw: what a step hangs off (its list entry, or the page of this lane's key), requested two steps ahead
+    // what a step hangs off (its list entry, or the page of this lane's key), requested one step before its rows
     struct Ahead {
       int start, len, page;
     };
     auto fetch = [&](int s) DBSA_INLINE {
       Ahead x{0, 0, -1};
       if (s < pool_steps) {
-        const int32_t* const e = p.ent + 2 * static_cast<int64_t>(ent_begin + s / (kChunkTile / kBN));
+        const int32_t* const e = p.ent + 2 * static_cast<int64_t>(ent_begin + s / kSteps);
         x.start = e[0];
         x.len = e[1];
       } else if (s < steps) {
@@ -207,66 +223,66 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       }
       return x;
     };
-    // a step's keys: row of this lane's key in the pool or in the pages (-1: nothing there), and what the rows see of them
+    // A step's keys: row of this lane's key in the pool or in the pages (-1: nothing there).  whole: every row sees all of them.
     struct Keys {
       int row;
-      bool own, whole;  // whole: every row sees all kBN keys
-      int first, len;   // pool: keys; own: index of the first key
+      bool own, whole;
     };
     auto place = [&](int s, const Ahead& x) DBSA_INLINE {
       Keys k;
       k.own = s >= pool_steps;
       if (!k.own) {
-        const int off = (s % (kChunkTile / kBN)) * kBN;
-        k.len = min((x.len & 0xFFFF) - off, kBN);
-        k.first = 0;
-        k.row = k.len > 0 ? x.start + off + min(lane, k.len - 1) : -1;
-        k.whole = k.len == kBN;
+        const int off = (s % kSteps) * kBN, len = min((x.len & 0xFFFF) - off, kBN);
+        k.row = len > 0 ? x.start + off + min(lane, len - 1) : -1;
+        k.whole = len == kBN;
       } else {
-        k.first = own_first + (s - pool_steps) * kBN;
-        k.len = kBN;
-        const int j = k.first + lane;
-        k.row = x.page >= 0 && x.page < p.n_pages ? (x.page << p.page_log2) + (j & ((1 << p.page_log2) - 1)) : -1;
-        k.whole = k.first + kBN - 1 <= first_pos && __builtin_amdgcn_ballot_w64(lane < kBN && k.row < 0) == 0;
+        const int first = own_first + (s - pool_steps) * kBN;
+        k.row = x.page >= 0 && x.page < p.n_pages ? (x.page << p.page_log2) + ((first + lane) & ((1 << p.page_log2) - 1)) : -1;
+        k.whole = first + kBN - 1 <= first_pos && __builtin_amdgcn_ballot_w64(lane < kBN && k.row < 0) == 0;
       }
       return k;
     };
     // This thread's pieces of a step: piece tid + i threads of K, then of V; the operand of piece i is the wave's.
     uintx4 raw[C::kLoads];
     auto is_v = [&](int i) DBSA_INLINE { return C::kApart ? wave >= kNW / 2 : i >= C::kLoads / 2; };
-    auto piece_row = [&](int i) DBSA_INLINE { return (tid + i * C::kThreads) % C::kOperand / C::kPieces; };
+    auto piece_row = [&](int i, int t) DBSA_INLINE { return (t + i * C::kThreads) % C::kOperand / C::kPieces; };
     auto load = [&](const Keys& k) DBSA_INLINE {
-      if (!k.own && k.whole) {
+      if (__builtin_expect(!k.own && k.whole, 1)) {
         const int64_t first = __builtin_amdgcn_readfirstlane(k.row);
 #pragma unroll
         for (int i = 0; i < C::kLoads; ++i) {
-          const unsigned char* const base = is_v(i) ? vpool : kpool;
-          const int64_t stride = is_v(i) ? vpool_stride : kpool_stride;
           const int row0 = i * C::kThreads % C::kOperand / C::kPieces;  // (whole rows per pass of the threads)
-          raw[i] = *reinterpret_cast<const uintx4*>(base + (first + row0) * stride + (is_v(i) ? v_lane : k_lane));
+          if (is_v(i)) raw[i] = *reinterpret_cast<const uintx4*>(vpool + (first + row0) * vpool_stride + v_lane);
+          else raw[i] = *reinterpret_cast<const uintx4*>(kpool + (first + row0) * kpool_stride + k_lane);
         }
         return;
       }
+      const int t = 64 * wave + lane_here();
       const int shift = k.own ? p.page_log2 : 31;
+      const unsigned char* const kb = static_cast<const unsigned char*>(k.own ? p.k_own.ptr : p.k_pool.ptr) +
+                                      hk * (k.own ? p.k_own.stride_head : p.k_pool.stride_head) * kEs;
+      const unsigned char* const vb = static_cast<const unsigned char*>(k.own ? p.v_own.ptr : p.v_pool.ptr) +
+                                      hk * (k.own ? p.v_own.stride_head : p.v_pool.stride_head) * kEs;
+      const int64_t ks = (k.own ? p.k_own.stride_tok : p.k_pool.stride_tok) * kEs;
+      const int64_t vs = (k.own ? p.v_own.stride_tok : p.v_pool.stride_tok) * kEs;
 #pragma unroll
       for (int i = 0; i < C::kLoads; ++i) {
-        const unsigned char* const base = k.own ? (is_v(i) ? vown : kown) : (is_v(i) ? vpool : kpool);
-        const int64_t stride = k.own ? (is_v(i) ? p.v_own.stride_tok : p.k_own.stride_tok) * Kind<T>::kStoredBytes
-                                     : (is_v(i) ? vpool_stride : kpool_stride);
-        const int row = __shfl(k.row, piece_row(i));
+        const int row = __shfl(k.row, piece_row(i, t));
         raw[i] = uintx4{0, 0, 0, 0};
         if (row >= 0) {
           const int64_t page = row >> shift, in = row - (page << shift);
-          raw[i] = *reinterpret_cast<const uintx4*>(base + page * p.stride_page * Kind<T>::kStoredBytes + in * stride + (tid % C::kPieces) * 16);
+          raw[i] = *reinterpret_cast<const uintx4*>((is_v(i) ? vb : kb) + page * p.stride_page * kEs + in * (is_v(i) ? vs : ks) +
+                                                    (t % C::kPieces) * 16);
         }
       }
     };
     // Where some rows do not see every key (the chunk's own diagonal), a non-finite value must not reach the others through
     // 0 * NaN: such rows of V are staged as zeros, and their keys added one by one to the rows that see them.
-    uint64_t* const poison = reinterpret_cast<uint64_t*>(smem + C::kStages * 2 * C::kTileBytes);
-    auto take_poison = [&](int st) DBSA_INLINE {
+    uint64_t* const poison = reinterpret_cast<uint64_t*>(smem + C::kPoisonAt);
+    auto take_poison = [&](int v_stage) DBSA_INLINE {
       uint64_t mask = 0;
       constexpr uint64_t kRowLanes = (1ull << C::kPieces) - 1;
+      const int ln = lane_here();
 #pragma unroll
       for (int i = 0; i < C::kLoads; ++i) {
         if (!is_v(i)) continue;
@@ -275,17 +291,17 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         const int row0 = (64 * wave + i * C::kThreads) % C::kOperand / C::kPieces;
         for (int rr = 0; rr < 64 / C::kPieces; ++rr)
           if ((bad >> (rr * C::kPieces)) & kRowLanes) mask |= 1ull << (row0 + rr);
-        if ((bad >> (lane / C::kPieces * C::kPieces)) & kRowLanes) raw[i] = uintx4{0, 0, 0, 0};
+        if ((bad >> (ln / C::kPieces * C::kPieces)) & kRowLanes) raw[i] = uintx4{0, 0, 0, 0};
       }
-      if (lane == 0) poison[st * kNW + wave] = mask;
+      if (ln == 0) poison[v_stage * kNW + wave] = mask;
     };
-    auto store = [&](int st) DBSA_INLINE {
+    auto store = [&](int k_stage, int v_stage) DBSA_INLINE {
 #pragma unroll
       for (int i = 0; i < C::kLoads; ++i) {
-        const int row = piece_row(i), col = tid % C::kPieces;
-        unsigned char* const at = smem + (2 * st + (is_v(i) ? 1 : 0)) * C::kTileBytes + row * C::kRowBytes;
+        const int row = piece_row(i, tid), col = tid % C::kPieces;
+        unsigned char* const at = smem + (is_v(i) ? C::kKStages + v_stage : k_stage) * C::kTileBytes + row * C::kRowBytes;
         const int swizzle = is_v(i) ? C::v_swizzle(row) : C::k_swizzle(row);
-        if constexpr (Kind<T>::kStoredBytes == 1) {
+        if constexpr (kEs == 1) {
           uintx4 lo, hi;
           widen16(raw[i], lo, hi);
           *reinterpret_cast<uintx4*>(at + ((2 * col) ^ swizzle) * 16) = lo;
@@ -295,129 +311,158 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         }
       }
     };
-
-    // ---- softmax state ----
-    floatx16 acc[kRB][kO];
-    float m[kRB], l[kRB];  // l: this lane's keys' share
-#pragma unroll
-    for (int rb = 0; rb < kRB; ++rb) {
-      m[rb] = -INFINITY;
-      l[rb] = 0.f;
-#pragma unroll
-      for (int ob = 0; ob < kO; ++ob)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[rb][ob][i] = 0.f;
-    }
-
-    // the keys that take_poison kept out of the product
-    auto add_poison = [&](const Keys& k, int st, floatx16 (&s)[kRB][kB]) DBSA_INLINE {
-      uint64_t mask = 0;
-#pragma unroll
-      for (int i = 0; i < kNW; ++i) mask |= poison[st * kNW + i];
-      mask = uniform64(mask);
-      while (mask) {
-        const int key = __builtin_ctzll(mask);
-        mask &= mask - 1;
-        const int row = __shfl(k.row, key);
-        const unsigned char* const v = vown + (row >> p.page_log2) * p.stride_page * Kind<T>::kStoredBytes +
-                                       (row & ((1 << p.page_log2) - 1)) * p.v_own.stride_tok * Kind<T>::kStoredBytes;
-#pragma unroll
-        for (int rb = 0; rb < kRB; ++rb) {
-          float mine = 0.f;  // the key's probability, in the half-wave that holds the key
-#pragma unroll
-          for (int kb = 0; kb < kB; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (key == 32 * kb + 8 * (i / 4) + 4 * half + i % 4) mine = s[rb][kb][i];
-          const float other = __shfl_xor(mine, 32);
-          const float prob = (key / 4) % 2 == half ? mine : other;
-#pragma unroll
-          for (int ob = 0; ob < kO; ++ob)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float x = stored_value<T>(v, 32 * ob + 8 * (i / 4) + 4 * half + i % 4);
-              if (prob != 0.f) acc[rb][ob][i] = fmaf(prob, x, acc[rb][ob][i]);
-            }
-        }
-      }
+    // Steps are staged in order: step s of the record is number base + s of the workgroup.  What its rows see is noted in a
+    // bit of `partly` (some row does not see some key) until its product is done: at most four steps are on their way.
+    const int base = n_stored;
+    uint32_t partly = 0;
+    Ahead next{};
+    bool raw_own_partly = false;  // the step in `raw`
+    auto request = [&](int s) DBSA_INLINE {  // s < steps: its entry is in `next`
+      const Keys k = place(s, next);
+      load(k);
+      const uint32_t bit = 1u << (s % 32);
+      partly = k.whole ? partly & ~bit : partly | bit;
+      raw_own_partly = k.own && !k.whole;
+      next = fetch(s + 1);
+    };
+    auto put = [&](int s) DBSA_INLINE {
+      const int v_stage = (base + s) % C::kVStages;
+      if (__builtin_expect(raw_own_partly, 0)) take_poison(v_stage);
+      store((base + s) % C::kKStages, v_stage);
     };
 
-    auto compute = [&](const Keys& k, int st) DBSA_INLINE {
-      const unsigned char* const kt = smem + st * 2 * C::kTileBytes;
-      const unsigned char* const vt = kt + C::kTileBytes;
-      floatx16 s[kRB][kB];
+    // ---- softmax state ----
+    floatx16 acc[kO];
+    float m = -INFINITY, l = 0.f;  // l: this lane's keys' share
 #pragma unroll
-      for (int rb = 0; rb < kRB; ++rb)
+    for (int ob = 0; ob < kO; ++ob)
 #pragma unroll
-        for (int kb = 0; kb < kB; ++kb)
+      for (int i = 0; i < 16; ++i) acc[ob][i] = 0.f;
+    floatx16 s[kB];                   // scores, then (fp32) probabilities
+    bf16x8 pf[kF32 ? 1 : kB][2];      // probabilities as operands of the product
+
+    auto scores = [&](int st) DBSA_INLINE {
+      const unsigned char* const kt = smem + (base + st) % C::kKStages * C::kTileBytes;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[rb][kb][i] = 0.f;
-      // scores: K fragment (kb, c) is row 32 kb + l32, place 2 c + half
+      for (int kb = 0; kb < kB; ++kb)
 #pragma unroll
-      for (int kb = 0; kb < kB; ++kb) {
-        const int row = 32 * kb + l32;
+        for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
 #pragma unroll
-        for (int c = 0; c < C::kSlots / 2; ++c) {
-          const unsigned char* const at = kt + row * C::kRowBytes + (((2 * c + half) ^ C::k_swizzle(row)) * 16);
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int kb = 0; kb < kB; ++kb) {
+          const unsigned char* const at = kt + (k_at ^ (32 * c)) + 32 * kb * C::kRowBytes;
           if constexpr (kF32) {
             const floatx4 kf = *reinterpret_cast<const floatx4*>(at);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-              for (int rb = 0; rb < kRB; ++rb) s[rb][kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[rb][c][e], s[rb][kb], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[c][e], s[kb], 0, 0, 0);
           } else {
-            const bf16x8 kf = *reinterpret_cast<const bf16x8*>(at);
+            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(at), qf[c], s[kb], 0, 0, 0);
+          }
+        }
+    };
+    // element i of block kb is key 32 kb + 8 (i / 4) + 4 half + i % 4 of the step
+    auto mask = [&](int st) DBSA_INLINE {
+      const int ln = lane_here();
+      uint64_t there = ~0ull;
+      int last;
+      if (st < pool_steps) {
+        last = (p.ent[2 * static_cast<int64_t>(ent_begin + st / kSteps) + 1] & 0xFFFF) - (st % kSteps) * kBN - 1;
+      } else {
+        const int first = own_first + (st - pool_steps) * kBN, j = first + ln;
+        int page = -1;
+        if (ln < kBN && j < own_n) page = p.page_table[static_cast<int64_t>(own_u) * p.table_stride + (j >> p.page_log2)];
+        there = __builtin_amdgcn_ballot_w64(page >= 0 && page < p.n_pages);
+        last = row_pos - first;
+      }
+      last -= 4 * (ln / 32);
+      there >>= 4 * (ln / 32);
 #pragma unroll
-            for (int rb = 0; rb < kRB; ++rb) s[rb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[rb][c], s[rb][kb], 0, 0, 0);
+      for (int kb = 0; kb < kB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = 32 * kb + 8 * (i / 4) + i % 4;
+          if (key > last || !((there >> key) & 1)) s[kb][i] = -INFINITY;
+        }
+    };
+    auto softmax = [&](int st) DBSA_INLINE {
+      if (__builtin_expect((partly >> (st % 32)) & 1, 0)) mask(st);
+      float top = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < kB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+      top = half_swap_max(top) * c2;
+      if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+        const float bigger = fmaxf(m, top);
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - bigger);
+        m = bigger;
+        l *= alpha;
+#pragma unroll
+        for (int ob = 0; ob < kO; ++ob)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[ob][i] *= alpha;
+      }
+      const float less = m == -INFINITY ? 0.f : -m;
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < kB; ++kb) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c2, less));
+          sum += s[kb][i];
+        }
+        if constexpr (!kF32) {
+#pragma unroll
+          for (int ch = 0; ch < 2; ++ch) {
+            union {
+              bf16x8 v;
+              bf16x2 p2[4];
+            } x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x.p2[e] = __builtin_convertvector(floatx2{s[kb][8 * ch + 2 * e], s[kb][8 * ch + 2 * e + 1]}, bf16x2);
+            pf[kb][ch] = x.v;
           }
         }
       }
-      // masks: element i of block kb is key 32 kb + 8 (i / 4) + 4 half + i % 4 of the step
-      if (!k.whole) {
-        const uint64_t there = k.own ? __builtin_amdgcn_ballot_w64(k.row >= 0) : ~0ull;
+      l += sum;
+    };
+    // the keys that take_poison kept out of the product
+    auto add_poison = [&](int st) DBSA_INLINE {
+      uint64_t keys = 0;
+      for (int i = 0; i < kNW; ++i) keys |= poison[(base + st) % C::kVStages * kNW + i];
+      keys = uniform64(keys);
+      const int h = lane_here() / 32;
+      while (keys) {
+        const int key = __builtin_ctzll(keys);
+        keys &= keys - 1;
+        const int j = own_first + (st - pool_steps) * kBN + key;
+        const int64_t page = p.page_table[static_cast<int64_t>(own_u) * p.table_stride + (j >> p.page_log2)];
+        const unsigned char* const v = static_cast<const unsigned char*>(p.v_own.ptr) +
+            (hk * p.v_own.stride_head + page * p.stride_page + (j & ((1 << p.page_log2) - 1)) * p.v_own.stride_tok) * kEs;
+        float mine = 0.f;  // the key's probability, in the half-wave that holds the key
 #pragma unroll
-        for (int rb = 0; rb < kRB; ++rb) {
-          const int last = k.own ? row_pos[rb] - k.first : k.len - 1;
+        for (int kb = 0; kb < kB; ++kb)
 #pragma unroll
-          for (int kb = 0; kb < kB; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int key = 32 * kb + 8 * (i / 4) + 4 * half + i % 4;
-              if (key > last || !((there >> key) & 1)) s[rb][kb][i] = -INFINITY;
+          for (int i = 0; i < 16; ++i)
+            if (key == 32 * kb + 8 * (i / 4) + 4 * h + i % 4) {
+              if constexpr (kF32) mine = s[kb][i];
+              else mine = static_cast<float>(pf[kb][i / 8][i % 8]);
             }
-        }
-      }
+        const float other = __shfl_xor(mine, 32);
+        const float prob = (key / 4) % 2 == h ? mine : other;
 #pragma unroll
-      for (int rb = 0; rb < kRB; ++rb) {
-        float top = s[rb][0][0];
-#pragma unroll
-        for (int kb = 0; kb < kB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) top = fmaxf(top, s[rb][kb][i]);
-        top = half_swap_max(top) * c2;
-        if (__builtin_amdgcn_ballot_w64(top > m[rb] + kSlack) != 0) {
-          const float next = fmaxf(m[rb], top);
-          const float alpha = m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rb] - next);
-          m[rb] = next;
-          l[rb] *= alpha;
-#pragma unroll
-          for (int ob = 0; ob < kO; ++ob)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[rb][ob][i] *= alpha;
-        }
-        const float less = m[rb] == -INFINITY ? 0.f : -m[rb];
-        float sum = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < kB; ++kb)
+        for (int ob = 0; ob < kO; ++ob)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            s[rb][kb][i] = __builtin_amdgcn_exp2f(fmaf(s[rb][kb][i], c2, less));
-            sum += s[rb][kb][i];
+            const float x = stored_value<T>(v, 32 * ob + 8 * (i / 4) + 4 * h + i % 4);
+            if (prob != 0.f) acc[ob][i] = fmaf(prob, x, acc[ob][i]);
           }
-        l[rb] += sum;
       }
-      // output
-      if (k.own && !k.whole) add_poison(k, st, s);
+    };
+    auto product = [&](int st) DBSA_INLINE {
+      const unsigned char* const vt = smem + (C::kKStages + (base + st) % C::kVStages) * C::kTileBytes;
+      if (__builtin_expect(st >= pool_steps && ((partly >> (st % 32)) & 1), 0)) add_poison(st);
       if constexpr (kF32) {
 #pragma unroll
         for (int kb = 0; kb < kB; ++kb)
@@ -428,99 +473,124 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
             for (int ob = 0; ob < kO; ++ob) {
               const int ch = 32 * ob + l32;
               const float vf = *reinterpret_cast<const float*>(vt + row * C::kRowBytes + (((ch / 4) ^ C::v_swizzle(row)) * 16) + (ch % 4) * 4);
-#pragma unroll
-              for (int rb = 0; rb < kRB; ++rb) acc[rb][ob] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[rb][kb][i], acc[rb][ob], 0, 0, 0);
+              acc[ob] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[kb][i], acc[ob], 0, 0, 0);
             }
           }
       } else {
-        // V fragment (kb, ch, ob): keys 32 kb + 16 ch + 4 half + {0..3, 8..11}, the order the probabilities lie in; read transposed:
-        // lane j of 16 fetches four channels of one key and gets four keys of one channel
-        const int j = (lane % 16) / 4;
-        const unsigned char* const vbase = vt + (4 * half + j) * C::kRowBytes + (lane % 2) * 8;
-        const int slot0 = (2 * (l32 / 16) + (lane % 4) / 2) ^ C::v_swizzle(j);
 #pragma unroll
         for (int kb = 0; kb < kB; ++kb)
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
-            bf16x8 pf[kRB];
-#pragma unroll
-            for (int rb = 0; rb < kRB; ++rb) {
-              union {
-                bf16x8 v;
-                bf16x2 p2[4];
-              } x;
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                x.p2[e] = __builtin_convertvector(floatx2{s[rb][kb][8 * ch + 2 * e], s[rb][kb][8 * ch + 2 * e + 1]}, bf16x2);
-              pf[rb] = x.v;
-            }
+          for (int ch = 0; ch < 2; ++ch)
 #pragma unroll
             for (int ob = 0; ob < kO; ++ob) {
-              const unsigned char* const at = vbase + (32 * kb + 16 * ch) * C::kRowBytes + ((slot0 ^ (4 * ob)) * 16);
+              const unsigned char* const at = vt + (v_at ^ (64 * ob)) + (32 * kb + 16 * ch) * C::kRowBytes;
               const bf16x4 lo = lds_read_tr(reinterpret_cast<const __bf16*>(at));
               const bf16x4 hi = lds_read_tr(reinterpret_cast<const __bf16*>(at + 8 * C::kRowBytes));
               const bf16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-              for (int rb = 0; rb < kRB; ++rb) acc[rb][ob] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[rb], acc[rb][ob], 0, 0, 0);
+              acc[ob] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[kb][ch], acc[ob], 0, 0, 0);
             }
-          }
       }
     };
+    // Order of a run of matrix instructions with their fragments' reads: kAhead reads first, then each instruction with the
+    // reads of a later one.
+    auto pipelined = [&](auto READS, auto COUNT) DBSA_INLINE {
+      constexpr int kReads = decltype(READS)::value, kCount = decltype(COUNT)::value, kAhead = 4;
+      __builtin_amdgcn_sched_group_barrier(0x100, kAhead * kReads, 0);
+      static_for<kCount - kAhead>([&](auto) DBSA_INLINE {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+      });
+      __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+    };
+    auto multiply_scores = [&](int st) DBSA_INLINE {
+      __builtin_amdgcn_sched_barrier(0);
+      scores(st);
+      if constexpr (!kF32) pipelined(std::integral_constant<int, 1>{}, std::integral_constant<int, kC * kB>{});
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply_product = [&](int st) DBSA_INLINE {
+      __builtin_amdgcn_sched_barrier(0);
+      product(st);
+      if constexpr (!kF32) pipelined(std::integral_constant<int, 2>{}, std::integral_constant<int, 2 * kB * kO>{});
+      __builtin_amdgcn_sched_barrier(0);
+    };
 
-    Ahead next{};
-    Keys cur{}, ahead{};
     if (steps > 0) {
-      ahead = place(0, fetch(0));
-      load(ahead);
-      next = fetch(1);
+      next = fetch(0);
+      request(0);
     }
-    for (int s = 0; s < steps; ++s) {
-      cur = ahead;
-      if (cur.own && !cur.whole) take_poison(stage);
-      store(stage);
-      if (s + 1 < steps) {
-        ahead = place(s + 1, next);
-        load(ahead);
-        next = fetch(s + 2);
+    if constexpr (C::kPingPong) {
+      if (steps > 0) {
+        const bool second = wave >= kNW / 2;
+        // one stage step: store what has arrived, request the next
+        auto advance = [&](int st) DBSA_INLINE {
+          if (st < steps) put(st);
+          if (st + 1 < steps) request(st + 1);
+        };
+        auto phase_end = [&] {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+        };
+        advance(0);
+        phase_end();
+        if (second) {
+          advance(1);
+          phase_end();
+        }
+        for (int st = 0; st < steps; ++st) {
+          __builtin_amdgcn_s_setprio(1);
+          if (st > 0) multiply_product(st - 1);
+          multiply_scores(st);
+          __builtin_amdgcn_s_setprio(0);
+          phase_end();
+          softmax(st);
+          advance(st + 1 + (second ? 1 : 0));
+          phase_end();
+        }
+        multiply_product(steps - 1);
+        if (!second) phase_end();
       }
-      // one barrier per step: the other stage was last read before the barrier of the step that filled this one
-      __syncthreads();
-      compute(cur, stage);
-      stage ^= 1;
+    } else {
+      for (int st = 0; st < steps; ++st) {
+        put(st);
+        if (st + 1 < steps) request(st + 1);
+        // one barrier per step: the other stage was last read before the barrier of the step that filled this one
+        __syncthreads();
+        multiply_scores(st);
+        softmax(st);
+        multiply_product(st);
+      }
     }
+    n_stored += steps;
 
     // ---- what the record leaves ----
+    const float sum = half_swap_sum(l);
+    const int row_head = hk * r + row_index % r;
+    if (!row_ok) {
+    } else if (part_base >= 0) {
+      float* const out = p.partial + (static_cast<int64_t>(part_base + row_in) * p.n_q_heads + row_head) * (kD + kPartialPad);
 #pragma unroll
-    for (int rb = 0; rb < kRB; ++rb) {
-      const float sum = half_swap_sum(l[rb]);
-      if (!row_ok[rb]) continue;
-      if (part_base >= 0) {
-        float* const out = p.partial + (static_cast<int64_t>(part_base + row_tok[rb]) * p.n_q_heads + row_head[rb]) * (kD + kPartialPad);
+      for (int ob = 0; ob < kO; ++ob)
 #pragma unroll
-        for (int ob = 0; ob < kO; ++ob)
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<floatx4*>(out + 32 * ob + 8 * g + 4 * half) =
+              floatx4{acc[ob][4 * g], acc[ob][4 * g + 1], acc[ob][4 * g + 2], acc[ob][4 * g + 3]};
+      if (half == 0) *reinterpret_cast<floatx2*>(out + kD) = floatx2{m, sum};
+    } else {
+      // (a row that saw no key is zero)
+      const float inv = sum > 0.f || sum != sum ? (p.v_scale ? p.v_scale[hk] : 1.f) / sum : 0.f;
+      Q* const out = static_cast<Q*>(const_cast<void*>(p.o.ptr)) + row_tok * p.o.stride_tok + row_head * p.o.stride_head;
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const floatx4 x = {acc[rb][ob][4 * g], acc[rb][ob][4 * g + 1], acc[rb][ob][4 * g + 2], acc[rb][ob][4 * g + 3]};
-            *reinterpret_cast<floatx4*>(out + 32 * ob + 8 * g + 4 * half) = x;
-          }
-        if (half == 0) *reinterpret_cast<floatx2*>(out + kD) = floatx2{m[rb], sum};
-      } else {
-        const int tok = p.toks[tok_begin + row_tok[rb]];
-        // (a row that saw no key is zero)
-        const float inv = sum > 0.f || sum != sum ? v_scale / sum : 0.f;
-        Q* const out = static_cast<Q*>(const_cast<void*>(p.o.ptr)) + tok * p.o.stride_tok + row_head[rb] * p.o.stride_head;
+      for (int ob = 0; ob < kO; ++ob)
 #pragma unroll
-        for (int ob = 0; ob < kO; ++ob)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            typedef Q four __attribute__((ext_vector_type(4)));
-            *reinterpret_cast<four*>(out + 32 * ob + 8 * g + 4 * half) =
-                four{static_cast<Q>(acc[rb][ob][4 * g] * inv), static_cast<Q>(acc[rb][ob][4 * g + 1] * inv),
-                     static_cast<Q>(acc[rb][ob][4 * g + 2] * inv), static_cast<Q>(acc[rb][ob][4 * g + 3] * inv)};
-          }
-        if (p.lse && half == 0)
-          p.lse[static_cast<int64_t>(row_head[rb]) * p.n_rows + tok] = (m[rb] + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
-      }
+        for (int g = 0; g < 4; ++g) {
+          typedef Q four __attribute__((ext_vector_type(4)));
+          *reinterpret_cast<four*>(out + 32 * ob + 8 * g + 4 * half) =
+              four{static_cast<Q>(acc[ob][4 * g] * inv), static_cast<Q>(acc[ob][4 * g + 1] * inv),
+                   static_cast<Q>(acc[ob][4 * g + 2] * inv), static_cast<Q>(acc[ob][4 * g + 3] * inv)};
+        }
+      if (p.lse && half == 0) p.lse[static_cast<int64_t>(row_head) * p.n_rows + row_tok] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     }
   }
 }
@@ -570,17 +640,17 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
   if (p.lse && lane == 0) p.lse[static_cast<int64_t>(head) * p.n_rows + tok] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
-template <typename T, int kD, int kNW, int kRB, int kBN>
+template <typename T, int kD, int kNW, int kBN>
 hipError_t launch_shape(const ChunkParams& p, hipStream_t stream) {
-  typedef Chunk<T, kD, kNW, kRB, kBN> C;
-  const void* const f = reinterpret_cast<const void*>(chunk_attn_kernel<T, kD, kNW, kRB, kBN>);
+  typedef Chunk<T, kD, kNW, kBN> C;
+  const void* const f = reinterpret_cast<const void*>(chunk_attn_kernel<T, kD, kNW, kBN>);
   static std::atomic<bool> attr_set{false};  // setting it twice from two threads is harmless
   if (!attr_set) {
     const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
     if (e != hipSuccess) return e;
     attr_set = true;
   }
-  chunk_attn_kernel<T, kD, kNW, kRB, kBN><<<dim3(static_cast<unsigned>(p.n_workers) * p.n_kv_heads), dim3(C::kThreads), C::kLds, stream>>>(p);
+  chunk_attn_kernel<T, kD, kNW, kBN><<<dim3(static_cast<unsigned>(p.n_workers) * p.n_kv_heads), dim3(C::kThreads), C::kLds, stream>>>(p);
   return hipGetLastError();
 }
 
@@ -588,10 +658,10 @@ template <typename T, int kD>
 hipError_t launch_kind(const ChunkParams& p, hipStream_t stream) {
   constexpr int kWide = Kind<T>::kBytes == 4 ? 32 : 64;
   hipError_t e = hipErrorInvalidValue;
-  if (p.rows == 32) e = launch_shape<T, kD, 1, 1, 32>(p, stream);
-  else if (p.rows == 64) e = launch_shape<T, kD, 2, 1, 32>(p, stream);
-  else if (p.rows == 128) e = launch_shape<T, kD, 4, 1, kWide>(p, stream);
-  else if (p.rows == 256) e = launch_shape<T, kD, 8, 1, kWide>(p, stream);
+  if (p.rows == 32) e = launch_shape<T, kD, 1, 32>(p, stream);
+  else if (p.rows == 64) e = launch_shape<T, kD, 2, 32>(p, stream);
+  else if (p.rows == 128) e = launch_shape<T, kD, 4, kWide>(p, stream);
+  else if (p.rows == 256) e = launch_shape<T, kD, 8, kWide>(p, stream);
   if (e != hipSuccess || !p.merge) return e;
   const int64_t pairs = static_cast<int64_t>(p.n_rows) * p.n_q_heads;
   chunk_merge_kernel<typename Kind<T>::Q, kD><<<dim3(static_cast<unsigned>((pairs + 3) / 4)), dim3(256), 0, stream>>>(p);
