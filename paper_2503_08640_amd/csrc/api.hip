@@ -1196,6 +1196,8 @@ int chunk_common(const dbsa_layout* L, dbsa_tensor q, dbsa_tensor k_pool, dbsa_t
   p.page_log2 = __builtin_ctz(static_cast<unsigned>(own->page_tokens));
   p.own_capacity = static_cast<int32_t>(std::min<int64_t>(int64_t{own->table_stride} * own->page_tokens, INT32_MAX - 2 * kChunkTile));
   p.merge = L->ck_part_rows > 0 ? 1 : 0;
+  const int64_t widest = std::max(std::max(k_pool.stride_tok, v_pool.stride_tok), std::max(own->k.stride_tok, own->v.stride_tok));
+  p.narrow = widest < (int64_t{1} << 22) ? 1 : 0;  // (64 rows of at most 4 bytes an element: 2^30)
   const size_t need = static_cast<size_t>(L->ck_part_rows) * n_q_heads * (head_dim + kPartialPad) * sizeof(float);
   if (need > 0 && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
     return DBSA_ERR_WORKSPACE;

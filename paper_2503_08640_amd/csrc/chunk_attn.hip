@@ -47,6 +47,12 @@ struct Kind<float> {
 };
 
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) uintx4 lds_piece;
+
+// dma16 (mfma_common.hpp) with an address of its own per lane
+__device__ inline void dma16_wide(uint64_t address, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(address) : "memory");
+}
 
 // sixteen e4m3 bytes as bf16
 __device__ DBSA_INLINE void widen16(const uintx4& raw, uintx4& lo, uintx4& hi) {
@@ -112,8 +118,15 @@ struct Chunk {
   static constexpr int kLoads = 2 * kOperand / kThreads;                                // pieces per thread
   static constexpr bool kApart = kOperand < kThreads;                                   // half the waves fetch K, half V
   static constexpr int kKeyBlocks = kBN / 32, kChBlocks = kD / 32;
-  static constexpr int kKStages = 2, kVStages = kPingPong ? 3 : 2;
-  static constexpr int kPoisonAt = (kKStages + kVStages) * kTileBytes;  // each wave's mask of poisoned rows, per stage of V
+  // Steps requested ahead of the one that is about to be read.  16-bit and fp32 rows go from memory straight into their
+  // stage; 8-bit rows into a ring of the wave's own, from where the same lanes widen them into the stages.
+  static constexpr bool kDirect = Kind<T>::kStoredBytes != 1;
+  static constexpr int kFlight = kDirect ? (kPingPong ? 2 : kNW == 8 || (kNW == 4 && !kF32) ? 3 : kF32 ? 1 : 2)
+                                         : (kNW == 8 ? 3 : kNW == 4 ? 4 : 6);
+  static constexpr int kKStages = !kDirect ? 2 : kPingPong ? kFlight + 2 : kFlight + 1;
+  static constexpr int kVStages = !kDirect ? (kPingPong ? 3 : 2) : kPingPong ? kFlight + 3 : kFlight + 1;
+  static constexpr int kRingAt = (kKStages + kVStages) * kTileBytes;
+  static constexpr int kPoisonAt = kRingAt + (kDirect ? 0 : kFlight * kThreads * kLoads * 16);  // per stage of V: each wave's mask of poisoned rows
   static constexpr int kLds = kPoisonAt + kVStages * kNW * 8;
   static_assert(kPieces <= 32 && 64 % kPieces == 0, "a stored row is fetched by neighbouring lanes of one wave");
   static_assert(kApart ? kOperand * 2 == kThreads : kOperand % kThreads == 0, "whole pieces per thread");
@@ -156,12 +169,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
   const bool negate = c2 < 0.f;
   c2 = fmaxf(fabsf(c2), 1e-30f);
 
-  const unsigned char* const kpool = static_cast<const unsigned char*>(p.k_pool.ptr) + hk * p.k_pool.stride_head * kEs;
-  const unsigned char* const vpool = static_cast<const unsigned char*>(p.v_pool.ptr) + hk * p.v_pool.stride_head * kEs;
-  const int64_t kpool_stride = p.k_pool.stride_tok * kEs, vpool_stride = p.v_pool.stride_tok * kEs;
-  // this thread's first piece of a whole step
-  const int64_t k_lane = (tid % C::kOperand / C::kPieces) * kpool_stride + (tid % C::kPieces) * 16;
-  const int64_t v_lane = (tid % C::kOperand / C::kPieces) * vpool_stride + (tid % C::kPieces) * 16;
+  const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_byte*)smem));
+  const const_words entries = (const_words)(reinterpret_cast<uintptr_t>(p.ent));
+  const const_words page_table = (const_words)(reinterpret_cast<uintptr_t>(p.page_table));
   // LDS addresses of fragments: K fragment (kb, c) is row 32 kb + l32, place 2 c + half; V fragment (16-bit: kb, ch, ob) keys
   // 32 kb + 16 ch + 4 half + {0..3, 8..11}, the order the probabilities lie in, read transposed: lane j of 16 fetches four
   // channels of one key and gets four keys of one channel.  (A place is xor-ed: base ^ (32 c), base ^ (64 ob).)
@@ -170,15 +180,18 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
                    (((2 * (l32 / 16) + (lane % 4) / 2) ^ C::v_swizzle((lane % 16) / 4)) * 16) + (lane % 2) * 8;
 
   int n_stored = 0;  // steps staged so far, over all records: their stages
-  const int rec_end = p.ptr[worker + 1];
-  for (int rec = p.ptr[worker]; rec < rec_end; ++rec) {
-    const int32_t* const w = p.rec + rec * kChunkWords;
+  const const_words workers = (const_words)(reinterpret_cast<uintptr_t>(p.ptr));
+  const const_words tokens = (const_words)(reinterpret_cast<uintptr_t>(p.toks));
+  const const_words lengths = (const_words)(reinterpret_cast<uintptr_t>(p.self_len));
+  const int rec_end = workers[worker + 1];
+  for (int rec = workers[worker]; rec < rec_end; ++rec) {
+    const const_words w = (const_words)(reinterpret_cast<uintptr_t>(p.rec)) + rec * kChunkWords;
     const int tok_begin = w[0], n_tok = w[1], ent_begin = w[2], n_ent = w[3], own_u = w[4], part_base = w[8];
     const int cu = w[9], t_new = w[10];
 
     // ---- the row of this lane (both half-waves hold it) ----
     int own_n = 0;  // own keys there are
-    if (own_u >= 0) own_n = min(max(p.self_len[own_u], 0), p.own_capacity);
+    if (own_u >= 0) own_n = min(max(lengths[own_u], 0), p.own_capacity);
     const int row_index = wave * 32 + l32;
     const bool row_ok = row_index / r < n_tok;
     const int row_in = min(row_index / r, n_tok - 1);
@@ -196,139 +209,185 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     }
     // own tiles of this record: its share of those up to the last token's own key
     int own_first = 0, own_steps = 0;
-    const int first_pos = own_n - t_new + (p.toks[tok_begin] - cu);  // (tokens of a question ascend)
+    const int first_pos = own_n - t_new + (tokens[tok_begin] - cu);  // (tokens of a question ascend)
     if (own_u >= 0) {
-      const int last = own_n - t_new + (p.toks[tok_begin + n_tok - 1] - cu);
+      const int last = own_n - t_new + (tokens[tok_begin + n_tok - 1] - cu);
       const int64_t tiles = max(0, (last + kChunkTile) / kChunkTile);
       const int lo = static_cast<int>(w[5] * tiles / w[7]), hi = static_cast<int>(w[6] * tiles / w[7]);
       own_first = lo * kChunkTile;
       own_steps = (hi - lo) * kSteps;
     }
     const int pool_steps = n_ent * kSteps, steps = pool_steps + own_steps;
+    const int base = n_stored;
 
     // ---- the stream of steps ----
-    // what a step hangs off (its list entry, or the page of this lane's key), requested one step before its rows
+    // What a step hangs off: its list entry, or the pages of its keys (scalar loads, requested one step before its rows).
+    // Own steps never straddle a page of kBN tokens or more; smaller pages are at most kPages to a step.
+    constexpr int kPages = kBN / 16;
     struct Ahead {
-      int start, len, page;
+      int start, len;
+      int page[kPages];
     };
     auto fetch = [&](int s) DBSA_INLINE {
-      Ahead x{0, 0, -1};
+      Ahead x{0, 0, {}};
       if (s < pool_steps) {
-        const int32_t* const e = p.ent + 2 * static_cast<int64_t>(ent_begin + s / kSteps);
+        const const_words e = entries + 2 * static_cast<int64_t>(ent_begin + s / kSteps);
         x.start = e[0];
         x.len = e[1];
-      } else if (s < steps) {
-        const int j = own_first + (s - pool_steps) * kBN + lane;
-        if (lane < kBN && j < own_n) x.page = p.page_table[static_cast<int64_t>(own_u) * p.table_stride + (j >> p.page_log2)];
+      } else {
+        const int first = (own_first + (s - pool_steps) * kBN) >> p.page_log2;
+        const const_words table = page_table + static_cast<int64_t>(own_u) * p.table_stride;
+#pragma unroll
+        for (int i = 0; i < kPages; ++i)  // (entries behind the step's last page are not used)
+          if (i == 0 || (1 << p.page_log2) < kBN) x.page[i] = table[min(first + i, p.table_stride - 1)];
       }
       return x;
     };
-    // A step's keys: row of this lane's key in the pool or in the pages (-1: nothing there).  whole: every row sees all of them.
-    struct Keys {
-      int row;
-      bool own, whole;
-    };
-    auto place = [&](int s, const Ahead& x) DBSA_INLINE {
-      Keys k;
-      k.own = s >= pool_steps;
-      if (!k.own) {
-        const int off = (s % kSteps) * kBN, len = min((x.len & 0xFFFF) - off, kBN);
-        k.row = len > 0 ? x.start + off + min(lane, len - 1) : -1;
-        k.whole = len == kBN;
-      } else {
-        const int first = own_first + (s - pool_steps) * kBN;
-        k.row = x.page >= 0 && x.page < p.n_pages ? (x.page << p.page_log2) + ((first + lane) & ((1 << p.page_log2) - 1)) : -1;
-        k.whole = first + kBN - 1 <= first_pos && __builtin_amdgcn_ballot_w64(lane < kBN && k.row < 0) == 0;
+    auto page_there = [&](int page) DBSA_INLINE { return page >= 0 && page < p.n_pages; };
+    // page of key `key` of an own step
+    auto page_of = [&](const Ahead& x, int key) DBSA_INLINE {
+      int page = x.page[0];
+      if ((1 << p.page_log2) < kBN) {
+        const int at = key >> p.page_log2;
+#pragma unroll
+        for (int i = 1; i < kPages; ++i) page = at == i ? x.page[i] : page;
       }
-      return k;
+      return page;
     };
+    // Which own keys of a step there are: bit key.
+    auto keys_there = [&](const Ahead& x, int first) DBSA_INLINE {
+      const int ln = lane_here();
+      return __builtin_amdgcn_ballot_w64(ln < kBN && first + ln < own_n && page_there(page_of(x, ln)));
+    };
+    constexpr uint64_t kAllKeys = kBN == 64 ? ~0ull : (1ull << kBN) - 1;
+
     // This thread's pieces of a step: piece tid + i threads of K, then of V; the operand of piece i is the wave's.
-    uintx4 raw[C::kLoads];
     auto is_v = [&](int i) DBSA_INLINE { return C::kApart ? wave >= kNW / 2 : i >= C::kLoads / 2; };
     auto piece_row = [&](int i, int t) DBSA_INLINE { return (t + i * C::kThreads) % C::kOperand / C::kPieces; };
-    auto load = [&](const Keys& k) DBSA_INLINE {
-      if (__builtin_expect(!k.own && k.whole, 1)) {
-        const int64_t first = __builtin_amdgcn_readfirstlane(k.row);
+    // first row of the rows that wave and pass i fetch (1 KiB: 64 pieces)
+    auto wave_row = [&](int i) DBSA_INLINE { return (64 * wave + i * C::kThreads) % C::kOperand / C::kPieces; };
+    // where piece i of step s lands: places of a stage are xor-ed on the way (the lane fetches the piece that belongs there), the
+    // ring holds pieces as they come
+    auto landing = [&](int s, int i) DBSA_INLINE {
+      unsigned at;
+      if constexpr (C::kDirect)
+        at = (is_v(i) ? C::kKStages + (base + s) % C::kVStages : (base + s) % C::kKStages) * C::kTileBytes + wave_row(i) * C::kRowBytes;
+      else
+        at = C::kRingAt + (((base + s) % C::kFlight * C::kLoads + i) * kNW + wave) * 1024;
+      return static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds0 + at)));
+    };
+    auto fetched_col = [&](int i, int t) DBSA_INLINE {
+      const int col = t % C::kPieces, row = piece_row(i, t);
+      return (C::kDirect ? col ^ (is_v(i) ? C::v_swizzle(row) : C::k_swizzle(row)) : col) * 16;
+    };
+    uint32_t partly = 0;  // bit s % 32: some row does not see some key of step s (kept until its product is done)
+    Ahead next = fetch(0);
+    auto request = [&](int s) DBSA_INLINE {  // s < steps: what it hangs off is in `next`
+      const Ahead x = next;
+      next = fetch(min(s + 1, steps - 1));
+      const bool own = s >= pool_steps;
+      const int off = own ? own_first + (s - pool_steps) * kBN : (s % kSteps) * kBN;
+      const int len = own ? min(own_n - off, kBN) : min((x.len & 0xFFFF) - off, kBN);
+      const bool one_page = own && (1 << p.page_log2) >= kBN;
+      bool whole = len == kBN;
+      if (own) {
+        whole = whole && off + kBN - 1 <= first_pos;
+        if (one_page) whole = whole && page_there(x.page[0]);
+        else whole = whole && keys_there(x, off) == kAllKeys;
+      }
+      const uint32_t bit = 1u << (s % 32);
+      partly = whole ? partly & ~bit : partly | bit;
+      const int64_t ks = (own ? p.k_own.stride_tok : p.k_pool.stride_tok) * kEs, vs = (own ? p.v_own.stride_tok : p.v_pool.stride_tok) * kEs;
+      const unsigned char* const kb = static_cast<const unsigned char*>(own ? p.k_own.ptr : p.k_pool.ptr) +
+                                      hk * (own ? p.k_own.stride_head : p.k_pool.stride_head) * kEs;
+      const unsigned char* const vb = static_cast<const unsigned char*>(own ? p.v_own.ptr : p.v_pool.ptr) +
+                                      hk * (own ? p.v_own.stride_head : p.v_pool.stride_head) * kEs;
+      if (__builtin_expect(p.narrow && whole && (!own || one_page), 1)) {
+        // kBN rows one after the other
+        const int64_t page = own ? x.page[0] * p.stride_page * kEs : 0;
+        const int row = own ? off & ((1 << p.page_log2) - 1) : x.start + off;
+        const uint64_t kt = reinterpret_cast<uint64_t>(kb) + page + row * ks, vt = reinterpret_cast<uint64_t>(vb) + page + row * vs;
 #pragma unroll
         for (int i = 0; i < C::kLoads; ++i) {
+          const int64_t stride = is_v(i) ? vs : ks;
           const int row0 = i * C::kThreads % C::kOperand / C::kPieces;  // (whole rows per pass of the threads)
-          if (is_v(i)) raw[i] = *reinterpret_cast<const uintx4*>(vpool + (first + row0) * vpool_stride + v_lane);
-          else raw[i] = *reinterpret_cast<const uintx4*>(kpool + (first + row0) * kpool_stride + k_lane);
+          dma16(uniform64((is_v(i) ? vt : kt) + row0 * stride),
+                static_cast<unsigned>(piece_row(0, tid) * static_cast<int>(stride) + fetched_col(i, tid)), landing(s, i));
         }
         return;
       }
       const int t = 64 * wave + lane_here();
-      const int shift = k.own ? p.page_log2 : 31;
-      const unsigned char* const kb = static_cast<const unsigned char*>(k.own ? p.k_own.ptr : p.k_pool.ptr) +
-                                      hk * (k.own ? p.k_own.stride_head : p.k_pool.stride_head) * kEs;
-      const unsigned char* const vb = static_cast<const unsigned char*>(k.own ? p.v_own.ptr : p.v_pool.ptr) +
-                                      hk * (k.own ? p.v_own.stride_head : p.v_pool.stride_head) * kEs;
-      const int64_t ks = (k.own ? p.k_own.stride_tok : p.k_pool.stride_tok) * kEs;
-      const int64_t vs = (k.own ? p.v_own.stride_tok : p.v_pool.stride_tok) * kEs;
 #pragma unroll
       for (int i = 0; i < C::kLoads; ++i) {
-        const int row = __shfl(k.row, piece_row(i, t));
-        raw[i] = uintx4{0, 0, 0, 0};
-        if (row >= 0) {
-          const int64_t page = row >> shift, in = row - (page << shift);
-          raw[i] = *reinterpret_cast<const uintx4*>((is_v(i) ? vb : kb) + page * p.stride_page * kEs + in * (is_v(i) ? vs : ks) +
-                                                    (t % C::kPieces) * 16);
+        const int key = piece_row(i, t);
+        int64_t at;
+        if (own) {
+          const int page = page_of(x, key);
+          at = key < len && page_there(page) ? page * p.stride_page * kEs + ((off + key) & ((1 << p.page_log2) - 1)) * (is_v(i) ? vs : ks) : 0;
+        } else {
+          at = (x.start + (len > 0 ? off + min(key, len - 1) : 0)) * (is_v(i) ? vs : ks);
         }
+        dma16_wide(reinterpret_cast<uint64_t>(is_v(i) ? vb : kb) + at + fetched_col(i, t), landing(s, i));
       }
     };
-    // Where some rows do not see every key (the chunk's own diagonal), a non-finite value must not reach the others through
-    // 0 * NaN: such rows of V are staged as zeros, and their keys added one by one to the rows that see them.
+    // step s has landed, as far as this wave fetched it; `newer` steps were requested since
+    auto wait_for = [&](int s, auto NEWER) DBSA_INLINE {
+      constexpr int kNewer = decltype(NEWER)::value;
+      if (s + kNewer < steps) wait_vmcnt<kNewer * C::kLoads>();
+      else wait_vmcnt<0>();
+    };
+    // Where some rows do not see every key (the chunk's own diagonal, keys that are not there), nothing may reach them through
+    // 0 * NaN: keys that are not there, and rows of V with a non-finite value, are staged as zeros, the latter's keys added
+    // one by one to the rows that see them.
     uint64_t* const poison = reinterpret_cast<uint64_t*>(smem + C::kPoisonAt);
-    auto take_poison = [&](int v_stage) DBSA_INLINE {
+    auto clean = [&](int s, uintx4 (&raw)[C::kLoads]) DBSA_INLINE {
       uint64_t mask = 0;
       constexpr uint64_t kRowLanes = (1ull << C::kPieces) - 1;
       const int ln = lane_here();
+      const int first = own_first + (s - pool_steps) * kBN;
+      const uint64_t there = keys_there(fetch(s), first);
 #pragma unroll
       for (int i = 0; i < C::kLoads; ++i) {
-        if (!is_v(i)) continue;
-        const uint64_t bad = __builtin_amdgcn_ballot_w64(not_finite<T>(raw[i]));
-        if (bad == 0) continue;
-        const int row0 = (64 * wave + i * C::kThreads) % C::kOperand / C::kPieces;
-        for (int rr = 0; rr < 64 / C::kPieces; ++rr)
-          if ((bad >> (rr * C::kPieces)) & kRowLanes) mask |= 1ull << (row0 + rr);
-        if ((bad >> (ln / C::kPieces * C::kPieces)) & kRowLanes) raw[i] = uintx4{0, 0, 0, 0};
+        const bool missing = !((there >> piece_row(i, 64 * wave + ln)) & 1);
+        uint64_t bad = 0;
+        if (is_v(i)) {
+          bad = __builtin_amdgcn_ballot_w64(!missing && not_finite<T>(raw[i]));
+          for (int rr = 0; rr < 64 / C::kPieces; ++rr)
+            if ((bad >> (rr * C::kPieces)) & kRowLanes) mask |= 1ull << (wave_row(i) + rr);
+        }
+        if (missing || ((bad >> (ln / C::kPieces * C::kPieces)) & kRowLanes)) raw[i] = uintx4{0, 0, 0, 0};
       }
-      if (ln == 0) poison[v_stage * kNW + wave] = mask;
+      if (ln == 0) poison[(base + s) % C::kVStages * kNW + wave] = mask;
     };
-    auto store = [&](int k_stage, int v_stage) DBSA_INLINE {
+    // What this wave does to its landed pieces of step s before the others read them.
+    auto put = [&](int s) DBSA_INLINE {
+      const bool own_partly = s >= pool_steps && ((partly >> (s % 32)) & 1);
+      if constexpr (C::kDirect) {
+        if (__builtin_expect(own_partly, 0)) {
+          uintx4 raw[C::kLoads];
+          const int ln = lane_here();
 #pragma unroll
-      for (int i = 0; i < C::kLoads; ++i) {
-        const int row = piece_row(i, tid), col = tid % C::kPieces;
-        unsigned char* const at = smem + (is_v(i) ? C::kKStages + v_stage : k_stage) * C::kTileBytes + row * C::kRowBytes;
-        const int swizzle = is_v(i) ? C::v_swizzle(row) : C::k_swizzle(row);
-        if constexpr (kEs == 1) {
+          for (int i = 0; i < C::kLoads; ++i) raw[i] = *reinterpret_cast<const lds_piece*>(static_cast<uintptr_t>(landing(s, i) + ln * 16));
+          clean(s, raw);
+#pragma unroll
+          for (int i = 0; i < C::kLoads; ++i) *reinterpret_cast<lds_piece*>(static_cast<uintptr_t>(landing(s, i) + ln * 16)) = raw[i];
+        }
+      } else {
+        uintx4 raw[C::kLoads];
+#pragma unroll
+        for (int i = 0; i < C::kLoads; ++i) raw[i] = *reinterpret_cast<const lds_piece*>(static_cast<uintptr_t>(landing(s, i) + lane * 16));
+        if (__builtin_expect(own_partly, 0)) clean(s, raw);
+#pragma unroll
+        for (int i = 0; i < C::kLoads; ++i) {
+          const int row = piece_row(i, tid), col = tid % C::kPieces;
+          unsigned char* const at = smem + (is_v(i) ? C::kKStages + (base + s) % C::kVStages : (base + s) % C::kKStages) * C::kTileBytes + row * C::kRowBytes;
+          const int swizzle = is_v(i) ? C::v_swizzle(row) : C::k_swizzle(row);
           uintx4 lo, hi;
           widen16(raw[i], lo, hi);
           *reinterpret_cast<uintx4*>(at + ((2 * col) ^ swizzle) * 16) = lo;
           *reinterpret_cast<uintx4*>(at + ((2 * col + 1) ^ swizzle) * 16) = hi;
-        } else {
-          *reinterpret_cast<uintx4*>(at + (col ^ swizzle) * 16) = raw[i];
         }
       }
-    };
-    // Steps are staged in order: step s of the record is number base + s of the workgroup.  What its rows see is noted in a
-    // bit of `partly` (some row does not see some key) until its product is done: at most four steps are on their way.
-    const int base = n_stored;
-    uint32_t partly = 0;
-    Ahead next{};
-    bool raw_own_partly = false;  // the step in `raw`
-    auto request = [&](int s) DBSA_INLINE {  // s < steps: its entry is in `next`
-      const Keys k = place(s, next);
-      load(k);
-      const uint32_t bit = 1u << (s % 32);
-      partly = k.whole ? partly & ~bit : partly | bit;
-      raw_own_partly = k.own && !k.whole;
-      next = fetch(s + 1);
-    };
-    auto put = [&](int s) DBSA_INLINE {
-      const int v_stage = (base + s) % C::kVStages;
-      if (__builtin_expect(raw_own_partly, 0)) take_poison(v_stage);
-      store((base + s) % C::kKStages, v_stage);
     };
 
     // ---- softmax state ----
@@ -366,13 +425,12 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       const int ln = lane_here();
       uint64_t there = ~0ull;
       int last;
+      const Ahead x = fetch(st);
       if (st < pool_steps) {
-        last = (p.ent[2 * static_cast<int64_t>(ent_begin + st / kSteps) + 1] & 0xFFFF) - (st % kSteps) * kBN - 1;
+        last = (x.len & 0xFFFF) - (st % kSteps) * kBN - 1;
       } else {
-        const int first = own_first + (st - pool_steps) * kBN, j = first + ln;
-        int page = -1;
-        if (ln < kBN && j < own_n) page = p.page_table[static_cast<int64_t>(own_u) * p.table_stride + (j >> p.page_log2)];
-        there = __builtin_amdgcn_ballot_w64(page >= 0 && page < p.n_pages);
+        const int first = own_first + (st - pool_steps) * kBN;
+        there = keys_there(x, first);
         last = row_pos - first;
       }
       last -= 4 * (ln / 32);
@@ -515,51 +573,70 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       __builtin_amdgcn_sched_barrier(0);
     };
 
+    // What happens to step n while step n - 1 is still being read.  (A wave's own ring place is free again once it has read it.)
+    auto lds_done = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+    auto barrier = [&] {
+      lds_done();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    constexpr std::integral_constant<int, C::kFlight> kAll{};
+    constexpr std::integral_constant<int, C::kFlight - 1> kRest{};
     if (steps > 0) {
-      next = fetch(0);
-      request(0);
-    }
-    if constexpr (C::kPingPong) {
-      if (steps > 0) {
+      for (int n = 0; n < min(C::kFlight, steps); ++n) request(n);
+      if constexpr (C::kPingPong) {
         const bool second = wave >= kNW / 2;
-        // one stage step: store what has arrived, request the next
-        auto advance = [&](int st) DBSA_INLINE {
-          if (st < steps) put(st);
-          if (st + 1 < steps) request(st + 1);
-        };
-        auto phase_end = [&] {
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          __builtin_amdgcn_s_barrier();
-          asm volatile("" ::: "memory");
+        auto advance = [&](int n) DBSA_INLINE {
+          if (n >= steps) return;
+          if constexpr (C::kDirect) {
+            if (n + C::kFlight < steps) request(n + C::kFlight);
+            wait_for(n, kAll);
+            put(n);
+          } else {
+            wait_for(n, kRest);
+            put(n);
+            lds_done();
+            if (n + C::kFlight < steps) request(n + C::kFlight);
+          }
         };
         advance(0);
-        phase_end();
+        barrier();
         if (second) {
           advance(1);
-          phase_end();
+          barrier();
         }
         for (int st = 0; st < steps; ++st) {
           __builtin_amdgcn_s_setprio(1);
           if (st > 0) multiply_product(st - 1);
           multiply_scores(st);
           __builtin_amdgcn_s_setprio(0);
-          phase_end();
+          barrier();
           softmax(st);
           advance(st + 1 + (second ? 1 : 0));
-          phase_end();
+          barrier();
         }
         multiply_product(steps - 1);
-        if (!second) phase_end();
-      }
-    } else {
-      for (int st = 0; st < steps; ++st) {
-        put(st);
-        if (st + 1 < steps) request(st + 1);
-        // one barrier per step: the other stage was last read before the barrier of the step that filled this one
-        __syncthreads();
-        multiply_scores(st);
-        softmax(st);
-        multiply_product(st);
+        if (!second) barrier();
+      } else {
+        // One barrier per step: behind it, step st has landed for all waves, and all have read step st - 1, whose stage
+        // the step requested now takes (8 bits: whose stage the step put before the next barrier takes).
+        for (int st = 0; st < steps; ++st) {
+          wait_for(st, kRest);
+          put(st);
+          if constexpr (!C::kDirect) {
+            lds_done();
+            if (st + C::kFlight < steps) request(st + C::kFlight);
+          }
+          barrier();
+          if constexpr (C::kDirect) {
+            if (st + C::kFlight < steps) request(st + C::kFlight);
+          }
+          multiply_scores(st);
+          softmax(st);
+          multiply_product(st);
+        }
+        // (the next record's first steps must not land under a wave that still reads this one's last)
+        if constexpr (C::kDirect) barrier();
       }
     }
     n_stored += steps;
@@ -660,7 +737,7 @@ hipError_t launch_kind(const ChunkParams& p, hipStream_t stream) {
   hipError_t e = hipErrorInvalidValue;
   if (p.rows == 32) e = launch_shape<T, kD, 1, 32>(p, stream);
   else if (p.rows == 64) e = launch_shape<T, kD, 2, 32>(p, stream);
-  else if (p.rows == 128) e = launch_shape<T, kD, 4, kWide>(p, stream);
+  else if (p.rows == 128) e = launch_shape<T, kD, 4, 32>(p, stream);
   else if (p.rows == 256) e = launch_shape<T, kD, 8, kWide>(p, stream);
   if (e != hipSuccess || !p.merge) return e;
   const int64_t pairs = static_cast<int64_t>(p.n_rows) * p.n_q_heads;

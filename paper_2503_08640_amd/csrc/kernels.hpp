@@ -140,6 +140,7 @@ struct ChunkParams {
   int32_t n_rows;             // new tokens
   int32_t n_q_heads, n_kv_heads, n_workers, rows;
   int32_t merge;              // 1: some records leave partial states
+  int32_t narrow;             // 1: 64 rows of every cache lie within 32 bits of bytes
   float scale_log2e;
 };
 enum class ChunkKind { kBf16, kF32, kE4m3 };
