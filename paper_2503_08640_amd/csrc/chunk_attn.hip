@@ -48,6 +48,7 @@ struct Kind<float> {
 
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) uintx4 lds_piece;
+typedef const __attribute__((address_space(3))) float lds_float;
 
 // dma16 (mfma_common.hpp) with an address of its own per lane
 __device__ inline void dma16_wide(uint64_t address, unsigned lds_addr) {
@@ -397,29 +398,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     for (int ob = 0; ob < kO; ++ob)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[ob][i] = 0.f;
-    floatx16 s[kB];                   // scores, then (fp32) probabilities
+    floatx16 s[kB], s_next[kB];       // scores, then (fp32) probabilities
     bf16x8 pf[kF32 ? 1 : kB][2];      // probabilities as operands of the product
 
-    auto scores = [&](int st) DBSA_INLINE {
-      const unsigned char* const kt = smem + (base + st) % C::kKStages * C::kTileBytes;
-#pragma unroll
-      for (int kb = 0; kb < kB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
-#pragma unroll
-      for (int c = 0; c < kC; ++c)
-#pragma unroll
-        for (int kb = 0; kb < kB; ++kb) {
-          const unsigned char* const at = kt + (k_at ^ (32 * c)) + 32 * kb * C::kRowBytes;
-          if constexpr (kF32) {
-            const floatx4 kf = *reinterpret_cast<const floatx4*>(at);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[c][e], s[kb], 0, 0, 0);
-          } else {
-            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(at), qf[c], s[kb], 0, 0, 0);
-          }
-        }
-    };
     // element i of block kb is key 32 kb + 8 (i / 4) + 4 half + i % 4 of the step
     auto mask = [&](int st) DBSA_INLINE {
       const int ln = lane_here();
@@ -518,59 +499,68 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           }
       }
     };
-    auto product = [&](int st) DBSA_INLINE {
-      const unsigned char* const vt = smem + (C::kKStages + (base + st) % C::kVStages) * C::kTileBytes;
-      if (__builtin_expect(st >= pool_steps && ((partly >> (st % 32)) & 1), 0)) add_poison(st);
-      if constexpr (kF32) {
-#pragma unroll
-        for (int kb = 0; kb < kB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int row = 32 * kb + 8 * (i / 4) + 4 * half + i % 4;
-#pragma unroll
-            for (int ob = 0; ob < kO; ++ob) {
-              const int ch = 32 * ob + l32;
-              const float vf = *reinterpret_cast<const float*>(vt + row * C::kRowBytes + (((ch / 4) ^ C::v_swizzle(row)) * 16) + (ch % 4) * 4);
-              acc[ob] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[kb][i], acc[ob], 0, 0, 0);
-            }
-          }
-      } else {
-#pragma unroll
-        for (int kb = 0; kb < kB; ++kb)
-#pragma unroll
-          for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-            for (int ob = 0; ob < kO; ++ob) {
-              const unsigned char* const at = vt + (v_at ^ (64 * ob)) + (32 * kb + 16 * ch) * C::kRowBytes;
-              const bf16x4 lo = lds_read_tr(reinterpret_cast<const __bf16*>(at));
-              const bf16x4 hi = lds_read_tr(reinterpret_cast<const __bf16*>(at + 8 * C::kRowBytes));
-              const bf16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-              acc[ob] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[kb][ch], acc[ob], 0, 0, 0);
-            }
+    // A run of matrix instructions: O += V(v_step) P, then S = K(k_step) Q (either may be left out).  Fragments are read from LDS
+    // kDist matrix instructions before the one that takes them, in an order the compiler is not left to change: it would
+    // otherwise read each right before its use and wait for it.
+    auto multiply = [&](auto PV, int v_step, auto QK, int k_step) DBSA_INLINE {
+      constexpr int nV = decltype(PV)::value ? (kF32 ? 16 * kB * kO : 2 * kB * kO) : 0, nK = decltype(QK)::value ? kC * kB : 0;
+      constexpr int kDist = kF32 ? 4 : 6;
+      const unsigned vt = lds0 + (C::kKStages + (base + v_step) % C::kVStages) * C::kTileBytes;
+      const unsigned kt = lds0 + (base + k_step) % C::kKStages * C::kTileBytes;
+      if constexpr (nV > 0) {
+        if (__builtin_expect(v_step >= pool_steps && ((partly >> (v_step % 32)) & 1), 0)) add_poison(v_step);
       }
-    };
-    // Order of a run of matrix instructions with their fragments' reads: kAhead reads first, then each instruction with the
-    // reads of a later one.
-    auto pipelined = [&](auto READS, auto COUNT) DBSA_INLINE {
-      constexpr int kReads = decltype(READS)::value, kCount = decltype(COUNT)::value, kAhead = 4;
-      __builtin_amdgcn_sched_group_barrier(0x100, kAhead * kReads, 0);
-      static_for<kCount - kAhead>([&](auto) DBSA_INLINE {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+      if constexpr (nK > 0) {
+#pragma unroll
+        for (int kb = 0; kb < kB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s_next[kb][i] = 0.f;
+      }
+      Piece ring[kDist];  // (fp32: V fragments are single floats)
+      auto read = [&](auto F) DBSA_INLINE {
+        constexpr int f = decltype(F)::value;
+        if constexpr (f < nV && kF32) {
+          constexpr int ob = f % kO, i = f / kO % 16, kb = f / kO / 16, row = 32 * kb + 8 * (i / 4) + i % 4;
+          const int ch = 32 * ob + l32;
+          ring[f % kDist][0] = *reinterpret_cast<lds_float*>(static_cast<uintptr_t>(
+              vt + (row + 4 * half) * C::kRowBytes + (((ch / 4) ^ (8 * ((row / 4 + half) % 2))) * 16) + (ch % 4) * 4));
+        } else if constexpr (f < nV) {
+          constexpr int ob = f % kO, ch = f / kO % 2, kb = f / kO / 2;
+          const lds_byte* const at = reinterpret_cast<const lds_byte*>(static_cast<uintptr_t>(vt + (v_at ^ (64 * ob)))) + (32 * kb + 16 * ch) * C::kRowBytes;
+          const bf16x4 lo = lds_read_tr(at), hi = lds_read_tr(at + 8 * C::kRowBytes);
+          ring[f % kDist] = __builtin_bit_cast(Piece, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+          constexpr int kb = (f - nV) % kB, c = (f - nV) / kB;
+          ring[f % kDist] = *(reinterpret_cast<const __attribute__((address_space(3))) Piece*>(static_cast<uintptr_t>(kt + (k_at ^ (32 * c)))) +
+                              32 * kb * C::kRowBytes / 16);
+        }
+      };
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<(kDist < nV + nK ? kDist : nV + nK)>([&](auto F) DBSA_INLINE { read(F); });
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<nV + nK>([&](auto F) DBSA_INLINE {
+        constexpr int f = decltype(F)::value;
+        if constexpr (f < nV && kF32) {
+          constexpr int ob = f % kO, i = f / kO % 16, kb = f / kO / 16;
+          acc[ob] = __builtin_amdgcn_mfma_f32_32x32x2f32(ring[f % kDist][0], s[kb][i], acc[ob], 0, 0, 0);
+        } else if constexpr (f < nV) {
+          constexpr int ob = f % kO, ch = f / kO % 2, kb = f / kO / 2;
+          acc[ob] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ring[f % kDist]), pf[kb][ch], acc[ob], 0, 0, 0);
+        } else if constexpr (kF32) {
+          constexpr int kb = (f - nV) % kB, c = (f - nV) / kB;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s_next[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(ring[f % kDist][e], qf[c][e], s_next[kb], 0, 0, 0);
+        } else {
+          constexpr int kb = (f - nV) % kB, c = (f - nV) / kB;
+          s_next[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ring[f % kDist]), __builtin_bit_cast(bf16x8, qf[c]), s_next[kb], 0, 0, 0);
+        }
+        if constexpr (f + kDist < nV + nK) read(std::integral_constant<int, f + kDist>{});
+        __builtin_amdgcn_sched_barrier(0);
       });
-      __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
-    };
-    auto multiply_scores = [&](int st) DBSA_INLINE {
-      __builtin_amdgcn_sched_barrier(0);
-      scores(st);
-      if constexpr (!kF32) pipelined(std::integral_constant<int, 1>{}, std::integral_constant<int, kC * kB>{});
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    auto multiply_product = [&](int st) DBSA_INLINE {
-      __builtin_amdgcn_sched_barrier(0);
-      product(st);
-      if constexpr (!kF32) pipelined(std::integral_constant<int, 2>{}, std::integral_constant<int, 2 * kB * kO>{});
-      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (nK > 0) {
+#pragma unroll
+        for (int kb = 0; kb < kB; ++kb) s[kb] = s_next[kb];
+      }
     };
 
     // What happens to step n while step n - 1 is still being read.  (A wave's own ring place is free again once it has read it.)
@@ -580,6 +570,8 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     };
+    constexpr std::true_type kYes{};
+    constexpr std::false_type kNo{};
     constexpr std::integral_constant<int, C::kFlight> kAll{};
     constexpr std::integral_constant<int, C::kFlight - 1> kRest{};
     if (steps > 0) {
@@ -607,15 +599,15 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         }
         for (int st = 0; st < steps; ++st) {
           __builtin_amdgcn_s_setprio(1);
-          if (st > 0) multiply_product(st - 1);
-          multiply_scores(st);
+          if (st > 0) multiply(kYes, st - 1, kYes, st);
+          else multiply(kNo, 0, kYes, 0);
           __builtin_amdgcn_s_setprio(0);
           barrier();
           softmax(st);
           advance(st + 1 + (second ? 1 : 0));
           barrier();
         }
-        multiply_product(steps - 1);
+        multiply(kYes, steps - 1, kNo, 0);
         if (!second) barrier();
       } else {
         // One barrier per step: behind it, step st has landed for all waves, and all have read step st - 1, whose stage
@@ -631,9 +623,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           if constexpr (C::kDirect) {
             if (st + C::kFlight < steps) request(st + C::kFlight);
           }
-          multiply_scores(st);
+          multiply(kNo, 0, kYes, st);
           softmax(st);
-          multiply_product(st);
+          multiply(kYes, st, kNo, 0);
         }
         // (the next record's first steps must not land under a wave that still reads this one's last)
         if constexpr (C::kDirect) barrier();
