@@ -4,8 +4,8 @@
 // Mathematics.  One softmax per row (a new token times a query head) over all its keys, taken in one pass over tiles of
 // keys: with m the running maximum of the scores and l the running sum of 2^(s - m),
 //     m' = max(m, max s),  l' = l 2^(m - m') + sum 2^(s - m'),  acc' = acc 2^(m - m') + sum 2^(s - m') v,   o = acc / l.
-// m, l and acc are held in fp32.  acc and l are only rescaled when a row's maximum has grown by more than kSlack: until then
-// the probabilities stay below 2^kSlack, far inside fp32 and bf16.  Scores are transposed, S^T = K Q^T, so that a lane
+// m, l and acc are held in fp32.  Any m will do that keeps the probabilities in range, so m stays what the row's first keys
+// give it while no score exceeds it by kRoom (walk).  Scores are transposed, S^T = K Q^T, so that a lane
 // holds 16 keys of ONE row per block of 32 keys: maxima and sums need one exchange between the two half-waves and no LDS,
 // and the probabilities are in place as the operand of O^T = V^T P^T.  bf16 products (8-bit caches are widened as they are
 // staged, exactly: every e4m3 value is a bf16 value), fp32 products for fp32 tensors; the only rounding to fewer bits besides
@@ -24,7 +24,7 @@
 namespace {
 using namespace dbsa_mfma;
 
-constexpr float kSlack = 8.f;  // log2 units a row's scores may exceed its running maximum by before acc is rescaled
+constexpr float kRoom = 24.f;  // log2 units a row's scores may exceed its reference maximum by
 
 struct E4m3 {};  // storage of 8-bit caches; q and o are bf16 then
 
@@ -54,6 +54,18 @@ typedef const __attribute__((address_space(3))) float lds_float;
 __device__ inline void dma16_wide(uint64_t address, unsigned lds_addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(address) : "memory");
 }
+
+// O += V P, as statements that change the accumulators where they are (left to itself the compiler keeps two sets of them and
+// copies one to the other in every step).  It does not know what these are, so the spacing rules are kept by the order of the
+// code: an accumulator's next product is at least two matrix instructions away, and the vector ALU reads one only behind
+// product_fence().
+__device__ DBSA_INLINE void product_bf16(floatx16& o, const bf16x8& v, const bf16x8& p) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
+}
+__device__ DBSA_INLINE void product_f32(floatx16& o, float v, float p) {
+  asm volatile("v_mfma_f32_32x32x2_f32 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
+}
+__device__ DBSA_INLINE void product_fence() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 
 // sixteen e4m3 bytes as bf16
 __device__ DBSA_INLINE void widen16(const uintx4& raw, uintx4& lo, uintx4& hi) {
@@ -97,20 +109,10 @@ __device__ DBSA_INLINE float stored_value(const unsigned char* row, int ch) {
 }
 
 // kBN keys per step (a 64-key tile is one or two steps), kNW waves of 32 rows.
-//
-// kPingPong (eight waves, two to a SIMD): the waves form two groups half a step apart.  While one group multiplies
-// (O += V(t-1) P(t-1), then S(t) = K(t) Q: 32 matrix instructions), the other turns its scores into probabilities and
-// fills the stages, so that each SIMD's matrix pipe and vector ALU work at the same time on one wave each; a barrier ends
-// every phase.  Phases of group 0: M(0) S(0) M(1) S(1) ...; group 1 one phase later:
-//     phase 2t    : group 0 multiplies K(t), V(t-1); group 1 is at S(t-1) and stores its pieces of K(t+1), V(t+1)
-//     phase 2t + 1: group 1 multiplies K(t), V(t-1); group 0 is at S(t)   and stores its pieces of K(t+1), V(t+1)
-// K(t+1) takes the place of K(t-1), last read in phase 2t - 1; V(t+1) that of V(t-2), last read in phase 2t - 1: two stages of
-// K, three of V.
 template <typename T, int kD, int kNW, int kBN>
 struct Chunk {
   typedef typename Kind<T>::Q Q;
   static constexpr bool kF32 = Kind<T>::kBytes == 4;
-  static constexpr bool kPingPong = kNW == 8 && !kF32;
   static constexpr int kThreads = 64 * kNW, kRows = 32 * kNW;
   static constexpr int kRowBytes = kD * Kind<T>::kBytes, kTileBytes = kBN * kRowBytes;  // as staged
   static constexpr int kSlots = kRowBytes / 16;                                         // 16-byte places of a staged row
@@ -122,13 +124,12 @@ struct Chunk {
   // Steps requested ahead of the one that is about to be read.  16-bit and fp32 rows go from memory straight into their
   // stage; 8-bit rows into a ring of the wave's own, from where the same lanes widen them into the stages.
   static constexpr bool kDirect = Kind<T>::kStoredBytes != 1;
-  static constexpr int kFlight = kDirect ? (kPingPong ? 2 : kNW == 8 || (kNW == 4 && !kF32) ? 3 : kF32 ? 1 : 2)
-                                         : (kNW == 8 ? 3 : kNW == 4 ? 4 : 6);
-  static constexpr int kKStages = !kDirect ? 2 : kPingPong ? kFlight + 2 : kFlight + 1;
-  static constexpr int kVStages = !kDirect ? (kPingPong ? 3 : 2) : kPingPong ? kFlight + 3 : kFlight + 1;
-  static constexpr int kRingAt = (kKStages + kVStages) * kTileBytes;
-  static constexpr int kPoisonAt = kRingAt + (kDirect ? 0 : kFlight * kThreads * kLoads * 16);  // per stage of V: each wave's mask of poisoned rows
-  static constexpr int kLds = kPoisonAt + kVStages * kNW * 8;
+  static constexpr int kFlight = kDirect ? (kNW == 8 || (kNW == 4 && !kF32) ? 3 : kF32 ? 1 : 2) : (kNW == 8 ? 3 : kNW == 4 ? 4 : 6);
+  static constexpr int kStages = kDirect ? kFlight + 1 : 2;
+  static constexpr int kRingAt = (2 * kStages) * kTileBytes;
+  static constexpr int kRingBytes = kThreads * kLoads * 16;
+  static constexpr int kPoisonAt = kRingAt + (kDirect ? 0 : kFlight * kRingBytes);  // per stage of V: each wave's mask of poisoned rows
+  static constexpr int kVotesAt = kPoisonAt + kStages * kNW * 8, kLds = kVotesAt + kNW * 4;
   static_assert(kPieces <= 32 && 64 % kPieces == 0, "a stored row is fetched by neighbouring lanes of one wave");
   static_assert(kApart ? kOperand * 2 == kThreads : kOperand % kThreads == 0, "whole pieces per thread");
   // K places: xor by row, so that the 16 rows a quarter wave reads of one column lie on different banks; V rows of 16-bit
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
 
   const int tid = threadIdx.x, lane = tid % 64, l32 = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int hk = static_cast<int>(blockIdx.x) % p.n_kv_heads, worker = static_cast<int>(blockIdx.x) / p.n_kv_heads;
+  const int hk = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x) % p.n_kv_heads);
+  const int worker = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x) / p.n_kv_heads);
   const int r = p.n_q_heads / p.n_kv_heads;
   // scores in log2 units: scale * log2 e (and the keys' scale) goes onto them in fp32.  A negative key scale turns the
   // rows of Q around; a scale of nothing stays above zero, so that a masked -inf stays one.
@@ -171,8 +173,28 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
   c2 = fmaxf(fabsf(c2), 1e-30f);
 
   const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_byte*)smem));
-  const const_words entries = (const_words)(reinterpret_cast<uintptr_t>(p.ent));
-  const const_words page_table = (const_words)(reinterpret_cast<uintptr_t>(p.page_table));
+  // What the step loop reads of the arguments, in registers of its own: the compiler otherwise picks the ADDRESS of the
+  // argument (pool or own) and loads it anew in every step, four scalar loads one behind the other.
+  auto own_register = [](auto x) DBSA_INLINE {
+    decltype(x) y;
+    if constexpr (sizeof(x) == 8) y = static_cast<decltype(x)>(uniform64(static_cast<uint64_t>(x)));
+    else y = __builtin_amdgcn_readfirstlane(x);
+    asm volatile("" : "+s"(y));
+    return y;
+  };
+  const const_words entries = (const_words)(own_register(reinterpret_cast<uintptr_t>(p.ent)));
+  const const_words page_table = (const_words)(own_register(reinterpret_cast<uintptr_t>(p.page_table)));
+  const uint64_t kpool = own_register(reinterpret_cast<uint64_t>(p.k_pool.ptr) + hk * p.k_pool.stride_head * kEs);
+  const uint64_t vpool = own_register(reinterpret_cast<uint64_t>(p.v_pool.ptr) + hk * p.v_pool.stride_head * kEs);
+  const uint64_t kown = own_register(reinterpret_cast<uint64_t>(p.k_own.ptr) + hk * p.k_own.stride_head * kEs);
+  const uint64_t vown = own_register(reinterpret_cast<uint64_t>(p.v_own.ptr) + hk * p.v_own.stride_head * kEs);
+  // (bytes; used where they fit: narrow)
+  const int kpool_stride = own_register(static_cast<int>(p.k_pool.stride_tok * kEs)), vpool_stride = own_register(static_cast<int>(p.v_pool.stride_tok * kEs));
+  const int kown_stride = own_register(static_cast<int>(p.k_own.stride_tok * kEs)), vown_stride = own_register(static_cast<int>(p.v_own.stride_tok * kEs));
+  const int64_t page_bytes = own_register(p.stride_page * kEs);
+  const int page_log2 = own_register(p.page_log2), n_pages = own_register(p.n_pages), table_stride = own_register(p.table_stride);
+  const bool narrow = own_register(p.narrow) != 0;
+  const int page_mask = (1 << page_log2) - 1;
   // LDS addresses of fragments: K fragment (kb, c) is row 32 kb + l32, place 2 c + half; V fragment (16-bit: kb, ch, ob) keys
   // 32 kb + 16 ch + 4 half + {0..3, 8..11}, the order the probabilities lie in, read transposed: lane j of 16 fetches four
   // channels of one key and gets four keys of one channel.  (A place is xor-ed: base ^ (32 c), base ^ (64 ob).)
@@ -180,7 +202,24 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
   const int v_at = (4 * half + (lane % 16) / 4) * C::kRowBytes +
                    (((2 * (l32 / 16) + (lane % 4) / 2) ^ C::v_swizzle((lane % 16) / 4)) * 16) + (lane % 2) * 8;
 
-  int n_stored = 0;  // steps staged so far, over all records: their stages
+  // Where a step's K and V lie in LDS (8 bits: and the ring place it lands in); steps take the places in turn, over all records.
+  struct Place {
+    unsigned k, v, ring, k0;
+    __device__ DBSA_INLINE void next_k() { k = k == k0 + (C::kStages - 1) * C::kTileBytes ? k0 : k + C::kTileBytes; }
+    __device__ DBSA_INLINE void next_v() { v = v == k0 + (2 * C::kStages - 1) * C::kTileBytes ? k0 + C::kStages * C::kTileBytes : v + C::kTileBytes; }
+    __device__ DBSA_INLINE void next_ring() { ring = ring == k0 + C::kRingAt + (C::kFlight - 1) * C::kRingBytes ? k0 + C::kRingAt : ring + C::kRingBytes; }
+    // a step that lands in its stage
+    __device__ DBSA_INLINE void next_direct() {
+      if (C::kDirect) {
+        next_k();
+        next_v();
+      } else {
+        next_ring();
+      }
+    }
+  };
+  const Place start{lds0, lds0 + C::kStages * C::kTileBytes, lds0 + C::kRingAt, lds0};
+  Place wanted = start, arrived = start, read = start;  // of the step requested next, put next; K and V read next
   const const_words workers = (const_words)(reinterpret_cast<uintptr_t>(p.ptr));
   const const_words tokens = (const_words)(reinterpret_cast<uintptr_t>(p.toks));
   const const_words lengths = (const_words)(reinterpret_cast<uintptr_t>(p.self_len));
@@ -219,7 +258,6 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       own_steps = (hi - lo) * kSteps;
     }
     const int pool_steps = n_ent * kSteps, steps = pool_steps + own_steps;
-    const int base = n_stored;
 
     // ---- the stream of steps ----
     // What a step hangs off: its list entry, or the pages of its keys (scalar loads, requested one step before its rows).
@@ -236,20 +274,22 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         x.start = e[0];
         x.len = e[1];
       } else {
-        const int first = (own_first + (s - pool_steps) * kBN) >> p.page_log2;
-        const const_words table = page_table + static_cast<int64_t>(own_u) * p.table_stride;
+        const int first = (own_first + (s - pool_steps) * kBN) >> page_log2;
+        const const_words table = page_table + static_cast<int64_t>(own_u) * table_stride;
+        x.page[0] = table[min(first, table_stride - 1)];
+        if (page_mask < kBN - 1) {
 #pragma unroll
-        for (int i = 0; i < kPages; ++i)  // (entries behind the step's last page are not used)
-          if (i == 0 || (1 << p.page_log2) < kBN) x.page[i] = table[min(first + i, p.table_stride - 1)];
+          for (int i = 1; i < kPages; ++i) x.page[i] = table[min(first + i, table_stride - 1)];  // (those behind the step are not used)
+        }
       }
       return x;
     };
-    auto page_there = [&](int page) DBSA_INLINE { return page >= 0 && page < p.n_pages; };
+    auto page_there = [&](int page) DBSA_INLINE { return page >= 0 && page < n_pages; };
     // page of key `key` of an own step
     auto page_of = [&](const Ahead& x, int key) DBSA_INLINE {
       int page = x.page[0];
-      if ((1 << p.page_log2) < kBN) {
-        const int at = key >> p.page_log2;
+      if (page_mask < kBN - 1) {
+        const int at = key >> page_log2;
 #pragma unroll
         for (int i = 1; i < kPages; ++i) page = at == i ? x.page[i] : page;
       }
@@ -260,76 +300,86 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       const int ln = lane_here();
       return __builtin_amdgcn_ballot_w64(ln < kBN && first + ln < own_n && page_there(page_of(x, ln)));
     };
-    constexpr uint64_t kAllKeys = kBN == 64 ? ~0ull : (1ull << kBN) - 1;
+    constexpr uint64_t kAllKeys = ~0ull >> (64 - kBN);
 
     // This thread's pieces of a step: piece tid + i threads of K, then of V; the operand of piece i is the wave's.
     auto is_v = [&](int i) DBSA_INLINE { return C::kApart ? wave >= kNW / 2 : i >= C::kLoads / 2; };
     auto piece_row = [&](int i, int t) DBSA_INLINE { return (t + i * C::kThreads) % C::kOperand / C::kPieces; };
     // first row of the rows that wave and pass i fetch (1 KiB: 64 pieces)
     auto wave_row = [&](int i) DBSA_INLINE { return (64 * wave + i * C::kThreads) % C::kOperand / C::kPieces; };
-    // where piece i of step s lands: places of a stage are xor-ed on the way (the lane fetches the piece that belongs there), the
-    // ring holds pieces as they come
-    auto landing = [&](int s, int i) DBSA_INLINE {
+    // where piece i of the step at `place` lands: places of a stage are xor-ed on the way (the lane fetches the piece that belongs
+    // there), the ring holds pieces as they come
+    auto landing = [&](const Place& place, int i) DBSA_INLINE {
       unsigned at;
-      if constexpr (C::kDirect)
-        at = (is_v(i) ? C::kKStages + (base + s) % C::kVStages : (base + s) % C::kKStages) * C::kTileBytes + wave_row(i) * C::kRowBytes;
-      else
-        at = C::kRingAt + (((base + s) % C::kFlight * C::kLoads + i) * kNW + wave) * 1024;
-      return static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds0 + at)));
+      if constexpr (C::kDirect) at = (is_v(i) ? place.v : place.k) + wave_row(i) * C::kRowBytes;
+      else at = place.ring + (i * kNW + wave) * 1024;
+      return static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(at)));
     };
     auto fetched_col = [&](int i, int t) DBSA_INLINE {
       const int col = t % C::kPieces, row = piece_row(i, t);
       return (C::kDirect ? col ^ (is_v(i) ? C::v_swizzle(row) : C::k_swizzle(row)) : col) * 16;
     };
-    uint32_t partly = 0;  // bit s % 32: some row does not see some key of step s (kept until its product is done)
-    Ahead next = fetch(0);
+    bool again;           // the quick walk does not do for this record (see there)
+    uint32_t partly;      // bit s % 32: some row does not see some key of step s (kept until its product is done)
+    Ahead next;
     auto request = [&](int s) DBSA_INLINE {  // s < steps: what it hangs off is in `next`
       const Ahead x = next;
       next = fetch(min(s + 1, steps - 1));
       const bool own = s >= pool_steps;
-      const int off = own ? own_first + (s - pool_steps) * kBN : (s % kSteps) * kBN;
-      const int len = own ? min(own_n - off, kBN) : min((x.len & 0xFFFF) - off, kBN);
-      const bool one_page = own && (1 << p.page_log2) >= kBN;
-      bool whole = len == kBN;
-      if (own) {
-        whole = whole && off + kBN - 1 <= first_pos;
-        if (one_page) whole = whole && page_there(x.page[0]);
-        else whole = whole && keys_there(x, off) == kAllKeys;
+      uint64_t kt = kpool, vt = vpool;
+      int ks = kpool_stride, vs = vpool_stride, off, len, row;
+      bool whole, in_line;  // in_line: kBN rows one after the other
+      if (!own) {
+        off = kSteps == 1 ? 0 : (s % kSteps) * kBN;
+        len = min((x.len & 0xFFFF) - off, kBN);
+        row = x.start + off;
+        whole = in_line = len == kBN;
+      } else {
+        off = own_first + (s - pool_steps) * kBN;
+        len = min(own_n - off, kBN);
+        whole = len == kBN && off + kBN - 1 <= first_pos;
+        row = off & page_mask;
+        in_line = false;
+        if (page_mask >= kBN - 1) {
+          in_line = len == kBN && page_there(x.page[0]);
+          whole = whole && in_line;
+        } else if (whole) {
+          whole = keys_there(x, off) == kAllKeys;
+        }
+        kt = kown + x.page[0] * page_bytes;
+        vt = vown + x.page[0] * page_bytes;
+        ks = kown_stride;
+        vs = vown_stride;
       }
       const uint32_t bit = 1u << (s % 32);
       partly = whole ? partly & ~bit : partly | bit;
-      const int64_t ks = (own ? p.k_own.stride_tok : p.k_pool.stride_tok) * kEs, vs = (own ? p.v_own.stride_tok : p.v_pool.stride_tok) * kEs;
-      const unsigned char* const kb = static_cast<const unsigned char*>(own ? p.k_own.ptr : p.k_pool.ptr) +
-                                      hk * (own ? p.k_own.stride_head : p.k_pool.stride_head) * kEs;
-      const unsigned char* const vb = static_cast<const unsigned char*>(own ? p.v_own.ptr : p.v_pool.ptr) +
-                                      hk * (own ? p.v_own.stride_head : p.v_pool.stride_head) * kEs;
-      if (__builtin_expect(p.narrow && whole && (!own || one_page), 1)) {
-        // kBN rows one after the other
-        const int64_t page = own ? x.page[0] * p.stride_page * kEs : 0;
-        const int row = own ? off & ((1 << p.page_log2) - 1) : x.start + off;
-        const uint64_t kt = reinterpret_cast<uint64_t>(kb) + page + row * ks, vt = reinterpret_cast<uint64_t>(vb) + page + row * vs;
+      if (__builtin_expect(in_line && narrow, 1)) {
+        kt += static_cast<int64_t>(row) * ks;
+        vt += static_cast<int64_t>(row) * vs;
 #pragma unroll
         for (int i = 0; i < C::kLoads; ++i) {
-          const int64_t stride = is_v(i) ? vs : ks;
+          const int stride = is_v(i) ? vs : ks;
           const int row0 = i * C::kThreads % C::kOperand / C::kPieces;  // (whole rows per pass of the threads)
-          dma16(uniform64((is_v(i) ? vt : kt) + row0 * stride),
-                static_cast<unsigned>(piece_row(0, tid) * static_cast<int>(stride) + fetched_col(i, tid)), landing(s, i));
+          dma16(uniform64((is_v(i) ? vt : kt) + static_cast<unsigned>(row0 * stride)),
+                static_cast<unsigned>(piece_row(0, tid) * stride + fetched_col(i, tid)), landing(wanted, i));
         }
-        return;
-      }
-      const int t = 64 * wave + lane_here();
+      } else {
+        const int t = 64 * wave + lane_here();
+        const int64_t ks64 = (own ? p.k_own.stride_tok : p.k_pool.stride_tok) * kEs, vs64 = (own ? p.v_own.stride_tok : p.v_pool.stride_tok) * kEs;
 #pragma unroll
-      for (int i = 0; i < C::kLoads; ++i) {
-        const int key = piece_row(i, t);
-        int64_t at;
-        if (own) {
-          const int page = page_of(x, key);
-          at = key < len && page_there(page) ? page * p.stride_page * kEs + ((off + key) & ((1 << p.page_log2) - 1)) * (is_v(i) ? vs : ks) : 0;
-        } else {
-          at = (x.start + (len > 0 ? off + min(key, len - 1) : 0)) * (is_v(i) ? vs : ks);
+        for (int i = 0; i < C::kLoads; ++i) {
+          const int key = piece_row(i, t);
+          int64_t at;
+          if (own) {
+            const int page = page_of(x, key);
+            at = key < len && page_there(page) ? page * page_bytes + ((off + key) & page_mask) * (is_v(i) ? vs64 : ks64) : 0;
+          } else {
+            at = (x.start + (len > 0 ? off + min(key, len - 1) : 0)) * (is_v(i) ? vs64 : ks64);
+          }
+          dma16_wide((own ? (is_v(i) ? vown : kown) : (is_v(i) ? vpool : kpool)) + at + fetched_col(i, t), landing(wanted, i));
         }
-        dma16_wide(reinterpret_cast<uint64_t>(is_v(i) ? vb : kb) + at + fetched_col(i, t), landing(s, i));
       }
+      wanted.next_direct();
     };
     // step s has landed, as far as this wave fetched it; `newer` steps were requested since
     auto wait_for = [&](int s, auto NEWER) DBSA_INLINE {
@@ -358,7 +408,8 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         }
         if (missing || ((bad >> (ln / C::kPieces * C::kPieces)) & kRowLanes)) raw[i] = uintx4{0, 0, 0, 0};
       }
-      if (ln == 0) poison[(base + s) % C::kVStages * kNW + wave] = mask;
+      if (ln == 0) poison[(arrived.v - start.v) / C::kTileBytes * kNW + wave] = mask;
+      again |= mask != 0;
     };
     // What this wave does to its landed pieces of step s before the others read them.
     auto put = [&](int s) DBSA_INLINE {
@@ -368,37 +419,38 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           uintx4 raw[C::kLoads];
           const int ln = lane_here();
 #pragma unroll
-          for (int i = 0; i < C::kLoads; ++i) raw[i] = *reinterpret_cast<const lds_piece*>(static_cast<uintptr_t>(landing(s, i) + ln * 16));
+          for (int i = 0; i < C::kLoads; ++i) raw[i] = *reinterpret_cast<const lds_piece*>(static_cast<uintptr_t>(landing(arrived, i) + ln * 16));
           clean(s, raw);
 #pragma unroll
-          for (int i = 0; i < C::kLoads; ++i) *reinterpret_cast<lds_piece*>(static_cast<uintptr_t>(landing(s, i) + ln * 16)) = raw[i];
+          for (int i = 0; i < C::kLoads; ++i) *reinterpret_cast<lds_piece*>(static_cast<uintptr_t>(landing(arrived, i) + ln * 16)) = raw[i];
         }
+        arrived.next_k();
+        arrived.next_v();
       } else {
         uintx4 raw[C::kLoads];
 #pragma unroll
-        for (int i = 0; i < C::kLoads; ++i) raw[i] = *reinterpret_cast<const lds_piece*>(static_cast<uintptr_t>(landing(s, i) + lane * 16));
+        for (int i = 0; i < C::kLoads; ++i) raw[i] = *reinterpret_cast<const lds_piece*>(static_cast<uintptr_t>(landing(arrived, i) + lane * 16));
         if (__builtin_expect(own_partly, 0)) clean(s, raw);
 #pragma unroll
         for (int i = 0; i < C::kLoads; ++i) {
           const int row = piece_row(i, tid), col = tid % C::kPieces;
-          unsigned char* const at = smem + (is_v(i) ? C::kKStages + (base + s) % C::kVStages : (base + s) % C::kKStages) * C::kTileBytes + row * C::kRowBytes;
+          const unsigned at = (is_v(i) ? arrived.v : arrived.k) + row * C::kRowBytes;
           const int swizzle = is_v(i) ? C::v_swizzle(row) : C::k_swizzle(row);
           uintx4 lo, hi;
           widen16(raw[i], lo, hi);
-          *reinterpret_cast<uintx4*>(at + ((2 * col) ^ swizzle) * 16) = lo;
-          *reinterpret_cast<uintx4*>(at + ((2 * col + 1) ^ swizzle) * 16) = hi;
+          *reinterpret_cast<lds_piece*>(static_cast<uintptr_t>(at + ((2 * col) ^ swizzle) * 16)) = lo;
+          *reinterpret_cast<lds_piece*>(static_cast<uintptr_t>(at + ((2 * col + 1) ^ swizzle) * 16)) = hi;
         }
+        arrived.next_k();
+        arrived.next_v();
+        arrived.next_ring();
       }
     };
 
     // ---- softmax state ----
     floatx16 acc[kO];
-    float m = -INFINITY, l = 0.f;  // l: this lane's keys' share
-#pragma unroll
-    for (int ob = 0; ob < kO; ++ob)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[ob][i] = 0.f;
-    floatx16 s[kB], s_next[kB];       // scores, then (fp32) probabilities
+    float m, l;                       // l: this lane's keys' share
+    floatx16 s[kB];                   // scores, then (fp32) probabilities
     bf16x8 pf[kF32 ? 1 : kB][2];      // probabilities as operands of the product
 
     // element i of block kb is key 32 kb + 8 (i / 4) + 4 half + i % 4 of the step
@@ -424,7 +476,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           if (key > last || !((there >> key) & 1)) s[kb][i] = -INFINITY;
         }
     };
-    auto softmax = [&](int st) DBSA_INLINE {
+    auto softmax = [&](auto CAREFUL, int st) DBSA_INLINE {
       if (__builtin_expect((partly >> (st % 32)) & 1, 0)) mask(st);
       float top = s[0][0];
 #pragma unroll
@@ -432,15 +484,16 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
       top = half_swap_max(top) * c2;
-      if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+      if constexpr (!decltype(CAREFUL)::value) {
+        m = m == -INFINITY ? top : m;
+        again |= top > m + kRoom;
+      } else if (__builtin_amdgcn_ballot_w64(top > m) != 0) {
         const float bigger = fmaxf(m, top);
         const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - bigger);
         m = bigger;
         l *= alpha;
 #pragma unroll
-        for (int ob = 0; ob < kO; ++ob)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[ob][i] *= alpha;
+        for (int ob = 0; ob < kO; ++ob) acc[ob] *= alpha;
       }
       const float less = m == -INFINITY ? 0.f : -m;
       float sum = 0.f;
@@ -469,16 +522,16 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     // the keys that take_poison kept out of the product
     auto add_poison = [&](int st) DBSA_INLINE {
       uint64_t keys = 0;
-      for (int i = 0; i < kNW; ++i) keys |= poison[(base + st) % C::kVStages * kNW + i];
+      for (int i = 0; i < kNW; ++i) keys |= poison[(read.v - start.v) / C::kTileBytes * kNW + i];
       keys = uniform64(keys);
       const int h = lane_here() / 32;
       while (keys) {
         const int key = __builtin_ctzll(keys);
         keys &= keys - 1;
         const int j = own_first + (st - pool_steps) * kBN + key;
-        const int64_t page = p.page_table[static_cast<int64_t>(own_u) * p.table_stride + (j >> p.page_log2)];
+        const int64_t page = page_table[static_cast<int64_t>(own_u) * table_stride + (j >> page_log2)];
         const unsigned char* const v = static_cast<const unsigned char*>(p.v_own.ptr) +
-            (hk * p.v_own.stride_head + page * p.stride_page + (j & ((1 << p.page_log2) - 1)) * p.v_own.stride_tok) * kEs;
+            (hk * p.v_own.stride_head + page * p.stride_page + (j & page_mask) * p.v_own.stride_tok) * kEs;
         float mine = 0.f;  // the key's probability, in the half-wave that holds the key
 #pragma unroll
         for (int kb = 0; kb < kB; ++kb)
@@ -499,25 +552,31 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           }
       }
     };
-    // A run of matrix instructions: O += V(v_step) P, then S = K(k_step) Q (either may be left out).  Fragments are read from LDS
+    // A run of matrix instructions: O += V P of step v_step, then S = K Q of the step behind the last one scored (either may be left out).  Fragments are read from LDS
     // kDist matrix instructions before the one that takes them, in an order the compiler is not left to change: it would
     // otherwise read each right before its use and wait for it.
-    auto multiply = [&](auto PV, int v_step, auto QK, int k_step) DBSA_INLINE {
+    auto multiply = [&](auto CAREFUL, auto PV, int v_step, auto QK) DBSA_INLINE {
       constexpr int nV = decltype(PV)::value ? (kF32 ? 16 * kB * kO : 2 * kB * kO) : 0, nK = decltype(QK)::value ? kC * kB : 0;
       constexpr int kDist = kF32 ? 4 : 6;
-      const unsigned vt = lds0 + (C::kKStages + (base + v_step) % C::kVStages) * C::kTileBytes;
-      const unsigned kt = lds0 + (base + k_step) % C::kKStages * C::kTileBytes;
+      const unsigned vt = read.v, kt = read.k;
+      int k_here = k_at, v_here = v_at;  // (a fragment's address is one instruction from these; kept, they are twelve registers)
+      asm volatile("" : "+v"(k_here), "+v"(v_here));
       if constexpr (nV > 0) {
-        if (__builtin_expect(v_step >= pool_steps && ((partly >> (v_step % 32)) & 1), 0)) add_poison(v_step);
+        if constexpr (decltype(CAREFUL)::value) {
+          if (v_step >= pool_steps && ((partly >> (v_step % 32)) & 1)) add_poison(v_step);
+        }
+        read.next_v();
       }
+      if constexpr (nK > 0) read.next_k();
+      if constexpr (nV > 0 && decltype(CAREFUL)::value) product_fence();
       if constexpr (nK > 0) {
 #pragma unroll
         for (int kb = 0; kb < kB; ++kb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s_next[kb][i] = 0.f;
+          for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
       }
       Piece ring[kDist];  // (fp32: V fragments are single floats)
-      auto read = [&](auto F) DBSA_INLINE {
+      auto read_fragment = [&](auto F) DBSA_INLINE {
         constexpr int f = decltype(F)::value;
         if constexpr (f < nV && kF32) {
           constexpr int ob = f % kO, i = f / kO % 16, kb = f / kO / 16, row = 32 * kb + 8 * (i / 4) + i % 4;
@@ -526,41 +585,37 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
               vt + (row + 4 * half) * C::kRowBytes + (((ch / 4) ^ (8 * ((row / 4 + half) % 2))) * 16) + (ch % 4) * 4));
         } else if constexpr (f < nV) {
           constexpr int ob = f % kO, ch = f / kO % 2, kb = f / kO / 2;
-          const lds_byte* const at = reinterpret_cast<const lds_byte*>(static_cast<uintptr_t>(vt + (v_at ^ (64 * ob)))) + (32 * kb + 16 * ch) * C::kRowBytes;
+          const lds_byte* const at = reinterpret_cast<const lds_byte*>(static_cast<uintptr_t>(vt + (v_here ^ (64 * ob)))) + (32 * kb + 16 * ch) * C::kRowBytes;
           const bf16x4 lo = lds_read_tr(at), hi = lds_read_tr(at + 8 * C::kRowBytes);
           ring[f % kDist] = __builtin_bit_cast(Piece, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
           constexpr int kb = (f - nV) % kB, c = (f - nV) / kB;
-          ring[f % kDist] = *(reinterpret_cast<const __attribute__((address_space(3))) Piece*>(static_cast<uintptr_t>(kt + (k_at ^ (32 * c)))) +
+          ring[f % kDist] = *(reinterpret_cast<const __attribute__((address_space(3))) Piece*>(static_cast<uintptr_t>(kt + (k_here ^ (32 * c)))) +
                               32 * kb * C::kRowBytes / 16);
         }
       };
       __builtin_amdgcn_sched_barrier(0);
-      static_for<(kDist < nV + nK ? kDist : nV + nK)>([&](auto F) DBSA_INLINE { read(F); });
+      static_for<(kDist < nV + nK ? kDist : nV + nK)>([&](auto F) DBSA_INLINE { read_fragment(F); });
       __builtin_amdgcn_sched_barrier(0);
       static_for<nV + nK>([&](auto F) DBSA_INLINE {
         constexpr int f = decltype(F)::value;
         if constexpr (f < nV && kF32) {
           constexpr int ob = f % kO, i = f / kO % 16, kb = f / kO / 16;
-          acc[ob] = __builtin_amdgcn_mfma_f32_32x32x2f32(ring[f % kDist][0], s[kb][i], acc[ob], 0, 0, 0);
+          product_f32(acc[ob], ring[f % kDist][0], s[kb][i]);
         } else if constexpr (f < nV) {
           constexpr int ob = f % kO, ch = f / kO % 2, kb = f / kO / 2;
-          acc[ob] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ring[f % kDist]), pf[kb][ch], acc[ob], 0, 0, 0);
+          product_bf16(acc[ob], __builtin_bit_cast(bf16x8, ring[f % kDist]), pf[kb][ch]);
         } else if constexpr (kF32) {
           constexpr int kb = (f - nV) % kB, c = (f - nV) / kB;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s_next[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(ring[f % kDist][e], qf[c][e], s_next[kb], 0, 0, 0);
+          for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(ring[f % kDist][e], qf[c][e], s[kb], 0, 0, 0);
         } else {
           constexpr int kb = (f - nV) % kB, c = (f - nV) / kB;
-          s_next[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ring[f % kDist]), __builtin_bit_cast(bf16x8, qf[c]), s_next[kb], 0, 0, 0);
+          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ring[f % kDist]), __builtin_bit_cast(bf16x8, qf[c]), s[kb], 0, 0, 0);
         }
-        if constexpr (f + kDist < nV + nK) read(std::integral_constant<int, f + kDist>{});
+        if constexpr (f + kDist < nV + nK) read_fragment(std::integral_constant<int, f + kDist>{});
         __builtin_amdgcn_sched_barrier(0);
       });
-      if constexpr (nK > 0) {
-#pragma unroll
-        for (int kb = 0; kb < kB; ++kb) s[kb] = s_next[kb];
-      }
     };
 
     // What happens to step n while step n - 1 is still being read.  (A wave's own ring place is free again once it has read it.)
@@ -572,67 +627,77 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     };
     constexpr std::true_type kYes{};
     constexpr std::false_type kNo{};
-    constexpr std::integral_constant<int, C::kFlight> kAll{};
-    constexpr std::integral_constant<int, C::kFlight - 1> kRest{};
-    if (steps > 0) {
-      for (int n = 0; n < min(C::kFlight, steps); ++n) request(n);
-      if constexpr (C::kPingPong) {
-        const bool second = wave >= kNW / 2;
-        auto advance = [&](int n) DBSA_INLINE {
-          if (n >= steps) return;
-          if constexpr (C::kDirect) {
-            if (n + C::kFlight < steps) request(n + C::kFlight);
-            wait_for(n, kAll);
-            put(n);
-          } else {
-            wait_for(n, kRest);
-            put(n);
-            lds_done();
-            if (n + C::kFlight < steps) request(n + C::kFlight);
-          }
-        };
-        advance(0);
-        barrier();
-        if (second) {
-          advance(1);
-          barrier();
-        }
-        for (int st = 0; st < steps; ++st) {
-          __builtin_amdgcn_s_setprio(1);
-          if (st > 0) multiply(kYes, st - 1, kYes, st);
-          else multiply(kNo, 0, kYes, 0);
-          __builtin_amdgcn_s_setprio(0);
-          barrier();
-          softmax(st);
-          advance(st + 1 + (second ? 1 : 0));
-          barrier();
-        }
-        multiply(kYes, steps - 1, kNo, 0);
-        if (!second) barrier();
-      } else {
-        // One barrier per step: behind it, step st has landed for all waves, and all have read step st - 1, whose stage
-        // the step requested now takes (8 bits: whose stage the step put before the next barrier takes).
-        for (int st = 0; st < steps; ++st) {
-          wait_for(st, kRest);
+    // All steps of the record.  The quick walk never touches the accumulators but in the product (a block that sometimes
+    // scales them costs a copy of all of them in every step): a row's reference maximum is that of the first step in which it
+    // sees a key, and later scores may exceed it by kRoom, where probabilities, their sums and the accumulators are still far
+    // inside fp32 and bf16.  Rows whose scores grow further, and values that are not finite under a mask, send the
+    // workgroup through the record once more, carefully: with the running maximum, and the poisoned keys one by one.
+    auto begin_walk = [&]() DBSA_INLINE {
+      m = -INFINITY;
+      l = 0.f;
+      again = false;
+#pragma unroll
+      for (int ob = 0; ob < kO; ++ob)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[ob][i] = 0.f;
+      partly = 0;
+      next = fetch(0);
+    };
+    auto walk = [&]() DBSA_INLINE {
+      begin_walk();
+      // One barrier per step: behind it, step st has landed for all waves, and all have read step st - 1, whose stage
+      // the step requested now takes (8 bits: whose stage the step put before the next barrier takes).
+      for (int st = -C::kFlight; st < steps; ++st) {
+        if (st >= 0) {
+          wait_for(st, std::integral_constant<int, C::kFlight - 1>{});
           put(st);
-          if constexpr (!C::kDirect) {
-            lds_done();
-            if (st + C::kFlight < steps) request(st + C::kFlight);
-          }
           barrier();
-          if constexpr (C::kDirect) {
-            if (st + C::kFlight < steps) request(st + C::kFlight);
-          }
-          multiply(kNo, 0, kYes, st);
-          softmax(st);
-          multiply(kYes, st, kNo, 0);
         }
-        // (the next record's first steps must not land under a wave that still reads this one's last)
-        if constexpr (C::kDirect) barrier();
+        if (st + C::kFlight < steps) request(st + C::kFlight);
+        if (st < 0) continue;
+        multiply(kNo, kNo, 0, kYes);
+        softmax(kNo, st);
+        multiply(kNo, kYes, st, kNo);
       }
+    };
+    // step by step, nothing ahead
+    auto walk_carefully = [&]() DBSA_INLINE {
+      begin_walk();
+      for (int st = 0; st < steps; ++st) {
+        request(st);
+        wait_vmcnt<0>();
+        put(st);
+        barrier();
+        multiply(kYes, kNo, 0, kYes);
+        softmax(kYes, st);
+        multiply(kYes, kYes, st, kNo);
+        barrier();
+      }
+    };
+    if (steps > 0) {
+      walk();
+      // (behind this barrier every wave is done with the stages: the next walk's first steps may land)
+      uint32_t* const votes = reinterpret_cast<uint32_t*>(smem + C::kVotesAt);
+      const bool any = __builtin_amdgcn_ballot_w64(again) != 0;
+      if (lane == 0) votes[wave] = any ? 1 : 0;
+      barrier();
+      uint32_t all = 0;
+#pragma unroll
+      for (int i = 0; i < kNW; ++i) all |= votes[i];
+      if (__builtin_expect(__builtin_amdgcn_readfirstlane(static_cast<int>(all)) != 0, 0)) {
+        barrier();
+        walk_carefully();
+      }
+    } else {
+      m = -INFINITY;
+      l = 0.f;
+#pragma unroll
+      for (int ob = 0; ob < kO; ++ob)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[ob][i] = 0.f;
     }
-    n_stored += steps;
 
+    product_fence();
     // ---- what the record leaves ----
     const float sum = half_swap_sum(l);
     const int row_head = hk * r + row_index % r;
