@@ -125,11 +125,13 @@ struct Chunk {
   // stage; 8-bit rows into a ring of the wave's own, from where the same lanes widen them into the stages.
   static constexpr bool kDirect = Kind<T>::kStoredBytes != 1;
   static constexpr int kFlight = kDirect ? (kNW == 8 || (kNW == 4 && !kF32) ? 3 : kF32 ? 1 : 2) : (kNW == 8 ? 3 : kNW == 4 ? 4 : 6);
-  static constexpr int kStages = kDirect ? kFlight + 1 : 2;
-  static constexpr int kRingAt = (2 * kStages) * kTileBytes;
+  // Eight waves of 16-bit operands run as a pipeline over half steps (walk): V is read one step behind K.
+  static constexpr bool kPipelined = kNW == 8 && !kF32;
+  static constexpr int kKStages = kDirect ? kFlight + 1 : 2, kVStages = kKStages + (kPipelined ? 1 : 0);
+  static constexpr int kRingAt = (kKStages + kVStages) * kTileBytes;
   static constexpr int kRingBytes = kThreads * kLoads * 16;
   static constexpr int kPoisonAt = kRingAt + (kDirect ? 0 : kFlight * kRingBytes);  // per stage of V: each wave's mask of poisoned rows
-  static constexpr int kVotesAt = kPoisonAt + kStages * kNW * 8, kLds = kVotesAt + kNW * 4;
+  static constexpr int kVotesAt = kPoisonAt + kVStages * kNW * 8, kLds = kVotesAt + kNW * 4;
   static_assert(kPieces <= 32 && 64 % kPieces == 0, "a stored row is fetched by neighbouring lanes of one wave");
   static_assert(kApart ? kOperand * 2 == kThreads : kOperand % kThreads == 0, "whole pieces per thread");
   // K places: xor by row, so that the 16 rows a quarter wave reads of one column lie on different banks; V rows of 16-bit
@@ -205,8 +207,8 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
   // Where a step's K and V lie in LDS (8 bits: and the ring place it lands in); steps take the places in turn, over all records.
   struct Place {
     unsigned k, v, ring, k0;
-    __device__ DBSA_INLINE void next_k() { k = k == k0 + (C::kStages - 1) * C::kTileBytes ? k0 : k + C::kTileBytes; }
-    __device__ DBSA_INLINE void next_v() { v = v == k0 + (2 * C::kStages - 1) * C::kTileBytes ? k0 + C::kStages * C::kTileBytes : v + C::kTileBytes; }
+    __device__ DBSA_INLINE void next_k() { k = k == k0 + (C::kKStages - 1) * C::kTileBytes ? k0 : k + C::kTileBytes; }
+    __device__ DBSA_INLINE void next_v() { v = v == k0 + (C::kKStages + C::kVStages - 1) * C::kTileBytes ? k0 + C::kKStages * C::kTileBytes : v + C::kTileBytes; }
     __device__ DBSA_INLINE void next_ring() { ring = ring == k0 + C::kRingAt + (C::kFlight - 1) * C::kRingBytes ? k0 + C::kRingAt : ring + C::kRingBytes; }
     // a step that lands in its stage
     __device__ DBSA_INLINE void next_direct() {
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       }
     }
   };
-  const Place start{lds0, lds0 + C::kStages * C::kTileBytes, lds0 + C::kRingAt, lds0};
+  const Place start{lds0, lds0 + C::kKStages * C::kTileBytes, lds0 + C::kRingAt, lds0};
   Place wanted = start, arrived = start, read = start;  // of the step requested next, put next; K and V read next
   const const_words workers = (const_words)(reinterpret_cast<uintptr_t>(p.ptr));
   const const_words tokens = (const_words)(reinterpret_cast<uintptr_t>(p.toks));
@@ -454,7 +456,8 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     bf16x8 pf[kF32 ? 1 : kB][2];      // probabilities as operands of the product
 
     // element i of block kb is key 32 kb + 8 (i / 4) + 4 half + i % 4 of the step
-    auto mask = [&](int st) DBSA_INLINE {
+    auto mask = [&](int st, auto KB) DBSA_INLINE {
+      constexpr int kb = decltype(KB)::value;
       const int ln = lane_here();
       uint64_t there = ~0ull;
       int last;
@@ -469,55 +472,74 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       last -= 4 * (ln / 32);
       there >>= 4 * (ln / 32);
 #pragma unroll
-      for (int kb = 0; kb < kB; ++kb)
+      for (int i = 0; i < 16; ++i) {
+        const int key = 32 * kb + 8 * (i / 4) + i % 4;
+        if (key > last || !((there >> key) & 1)) s[kb][i] = -INFINITY;
+      }
+    };
+    auto row_max = [&](auto KB) DBSA_INLINE {
+      constexpr int kb = decltype(KB)::value;
+      float top = s[kb][0];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = 32 * kb + 8 * (i / 4) + i % 4;
-          if (key > last || !((there >> key) & 1)) s[kb][i] = -INFINITY;
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+      return half_swap_max(top) * c2;
+    };
+    // the scores of half step (st, kb) masked, and a reference maximum for rows that had none
+    auto prepare = [&](int st, auto KB) DBSA_INLINE {
+      if (__builtin_expect((partly >> (st % 32)) & 1, 0)) mask(st, KB);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(m == -INFINITY) != 0, 0)) {
+        const float top = row_max(KB);
+        m = m == -INFINITY ? top : m;
+      }
+    };
+    // a step's sum of probabilities in one lane above this: some score has outgrown its reference by more than kRoom, give or take
+    const float outgrown = __builtin_exp2f(kRoom);
+    // one probability and its share of the sum
+    auto probability = [&](float score, float less) DBSA_INLINE { return __builtin_amdgcn_exp2f(fmaf(score, c2, less)); };
+    auto pack = [&](auto KB) DBSA_INLINE {
+      constexpr int kb = decltype(KB)::value;
+      if constexpr (!kF32) {
+#pragma unroll
+        for (int ch = 0; ch < 2; ++ch) {
+          union {
+            bf16x8 v;
+            bf16x2 p2[4];
+          } x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x.p2[e] = __builtin_convertvector(floatx2{s[kb][8 * ch + 2 * e], s[kb][8 * ch + 2 * e + 1]}, bf16x2);
+          pf[kb][ch] = x.v;
         }
+      }
     };
     auto softmax = [&](auto CAREFUL, int st) DBSA_INLINE {
-      if (__builtin_expect((partly >> (st % 32)) & 1, 0)) mask(st);
-      float top = s[0][0];
+      static_for<kB>([&](auto KB) DBSA_INLINE {
+        constexpr int kb = decltype(KB)::value;
+        if constexpr (!decltype(CAREFUL)::value) {
+          prepare(st, KB);
+        } else {
+          if ((partly >> (st % 32)) & 1) mask(st, KB);
+          const float bigger = fmaxf(m, row_max(KB));
+          const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - bigger);
+          m = bigger;
+          l *= alpha;
 #pragma unroll
-      for (int kb = 0; kb < kB; ++kb)
+          for (int ob = 0; ob < kO; ++ob) acc[ob] *= alpha;
+          if constexpr (kb > 0) {  // (the first half's probabilities go by the same maximum)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-      top = half_swap_max(top) * c2;
-      if constexpr (!decltype(CAREFUL)::value) {
-        m = m == -INFINITY ? top : m;
-        again |= top > m + kRoom;
-      } else if (__builtin_amdgcn_ballot_w64(top > m) != 0) {
-        const float bigger = fmaxf(m, top);
-        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - bigger);
-        m = bigger;
-        l *= alpha;
-#pragma unroll
-        for (int ob = 0; ob < kO; ++ob) acc[ob] *= alpha;
-      }
-      const float less = m == -INFINITY ? 0.f : -m;
-      float sum = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < kB; ++kb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c2, less));
-          sum += s[kb][i];
-        }
-        if constexpr (!kF32) {
-#pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
-            union {
-              bf16x8 v;
-              bf16x2 p2[4];
-            } x;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x.p2[e] = __builtin_convertvector(floatx2{s[kb][8 * ch + 2 * e], s[kb][8 * ch + 2 * e + 1]}, bf16x2);
-            pf[kb][ch] = x.v;
+            for (int i = 0; i < 16; ++i) s[0][i] *= alpha;
           }
         }
-      }
-      l += sum;
+        const float less = m == -INFINITY ? 0.f : -m;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[kb][i] = probability(s[kb][i], less);
+          sum += s[kb][i];
+        }
+        l += sum;
+        if constexpr (!decltype(CAREFUL)::value) again |= sum > outgrown;
+      });
+      static_for<kB>([&](auto KB) DBSA_INLINE { pack(KB); });
     };
     // the keys that take_poison kept out of the product
     auto add_poison = [&](int st) DBSA_INLINE {
@@ -552,70 +574,92 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           }
       }
     };
-    // A run of matrix instructions: O += V P of step v_step, then S = K Q of the step behind the last one scored (either may be left out).  Fragments are read from LDS
-    // kDist matrix instructions before the one that takes them, in an order the compiler is not left to change: it would
-    // otherwise read each right before its use and wait for it.
-    auto multiply = [&](auto CAREFUL, auto PV, int v_step, auto QK) DBSA_INLINE {
-      constexpr int nV = decltype(PV)::value ? (kF32 ? 16 * kB * kO : 2 * kB * kO) : 0, nK = decltype(QK)::value ? kC * kB : 0;
+    // A run of matrix instructions: S = K Q for half QK of the step whose K is read next, and O += V P for half PV of the step
+    // whose V is read next (-1: left out).  Fragments are read from LDS kDist matrix instructions before the one that takes
+    // them, in an order the compiler is not left to change: it would otherwise read each right before its use and wait for
+    // it.  Half SM's scores become probabilities on the way, a few vector instructions behind every matrix instruction.
+    auto run = [&](auto QK, auto PV, auto SM) DBSA_INLINE {
+      constexpr int kq = decltype(QK)::value, kv = decltype(PV)::value, ks = decltype(SM)::value;
+      constexpr int nK = kq >= 0 ? kC : 0, nV = kv >= 0 ? (kF32 ? 16 * kO : 2 * kO) : 0, n = nK + nV;
       constexpr int kDist = kF32 ? 4 : 6;
+      // K fragments among the first j: two to each of V, so that scores are ready some instructions before the run ends
+      constexpr auto k_before = [](int j) { return nV == 0 ? j : (2 * j + 2) / 3 < nK ? (2 * j + 2) / 3 : nK; };
       const unsigned vt = read.v, kt = read.k;
       int k_here = k_at, v_here = v_at;  // (a fragment's address is one instruction from these; kept, they are twelve registers)
       asm volatile("" : "+v"(k_here), "+v"(v_here));
-      if constexpr (nV > 0) {
-        if constexpr (decltype(CAREFUL)::value) {
-          if (v_step >= pool_steps && ((partly >> (v_step % 32)) & 1)) add_poison(v_step);
-        }
-        read.next_v();
-      }
-      if constexpr (nK > 0) read.next_k();
-      if constexpr (nV > 0 && decltype(CAREFUL)::value) product_fence();
       if constexpr (nK > 0) {
 #pragma unroll
-        for (int kb = 0; kb < kB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+        for (int i = 0; i < 16; ++i) s[kq][i] = 0.f;
       }
+      const float less = m == -INFINITY ? 0.f : -m;
+      float sum = 0.f, two[2];
+      bf16x2 packed[8];
       Piece ring[kDist];  // (fp32: V fragments are single floats)
       auto read_fragment = [&](auto F) DBSA_INLINE {
-        constexpr int f = decltype(F)::value;
-        if constexpr (f < nV && kF32) {
-          constexpr int ob = f % kO, i = f / kO % 16, kb = f / kO / 16, row = 32 * kb + 8 * (i / 4) + i % 4;
+        constexpr int f = decltype(F)::value, k = k_before(f), v = f - k;
+        if constexpr (k_before(f + 1) > k) {
+          ring[f % kDist] = *(reinterpret_cast<const __attribute__((address_space(3))) Piece*>(static_cast<uintptr_t>(kt + (k_here ^ (32 * k)))) +
+                              32 * kq * C::kRowBytes / 16);
+        } else if constexpr (kF32) {
+          constexpr int ob = v % kO, i = v / kO, row = 32 * kv + 8 * (i / 4) + i % 4;
           const int ch = 32 * ob + l32;
           ring[f % kDist][0] = *reinterpret_cast<lds_float*>(static_cast<uintptr_t>(
               vt + (row + 4 * half) * C::kRowBytes + (((ch / 4) ^ (8 * ((row / 4 + half) % 2))) * 16) + (ch % 4) * 4));
-        } else if constexpr (f < nV) {
-          constexpr int ob = f % kO, ch = f / kO % 2, kb = f / kO / 2;
-          const lds_byte* const at = reinterpret_cast<const lds_byte*>(static_cast<uintptr_t>(vt + (v_here ^ (64 * ob)))) + (32 * kb + 16 * ch) * C::kRowBytes;
+        } else {
+          constexpr int ob = v % kO, ch = v / kO;
+          const lds_byte* const at = reinterpret_cast<const lds_byte*>(static_cast<uintptr_t>(vt + (v_here ^ (64 * ob)))) + (32 * kv + 16 * ch) * C::kRowBytes;
           const bf16x4 lo = lds_read_tr(at), hi = lds_read_tr(at + 8 * C::kRowBytes);
           ring[f % kDist] = __builtin_bit_cast(Piece, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        } else {
-          constexpr int kb = (f - nV) % kB, c = (f - nV) / kB;
-          ring[f % kDist] = *(reinterpret_cast<const __attribute__((address_space(3))) Piece*>(static_cast<uintptr_t>(kt + (k_here ^ (32 * c)))) +
-                              32 * kb * C::kRowBytes / 16);
         }
       };
       __builtin_amdgcn_sched_barrier(0);
-      static_for<(kDist < nV + nK ? kDist : nV + nK)>([&](auto F) DBSA_INLINE { read_fragment(F); });
+      static_for<(kDist < n ? kDist : n)>([&](auto F) DBSA_INLINE { read_fragment(F); });
       __builtin_amdgcn_sched_barrier(0);
-      static_for<nV + nK>([&](auto F) DBSA_INLINE {
-        constexpr int f = decltype(F)::value;
-        if constexpr (f < nV && kF32) {
-          constexpr int ob = f % kO, i = f / kO % 16, kb = f / kO / 16;
-          product_f32(acc[ob], ring[f % kDist][0], s[kb][i]);
-        } else if constexpr (f < nV) {
-          constexpr int ob = f % kO, ch = f / kO % 2, kb = f / kO / 2;
-          product_bf16(acc[ob], __builtin_bit_cast(bf16x8, ring[f % kDist]), pf[kb][ch]);
-        } else if constexpr (kF32) {
-          constexpr int kb = (f - nV) % kB, c = (f - nV) / kB;
+      static_for<n>([&](auto F) DBSA_INLINE {
+        constexpr int f = decltype(F)::value, k = k_before(f), v = f - k;
+        if constexpr (k_before(f + 1) > k) {
+          if constexpr (kF32) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(ring[f % kDist][e], qf[c][e], s[kb], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) s[kq] = __builtin_amdgcn_mfma_f32_32x32x2f32(ring[f % kDist][e], qf[k][e], s[kq], 0, 0, 0);
+          } else {
+            s[kq] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ring[f % kDist]), __builtin_bit_cast(bf16x8, qf[k]), s[kq], 0, 0, 0);
+          }
+        } else if constexpr (kF32) {
+          product_f32(acc[v % kO], ring[f % kDist][0], s[kv][v / kO]);
         } else {
-          constexpr int kb = (f - nV) % kB, c = (f - nV) / kB;
-          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ring[f % kDist]), __builtin_bit_cast(bf16x8, qf[c]), s[kb], 0, 0, 0);
+          product_bf16(acc[v % kO], __builtin_bit_cast(bf16x8, ring[f % kDist]), pf[kv][v / kO]);
         }
-        if constexpr (f + kDist < nV + nK) read_fragment(std::integral_constant<int, f + kDist>{});
+        if constexpr (f + kDist < n) read_fragment(std::integral_constant<int, f + kDist>{});
+        if constexpr (ks >= 0) {
+          // 16 probabilities over n slots; a pair is packed and summed behind the next one (a result of the transcendental unit
+          // cannot be used by the very next instructions)
+          static_for<16 * (f + 1) / n - 16 * f / n>([&](auto J) DBSA_INLINE {
+            constexpr int i = 16 * f / n + decltype(J)::value;
+            if constexpr (i % 2 == 0 && i > 0) {
+              packed[i / 2 - 1] = __builtin_convertvector(floatx2{two[0], two[1]}, bf16x2);
+              sum += two[0] + two[1];
+            }
+            two[i % 2] = probability(s[ks][i], less);
+          });
+        }
         __builtin_amdgcn_sched_barrier(0);
       });
+      if constexpr (ks >= 0) {
+        packed[7] = __builtin_convertvector(floatx2{two[0], two[1]}, bf16x2);
+        sum += two[0] + two[1];
+        l += sum;
+        again |= sum > outgrown;
+#pragma unroll
+        for (int ch = 0; ch < 2; ++ch) {
+          union {
+            bf16x8 v;
+            bf16x2 p2[4];
+          } x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x.p2[e] = packed[4 * ch + e];
+          pf[ks][ch] = x.v;
+        }
+      }
     };
 
     // What happens to step n while step n - 1 is still being read.  (A wave's own ring place is free again once it has read it.)
@@ -625,8 +669,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     };
-    constexpr std::true_type kYes{};
-    constexpr std::false_type kNo{};
+    constexpr std::integral_constant<int, -1> kNone{};
+    constexpr std::integral_constant<int, 0> k0{};
+    constexpr std::integral_constant<int, kB - 1> k1{};  // the second half of a step, where it has one
     // All steps of the record.  The quick walk never touches the accumulators but in the product (a block that sometimes
     // scales them costs a copy of all of them in every step): a row's reference maximum is that of the first step in which it
     // sees a key, and later scores may exceed it by kRoom, where probabilities, their sums and the accumulators are still far
@@ -643,21 +688,61 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       partly = 0;
       next = fetch(0);
     };
+    // Step n is put, and the one kFlight behind it requested.  One barrier per step: behind it, step n has landed for all
+    // waves, and all have read what they read before it, whose stages the step requested now takes (8 bits: whose stages the
+    // step put before the next barrier takes).
+    auto advance = [&](int n) DBSA_INLINE {
+      if (n >= 0) {
+        wait_for(n, std::integral_constant<int, C::kFlight - 1>{});
+        put(n);
+        barrier();
+      }
+      if (n + C::kFlight < steps) request(n + C::kFlight);
+    };
     auto walk = [&]() DBSA_INLINE {
       begin_walk();
-      // One barrier per step: behind it, step st has landed for all waves, and all have read step st - 1, whose stage
-      // the step requested now takes (8 bits: whose stage the step put before the next barrier takes).
-      for (int st = -C::kFlight; st < steps; ++st) {
-        if (st >= 0) {
-          wait_for(st, std::integral_constant<int, C::kFlight - 1>{});
-          put(st);
-          barrier();
+      if constexpr (C::kPipelined) {
+        // Half steps of 32 keys in three stages, one apart: while the probabilities of a half are made, the scores of the next
+        // half and the product of the one before it run on the matrix pipe; no instruction waits for one of its own half.
+        // (One barrier per step keeps the two waves of a SIMD side by side, so that each has to mix its matrix and vector
+        // instructions itself: with the two kinds one after the other a step of eight waves took 2.2 us, so 1.4.)
+        for (int n = -C::kFlight; n <= 0; ++n) advance(n);
+        run(k0, kNone, kNone);
+        prepare(0, k0);
+        run(k1, kNone, k0);
+        read.next_k();
+        for (int st = 0; st < steps - 1; ++st) {
+          advance(st + 1);
+          prepare(st, k1);
+          run(k0, k0, k1);
+          prepare(st + 1, k0);
+          run(k1, k1, k0);
+          read.next_k();
+          read.next_v();
         }
-        if (st + C::kFlight < steps) request(st + C::kFlight);
-        if (st < 0) continue;
-        multiply(kNo, kNo, 0, kYes);
-        softmax(kNo, st);
-        multiply(kNo, kYes, st, kNo);
+        prepare(steps - 1, k1);
+        run(kNone, k0, k1);
+        run(kNone, k1, kNone);
+        read.next_v();
+      } else {
+        for (int st = -C::kFlight; st < steps; ++st) {
+          advance(st);
+          if (st < 0) continue;
+          run(k0, kNone, kNone);
+          softmax(std::false_type{}, st);
+          run(kNone, k0, kNone);
+          read.next_k();
+          read.next_v();
+        }
+      }
+    };
+    // a wave without rows brings its pieces
+    auto walk_idle = [&]() DBSA_INLINE {
+      begin_walk();
+      for (int n = -C::kFlight; n < steps; ++n) advance(n);
+      for (int n = 0; n < steps; ++n) {
+        read.next_k();
+        read.next_v();
       }
     };
     // step by step, nothing ahead
@@ -668,14 +753,20 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         wait_vmcnt<0>();
         put(st);
         barrier();
-        multiply(kYes, kNo, 0, kYes);
-        softmax(kYes, st);
-        multiply(kYes, kYes, st, kNo);
+        static_for<kB>([&](auto KB) DBSA_INLINE { run(KB, kNone, kNone); });
+        softmax(std::true_type{}, st);
+        if (st >= pool_steps && ((partly >> (st % 32)) & 1)) add_poison(st);
+        product_fence();
+        static_for<kB>([&](auto KB) DBSA_INLINE { run(kNone, KB, kNone); });
+        product_fence();
+        read.next_k();
+        read.next_v();
         barrier();
       }
     };
     if (steps > 0) {
-      walk();
+      if (kNW == 1 || wave * 32 < n_tok * r) walk();
+      else walk_idle();
       // (behind this barrier every wave is done with the stages: the next walk's first steps may land)
       uint32_t* const votes = reinterpret_cast<uint32_t*>(smem + C::kVotesAt);
       const bool any = __builtin_amdgcn_ballot_w64(again) != 0;
