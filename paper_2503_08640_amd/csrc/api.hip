@@ -180,14 +180,14 @@ hipError_t upload_lists(dbsa_layout* L, hipStream_t stream) {
                b_mqs = L->mx_qshift.size() * sizeof(int32_t), b_msp = L->mx_slot_ptr.size() * sizeof(int64_t),
                b_crec = L->ck_rec.size() * sizeof(int32_t), b_cptr = L->ck_ptr.size() * sizeof(int32_t),
                b_ctok = L->ck_toks.size() * sizeof(int32_t), b_cent = L->ck_ent.size() * sizeof(int32_t),
-               b_ctp = L->ck_tok_ptr.size() * sizeof(int32_t), b_ctq = L->ck_tok_part.size() * sizeof(int32_t);
+               b_cmg = L->ck_merge.size() * sizeof(int32_t), b_ctq = L->ck_tok_part.size() * sizeof(int32_t);
   const size_t o_tab = 0, o_ptr = o_tab + pad(b_tab), o_ent = o_ptr + pad(b_ptr), o_ord = o_ent + pad(b_ent),
                o_dec = o_ord + pad(b_ord), o_spl = o_dec + pad(b_dec), o_gsp = o_spl + pad(b_spl),
                o_lsh = o_gsp + pad(b_gsp), o_gir = o_lsh + pad(b_lsh), o_grp = o_gir + pad(b_gir),
                o_grw = o_grp + pad(b_grp), o_gse = o_grw + pad(b_grw), o_gqr = o_gse + pad(b_gse),
                o_dsh = o_gqr + pad(b_gqr), o_gqs = o_dsh + pad(b_dsh), o_mqr = o_gqs + pad(b_gqs), o_mqs = o_mqr + pad(b_mqr), o_msp = o_mqs + pad(b_mqs),
                o_crec = o_msp + pad(b_msp), o_cptr = o_crec + pad(b_crec), o_ctok = o_cptr + pad(b_cptr),
-               o_cent = o_ctok + pad(b_ctok), o_ctp = o_cent + pad(b_cent), o_ctq = o_ctp + pad(b_ctp),
+               o_cent = o_ctok + pad(b_ctok), o_cmg = o_cent + pad(b_cent), o_ctq = o_cmg + pad(b_cmg),
                o_cut = o_ctq + pad(b_ctq), o_srec = o_cut + pad(cut_room_bytes(L)), o_sptr = o_srec + pad(b_srec),
                o_mrec = o_sptr + pad(b_sptr), o_mptr = o_mrec + pad(b_mrec), total = o_mptr + pad(b_sptr) + 256;
   ListBlock blk{};
@@ -219,7 +219,7 @@ hipError_t upload_lists(dbsa_layout* L, hipStream_t stream) {
   put(o_cptr, L->ck_ptr.data(), b_cptr);
   put(o_ctok, L->ck_toks.data(), b_ctok);
   put(o_cent, L->ck_ent.data(), b_cent);
-  put(o_ctp, L->ck_tok_ptr.data(), b_ctp);
+  put(o_cmg, L->ck_merge.data(), b_cmg);
   put(o_ctq, L->ck_tok_part.data(), b_ctq);
   L->dev.cut_room = static_cast<unsigned char*>(blk.dev) + o_cut;
   // the staging twin stays with the block, so nothing has to wait for the copy here; calls on
@@ -268,7 +268,7 @@ hipError_t upload_lists(dbsa_layout* L, hipStream_t stream) {
   L->dev.ck_ptr = reinterpret_cast<int32_t*>(b + o_cptr);
   L->dev.ck_toks = reinterpret_cast<int32_t*>(b + o_ctok);
   L->dev.ck_ent = reinterpret_cast<int32_t*>(b + o_cent);
-  L->dev.ck_tok_ptr = reinterpret_cast<int32_t*>(b + o_ctp);
+  L->dev.ck_merge = reinterpret_cast<int32_t*>(b + o_cmg);
   L->dev.ck_tok_part = reinterpret_cast<int32_t*>(b + o_ctq);
   L->dev.sched_rec = reinterpret_cast<int32_t*>(b + o_srec);
   L->dev.sched_ptr = reinterpret_cast<int32_t*>(b + o_sptr);
@@ -1195,7 +1195,7 @@ int chunk_common(const dbsa_layout* L, dbsa_tensor q, dbsa_tensor k_pool, dbsa_t
   ChunkParams p{};
   p.page_log2 = __builtin_ctz(static_cast<unsigned>(own->page_tokens));
   p.own_capacity = static_cast<int32_t>(std::min<int64_t>(int64_t{own->table_stride} * own->page_tokens, INT32_MAX - 2 * kChunkTile));
-  p.merge = L->ck_part_rows > 0 ? 1 : 0;
+  p.n_merge = static_cast<int32_t>(L->ck_merge.size() / 3);
   const int64_t widest = std::max(std::max(k_pool.stride_tok, v_pool.stride_tok), std::max(own->k.stride_tok, own->v.stride_tok));
   p.narrow = widest < (int64_t{1} << 22) ? 1 : 0;  // (64 rows of at most 4 bytes an element: 2^30)
   const size_t need = static_cast<size_t>(L->ck_part_rows) * n_q_heads * (head_dim + kPartialPad) * sizeof(float);
@@ -1206,7 +1206,7 @@ int chunk_common(const dbsa_layout* L, dbsa_tensor q, dbsa_tensor k_pool, dbsa_t
   p.ptr = L->dev.ck_ptr;
   p.toks = L->dev.ck_toks;
   p.ent = L->dev.ck_ent;
-  p.tok_ptr = L->dev.ck_tok_ptr;
+  p.merge = L->dev.ck_merge;
   p.tok_part = L->dev.ck_tok_part;
   p.q = view(q);
   p.o = view(o);

@@ -638,8 +638,10 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
             if constexpr (i % 2 == 0 && i > 0) {
               packed[i / 2 - 1] = __builtin_convertvector(floatx2{two[0], two[1]}, bf16x2);
               sum += two[0] + two[1];
+              asm volatile("" : "+v"(packed[i / 2 - 1]), "+v"(sum));  // (else it sinks behind the run)
             }
             two[i % 2] = probability(s[ks][i], less);
+            asm volatile("" : "+v"(two[i % 2]));
           });
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -820,49 +822,67 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
   }
 }
 
-// Joins the partial states of one (token, query head): m* = max m_s, o = sum acc_s 2^(m_s - m*) / sum l_s 2^(m_s - m*).  One wave
-// each, kD / 64 channels per lane; maxima and sums are read with one state per lane.
+// Joins the partial states of one (token, query head): m* = max m_s, o = sum acc_s 2^(m_s - m*) / sum l_s 2^(m_s - m*).  Memory
+// bound, and for few tokens bound by its chain of loads (the token, its states, their maxima, their rows): sixteen lanes take a
+// pair, kD / 16 channels each, the maxima and sums are read with one state per lane, and four rows are in flight.
 template <typename Q, int kD>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
-  constexpr int kRow = kD + kPartialPad, kPer = kD / 64;
-  const int lane = threadIdx.x % 64;
-  const int64_t pair = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
-  if (pair >= static_cast<int64_t>(p.n_rows) * p.n_q_heads) return;
-  const int tok = static_cast<int>(pair / p.n_q_heads), head = static_cast<int>(pair % p.n_q_heads);
-  const int lo = p.tok_ptr[tok], n = p.tok_ptr[tok + 1] - lo;
-  if (n == 0) return;  // finished by its record
-  const float v_scale = p.v_scale ? p.v_scale[head / (p.n_q_heads / p.n_kv_heads)] : 1.f;
+  constexpr int kRow = kD + kPartialPad, kPer = kD / 16, kTeam = 16;
+  const int in = threadIdx.x % kTeam;
+  const int64_t pair = static_cast<int64_t>(blockIdx.x) * (256 / kTeam) + threadIdx.x / kTeam;
+  if (pair >= static_cast<int64_t>(p.n_merge) * p.n_q_heads) return;  // (whole teams, which exchange among themselves alone)
+  const int at = static_cast<int>(pair / p.n_q_heads), head = static_cast<int>(pair % p.n_q_heads);
+  const int tok = p.merge[3 * static_cast<int64_t>(at)], n = p.merge[3 * static_cast<int64_t>(at) + 2];
+  const int32_t* const parts = p.tok_part + p.merge[3 * static_cast<int64_t>(at) + 1];
   const float* const base = p.partial + static_cast<int64_t>(head) * kRow;
   const int64_t stride = static_cast<int64_t>(p.n_q_heads) * kRow;
   float m = -INFINITY;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, base[p.tok_part[lo + i] * stride + kD]);
+  for (int i = in; i < n; i += kTeam) m = fmaxf(m, base[parts[i] * stride + kD]);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  float sum = 0.f, acc[kPer] = {};
-  for (int at = 0; at < n; at += 64) {
-    int part = 0;
+  for (int o = kTeam / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kTeam));
+  float sum = 0.f;
+  floatx4 acc[kPer / 4] = {};
+  for (int first = 0; first < n; first += kTeam) {
+    const int part = parts[min(first + in, n - 1)];  // (behind the last: the last again, with nothing as its weight)
     float weight = 0.f;
-    if (at + lane < n) {
-      part = p.tok_part[lo + at + lane];
-      const float ms = base[part * stride + kD], ls = base[part * stride + kD + 1];
-      weight = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - m);
-      sum = fmaf(ls, weight, sum);
+    if (first + in < n) {
+      const floatx2 ml = *reinterpret_cast<const floatx2*>(base + part * stride + kD);
+      weight = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m);
+      sum = fmaf(ml[1], weight, sum);
     }
-    const int here = min(64, n - at);
-    for (int i = 0; i < here; ++i) {
-      const float* const row = base + __shfl(part, i) * stride + lane * kPer;
-      const float wi = __shfl(weight, i);
+    const int here = min(kTeam, n - first);
+    for (int i = 0; i < here; i += 4) {
+      floatx4 x[4][kPer / 4];
+      float w[4];
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[e] = fmaf(row[e], wi, acc[e]);
+      for (int j = 0; j < 4; ++j) {
+        const int from = min(i + j, here - 1);
+        const float* const row = base + __shfl(part, from, kTeam) * stride + in * kPer;
+        w[j] = i + j < here ? __shfl(weight, from, kTeam) : 0.f;
+#pragma unroll
+        for (int e = 0; e < kPer / 4; ++e) x[j][e] = *reinterpret_cast<const floatx4*>(row + 4 * e);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + j < here) {  // (a state's rows may hold what is not finite)
+#pragma unroll
+          for (int e = 0; e < kPer / 4; ++e)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) acc[e][f] = fmaf(x[j][e][f], w[j], acc[e][f]);
+        }
     }
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  for (int o = kTeam / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kTeam);
+  const float v_scale = p.v_scale ? p.v_scale[head / (p.n_q_heads / p.n_kv_heads)] : 1.f;
   const float inv = sum > 0.f || sum != sum ? v_scale / sum : 0.f;
-  Q* const out = static_cast<Q*>(const_cast<void*>(p.o.ptr)) + tok * p.o.stride_tok + head * p.o.stride_head + lane * kPer;
+  Q* const out = static_cast<Q*>(const_cast<void*>(p.o.ptr)) + tok * p.o.stride_tok + head * p.o.stride_head + in * kPer;
+  typedef Q four __attribute__((ext_vector_type(4)));
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) out[e] = static_cast<Q>(acc[e] * inv);
-  if (p.lse && lane == 0) p.lse[static_cast<int64_t>(head) * p.n_rows + tok] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  for (int e = 0; e < kPer / 4; ++e)
+    *reinterpret_cast<four*>(out + 4 * e) = four{static_cast<Q>(acc[e][0] * inv), static_cast<Q>(acc[e][1] * inv),
+                                                 static_cast<Q>(acc[e][2] * inv), static_cast<Q>(acc[e][3] * inv)};
+  if (p.lse && in == 0) p.lse[static_cast<int64_t>(head) * p.n_rows + tok] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 template <typename T, int kD, int kNW, int kBN>
@@ -887,9 +907,9 @@ hipError_t launch_kind(const ChunkParams& p, hipStream_t stream) {
   else if (p.rows == 64) e = launch_shape<T, kD, 2, 32>(p, stream);
   else if (p.rows == 128) e = launch_shape<T, kD, 4, 32>(p, stream);
   else if (p.rows == 256) e = launch_shape<T, kD, 8, kWide>(p, stream);
-  if (e != hipSuccess || !p.merge) return e;
-  const int64_t pairs = static_cast<int64_t>(p.n_rows) * p.n_q_heads;
-  chunk_merge_kernel<typename Kind<T>::Q, kD><<<dim3(static_cast<unsigned>((pairs + 3) / 4)), dim3(256), 0, stream>>>(p);
+  if (e != hipSuccess || p.n_merge == 0) return e;
+  const int64_t pairs = static_cast<int64_t>(p.n_merge) * p.n_q_heads;
+  chunk_merge_kernel<typename Kind<T>::Q, kD><<<dim3(static_cast<unsigned>((pairs + 15) / 16)), dim3(256), 0, stream>>>(p);
   return hipGetLastError();
 }
 

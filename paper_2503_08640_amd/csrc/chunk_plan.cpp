@@ -26,8 +26,8 @@ struct Unit {
 
 // What starting and finishing a record costs, in tiles: its rows of Q, the first tiles' latency, the partial states.
 constexpr int64_t kRecordCost = 3;
-// fewest tiles a worker's share is cut to, and fewest tiles of a piece
-constexpr int64_t kChunkShare = 4, kChunkPiece = 3;
+// tiles of a unit that is not worth cutting
+constexpr int64_t kShortUnit = 3;
 
 }  // namespace
 
@@ -99,13 +99,9 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
     weight += tiles;
   }
   const int32_t typical = weight > 0.0 ? static_cast<int32_t>(wanted / weight + 0.999) : std::min(kMostRows, new_tokens(0) * r);
-  const ChunkShape shape = dbsa_chunk_shape(std::max(typical, r));
-  const int32_t per_block = shape.rows / r;  // tokens of a unit
-  L->ck_rows = shape.rows;
-
   // ---- units ----
   std::vector<Unit> units;
-  L->ck_ent = lists.gm_seg_ent;
+  int32_t per_block = 1;  // tokens of a unit
   auto own_tiles = [&](int32_t u, int32_t tokens_before_end) {
     const int64_t n = own_tokens ? std::max(own_tokens[u], new_tokens(u)) : new_tokens(u);
     const int64_t last = std::max<int64_t>(1, n - tokens_before_end);
@@ -123,69 +119,86 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
   };
   std::vector<char> alone(B, 0);
   std::vector<int32_t> toks;
-  for (int32_t u = 0; u < B; ++u) {
-    alone[u] = new_tokens(u) >= per_block || B == 1;
-    if (!alone[u]) continue;
-    const int32_t at = static_cast<int32_t>(L->ck_ent.size() / 2), n = static_cast<int32_t>(lists.dec_ptr[u + 1] - lists.dec_ptr[u]);
-    L->ck_ent.insert(L->ck_ent.end(), lists.dec_ent.begin() + 2 * lists.dec_ptr[u], lists.dec_ent.begin() + 2 * lists.dec_ptr[u + 1]);
-    toks.clear();
+  auto tokens_of = [&](int32_t u) {
     for (int32_t t = sel->cu_qlens[u]; t < sel->cu_qlens[u + 1]; ++t) toks.push_back(t);
-    add_blocks(toks, [&](Unit& x, int32_t behind) {
-      x.ent_begin = at;
-      x.n_ent = n;
-      x.own_u = u;
-      x.own_tiles = own_tiles(u, behind);
-    });
+  };
+  auto make_units = [&](int32_t rows) {
+    per_block = rows / r;
+    units.clear();
+    L->ck_toks.clear();
+    L->ck_ent = lists.gm_seg_ent;
+    for (int32_t u = 0; u < B; ++u) {
+      alone[u] = new_tokens(u) >= per_block || B == 1;
+      if (!alone[u]) continue;
+      const int32_t at = static_cast<int32_t>(L->ck_ent.size() / 2), n = static_cast<int32_t>(lists.dec_ptr[u + 1] - lists.dec_ptr[u]);
+      L->ck_ent.insert(L->ck_ent.end(), lists.dec_ent.begin() + 2 * lists.dec_ptr[u], lists.dec_ent.begin() + 2 * lists.dec_ptr[u + 1]);
+      toks.clear();
+      tokens_of(u);
+      add_blocks(toks, [&](Unit& x, int32_t behind) {
+        x.ent_begin = at;
+        x.n_ent = n;
+        x.own_u = u;
+        x.own_tiles = own_tiles(u, behind);
+      });
+    }
+    for (int32_t s = 0; s < n_seg; ++s) {
+      toks.clear();
+      for (int32_t u : users[s])
+        if (!alone[u]) tokens_of(u);
+      if (toks.empty() || seg_tiles(s) == 0) continue;
+      add_blocks(toks, [&](Unit& x, int32_t) {
+        x.ent_begin = static_cast<int32_t>(lists.gm_seg_ptr[s]);
+        x.n_ent = static_cast<int32_t>(seg_tiles(s));
+      });
+    }
+    for (int32_t u = 0; u < B; ++u) {
+      if (alone[u]) continue;
+      toks.clear();
+      tokens_of(u);
+      add_blocks(toks, [&](Unit& x, int32_t behind) {
+        x.own_u = u;
+        x.own_tiles = own_tiles(u, behind);
+      });
+    }
+    int64_t tiles = 0;
+    for (const Unit& x : units) tiles += x.cost();
+    return tiles;
+  };
+  // Fewer tiles than there are compute units for them: smaller blocks bring in more of those (three questions in fp32, 99
+  // tokens and 60 tiles of 256 rows: 66 us, in blocks of 128 rows 51).
+  const int64_t units_of_head = std::max<int64_t>(1, L->compute_units / n_kv_heads);
+  ChunkShape shape = dbsa_chunk_shape(std::max(typical, r));
+  int64_t tiles = make_units(shape.rows);
+  while (shape.rows > 32 && tiles < units_of_head) {
+    shape = dbsa_chunk_shape(shape.rows / 2);
+    tiles = make_units(shape.rows);
   }
-  for (int32_t s = 0; s < n_seg; ++s) {
-    toks.clear();
-    for (int32_t u : users[s])
-      if (!alone[u])
-        for (int32_t t = sel->cu_qlens[u]; t < sel->cu_qlens[u + 1]; ++t) toks.push_back(t);
-    if (toks.empty() || seg_tiles(s) == 0) continue;
-    add_blocks(toks, [&](Unit& x, int32_t) {
-      x.ent_begin = static_cast<int32_t>(lists.gm_seg_ptr[s]);
-      x.n_ent = static_cast<int32_t>(seg_tiles(s));
-    });
-  }
-  for (int32_t u = 0; u < B; ++u) {
-    if (alone[u]) continue;
-    toks.clear();
-    for (int32_t t = sel->cu_qlens[u]; t < sel->cu_qlens[u + 1]; ++t) toks.push_back(t);
-    add_blocks(toks, [&](Unit& x, int32_t behind) {
-      x.own_u = u;
-      x.own_tiles = own_tiles(u, behind);
-    });
-  }
+  L->ck_rows = shape.rows;
 
   // ---- dealing ----
   int64_t total = 0;
   for (const Unit& x : units) total += x.cost() + kRecordCost;
   const int64_t places = std::max<int64_t>(1, int64_t{L->compute_units} * shape.per_cu / n_kv_heads);
-  const int64_t workers = std::max<int64_t>(1, std::min(places, (total + kChunkShare + kRecordCost - 1) / (kChunkShare + kRecordCost)));
+  const int64_t workers = std::max<int64_t>(1, std::min(places, tiles));
   // one dealing at a share: records (unit, first tile, tiles) worker by worker; true if every tile found a worker
   struct Record {
     int32_t unit, lo, n;
   };
   std::vector<Record> recs;
   std::vector<int32_t> ptr;
-  auto deal = [&](int64_t share) {
+  auto deal = [&](int64_t share, bool whole) {
     recs.clear();
     ptr.assign(1, 0);
     int64_t room = share;
-    auto next_worker = [&] {
-      ptr.push_back(static_cast<int32_t>(recs.size()));
-      room = share;
-      return static_cast<int64_t>(ptr.size()) <= workers;
-    };
     for (size_t i = 0; i < units.size(); ++i) {
       const int64_t all = units[i].cost();
       for (int64_t lo = 0; lo < all;) {
-        int64_t n = std::min(all - lo, room - kRecordCost);
-        // (no piece shorter than kChunkPiece on either side of a cut)
-        if (n < all - lo && all - lo - n < kChunkPiece) n = all - lo - kChunkPiece;
-        if (n < std::min(all - lo, kChunkPiece)) {
-          if (!next_worker()) return false;
+        const int64_t n = std::min(all - lo, room - kRecordCost);
+        if (n < (whole ? all : 1)) {
+          if (room == share) return false;
+          ptr.push_back(static_cast<int32_t>(recs.size()));
+          room = share;
+          if (static_cast<int64_t>(ptr.size()) > workers) return false;
           continue;
         }
         recs.push_back({static_cast<int32_t>(i), static_cast<int32_t>(lo), static_cast<int32_t>(n)});
@@ -196,9 +209,12 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
     ptr.push_back(static_cast<int32_t>(recs.size()));
     return true;
   };
-  // (a share has to hold the smallest piece and what is left when a cut is moved to keep the rest long enough)
-  int64_t share = std::max<int64_t>(total / workers, 2 * kChunkPiece + kRecordCost);
-  while (!deal(share)) share += std::max<int64_t>(1, share / 64);
+  // Units stay whole where that costs no worker more than a sixteenth above its share: a cut costs two partial states and the
+  // merge of them (2048 tokens behind 90k, 32 units of nearly equal length: 1960 us cut into equal shares, 1830 whole).
+  // And where they are so short that the merge's launch (4 us) would cost more than their few tiles one behind the other (1.3 us each).
+  const int64_t fair = std::max<int64_t>((total + workers - 1) / workers, 1 + kRecordCost);
+  if (!deal(std::max(fair + fair / 16, kShortUnit + kRecordCost), true))
+    for (int64_t share = fair; !deal(share, false);) share += std::max<int64_t>(1, share / 64);
 
   // ---- records, and where each token's partial states lie ----
   std::vector<int32_t> pieces(units.size(), 0);
@@ -233,6 +249,7 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
   L->ck_tok_ptr.assign(1, 0);
   for (int32_t t = 0; t < L->n_query_tokens; ++t) {
     L->ck_tok_part.insert(L->ck_tok_part.end(), parts[t].begin(), parts[t].end());
+    if (!parts[t].empty()) L->ck_merge.insert(L->ck_merge.end(), {t, L->ck_tok_ptr.back(), static_cast<int32_t>(parts[t].size())});
     L->ck_tok_ptr.push_back(static_cast<int32_t>(L->ck_tok_part.size()));
   }
   return DBSA_OK;

@@ -125,7 +125,7 @@ hipError_t launch_decode_plain(const AttnParams& p, int head_dim, bool bf16_stor
 
 // Chunk attention (chunk_attn.hip) over the plan of a chunk layout (layout.hpp: ck_*).
 struct ChunkParams {
-  const int32_t *rec, *ptr, *toks, *ent, *tok_ptr, *tok_part;  // device
+  const int32_t *rec, *ptr, *toks, *ent, *merge, *tok_part;  // device
   TensorView q, o;            // [new tokens, Hq, D]
   TensorView k_pool, v_pool;  // [rows, Hkv, D]
   TensorView k_own, v_own;    // a page: [page tokens, Hkv, D]; pages stride_page elements apart
@@ -139,7 +139,7 @@ struct ChunkParams {
   float* partial;             // [partial row][Hq][D + kPartialPad]
   int32_t n_rows;             // new tokens
   int32_t n_q_heads, n_kv_heads, n_workers, rows;
-  int32_t merge;              // 1: some records leave partial states
+  int32_t n_merge;            // tokens some records leave partial states of
   int32_t narrow;             // 1: 64 rows of every cache lie within 32 bits of bytes
   float scale_log2e;
 };

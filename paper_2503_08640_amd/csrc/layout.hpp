@@ -61,7 +61,7 @@ struct dbsa_device_lists {
   int32_t* ck_ptr = nullptr;      // [ck_workers + 1]
   int32_t* ck_toks = nullptr;
   int32_t* ck_ent = nullptr;      // [n_ent][2]
-  int32_t* ck_tok_ptr = nullptr;  // [n_query_tokens + 1]
+  int32_t* ck_merge = nullptr;    // [n][3]
   int32_t* ck_tok_part = nullptr;
   // ordering of the asynchronous upload against the calls that read the lists (HIP handles kept
   // as plain pointers so that host-only code can include this header)
@@ -149,10 +149,11 @@ struct dbsa_layout {
   //   4 question whose own keys follow (-1: none), 5 / 6 first tile of them and the one behind the last, out of 7 expected
   //   tiles (the device scales them to the tiles there are), 8 first partial row (-1: the record finishes its rows),
   //   9 / 10 first new token and new tokens of that question
-  // Partial row p + i of a record is its token i's.  Token t's partial rows: ck_tok_part[ck_tok_ptr[t] ..].
+  // Partial row p + i of a record is its token i's.  Token t's partial rows: ck_tok_part[ck_tok_ptr[t] ..]; ck_merge lists
+  // the tokens that have any: token, first place in ck_tok_part, partial rows.
   int32_t ck_q_heads = 0, ck_kv_heads = 0, ck_rows = 0, ck_workers = 0;
   int64_t ck_part_rows = 0;
-  std::vector<int32_t> ck_rec, ck_ptr, ck_toks, ck_ent, ck_tok_ptr, ck_tok_part;
+  std::vector<int32_t> ck_rec, ck_ptr, ck_toks, ck_ent, ck_tok_ptr, ck_tok_part, ck_merge;
 
   // Schedule of a persistent prefill-shaped launch for n_classes workers (dbsa_balance_schedule),
   // computed by the first call that needs one and kept: class c walks records
