@@ -604,34 +604,40 @@ def dbsa_decode_attn_kv8(layout: Layout, q_step, k_cache, v_cache, self_len, k_p
 # chunks of new tokens over paged caches, 8-bit caches
 # ---------------------------------------------------------------------------
 
-def _here(*tensors) -> None:
-    """These calls launch on the current device's current stream: every tensor has to be on that device."""
-    device = _stream_calls()[0]()
+def _here(*tensors) -> int:
+    """Handle of the current stream, where these calls launch: every tensor has to be on its device.  (One question after the
+    device per call, and the device of a tensor as a number: the append of 16 tokens, which the host bounds, 12.3 -> 10.6 us.)"""
+    device, raw, stream = _stream_calls()
+    here = device()
     for t in tensors:
-        assert t is None or t.device.index == device, "expected tensors on the current device"
+        assert t is None or t.get_device() == here, "expected tensors on the current device"
+    return stream().cuda_stream if raw is None else raw(here)
 
 
-def _pages(k_pages, v_pages, page_table):
-    """[pages, page tokens, heads, D] device tensors and an int32 [B, pages of a question] table."""
-    s = k_pages.stride()
-    assert k_pages.dim() == 4 and s[3] == 1 and v_pages.stride() == s and v_pages.shape == k_pages.shape
-    assert page_table.dim() == 2 and page_table.element_size() == 4 and not page_table.is_floating_point()
-    assert page_table.is_contiguous(), "expected a contiguous page table"
-    return Pages(_cache(k_pages), _cache(v_pages), s[0], page_table.data_ptr(), page_table.shape[1], k_pages.shape[1],
-                 k_pages.shape[0])
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
-def _chunk_args(layout: Layout, q, k_pages, page_table, self_len, k_pool, out, lse, workspace):
+def _int32(t) -> bool:
+    return t.element_size() == 4 and not t.is_floating_point() and t.is_contiguous()
+
+
+def _chunk_args(layout: Layout, q, k_pool, v_pool, k_pages, v_pages, page_table, self_len, out, lse, workspace, *scales):
+    """(result, its lse, pages, workspace's pointer and bytes, stream): the arguments both chunk calls share, checked.  k_pages,
+    v_pages: [pages, page tokens, heads, D], page_table int32 [B, pages of a question]."""
     import torch
-    assert self_len.element_size() == 4 and not self_len.is_floating_point() and self_len.is_contiguous()
-    assert self_len.shape[0] == page_table.shape[0] and k_pool.shape[1:] == k_pages.shape[2:]
+    s, shape, ask = k_pages.stride(), k_pages.shape, page_table.shape
+    assert len(shape) == 4 and s[3] == 1 and v_pages.stride() == s and v_pages.shape == shape
+    assert len(ask) == 2 and _int32(page_table), "expected a contiguous int32 page table"
+    assert _int32(self_len) and self_len.shape == ask[:1] and k_pool.shape[1:] == shape[2:] and v_pool.shape == k_pool.shape
     o = torch.empty_like(q) if out is None else out
     assert o.shape == q.shape and o.dtype == q.dtype
     assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous())
-    _here(q, k_pages, page_table, self_len, k_pool, o, lse)
     ws, ws_ptr, ws_bytes = _workspace(layout, q, workspace)
-    _here(ws)
-    return o, ws, ws_ptr, ws_bytes
+    stream = _here(q, k_pool, v_pool, k_pages, v_pages, page_table, self_len, o, lse, ws, *scales)
+    pages = Pages(Tensor(k_pages.data_ptr(), s[1], s[2]), Tensor(v_pages.data_ptr(), s[1], s[2]), s[0], page_table.data_ptr(),
+                  ask[1], shape[1], shape[0])
+    return o, ws, C.byref(pages), ws_ptr, ws_bytes, stream
 
 
 def dbsa_chunk_attn(layout: Layout, q, k_pool, v_pool, k_pages, v_pages, page_table, self_len, scale: float, out=None, lse=None,
@@ -639,13 +645,11 @@ def dbsa_chunk_attn(layout: Layout, q, k_pool, v_pool, k_pages, v_pages, page_ta
     """Stage 2 for the new tokens q [sum T, Hq, D] of every question: pool part as the layout lists it, own keys (older ones
     and the new tokens', self_len int32 [B] on the device) in pages k_pages / v_pages [pages, page tokens, Hkv, D] by page_table
     int32 [B, pages of a question].  Returns O [sum T, Hq, D]."""
-    o, ws, ws_ptr, ws_bytes = _chunk_args(layout, q, k_pages, page_table, self_len, k_pool, out, lse, workspace)
+    o, ws, pages, ws_ptr, ws_bytes, stream = _chunk_args(layout, q, k_pool, v_pool, k_pages, v_pages, page_table, self_len, out, lse,
+                                                         workspace)
     assert q.dtype == k_pool.dtype == v_pool.dtype == k_pages.dtype == v_pages.dtype
-    pages = _pages(k_pages, v_pages, page_table)
-    rc = lib().dbsa_chunk_attn(layout.handle, _tensor(q), _tensor(k_pool), _tensor(v_pool), C.byref(pages),
-                               C.c_void_p(self_len.data_ptr()), _tensor(o), C.c_void_p(lse.data_ptr() if lse is not None else None),
-                               _dtype_code(q), q.shape[1], k_pool.shape[1], q.shape[2], float(scale), ws_ptr, ws_bytes,
-                               C.c_void_p(_stream()))
+    rc = lib().dbsa_chunk_attn(layout.handle, _tensor(q), _tensor(k_pool), _tensor(v_pool), pages, self_len.data_ptr(), _tensor(o),
+                               _at(lse), _dtype_code(q), q.shape[1], k_pool.shape[1], q.shape[2], float(scale), ws_ptr, ws_bytes, stream)
     _check(rc, "dbsa_chunk_attn")
     return o
 
@@ -655,14 +659,13 @@ def dbsa_chunk_attn_kv8(layout: Layout, q, k_pool8, v_pool8, k_pages8, v_pages8,
     """dbsa_chunk_attn over an 8-bit pool and 8-bit pages (float8_e4m3fn or uint8 tensors) with float32 scales [Hkv] on the
     device, as dbsa_kv8_write leaves them; q and the result are bf16."""
     import torch
-    o, ws, ws_ptr, ws_bytes = _chunk_args(layout, q, k_pages8, page_table, self_len, k_pool8, out, lse, workspace)
+    o, ws, pages, ws_ptr, ws_bytes, stream = _chunk_args(layout, q, k_pool8, v_pool8, k_pages8, v_pages8, page_table, self_len, out,
+                                                         lse, workspace, k_scale, v_scale)
     assert q.dtype == torch.bfloat16 and all(t.element_size() == 1 for t in (k_pool8, v_pool8, k_pages8, v_pages8))
     _scales(k_scale, v_scale, k_pool8.shape[1])
-    pages = _pages(k_pages8, v_pages8, page_table)
-    rc = lib().dbsa_chunk_attn_kv8(layout.handle, _tensor(q), _tensor(k_pool8), _tensor(v_pool8), C.byref(pages),
-                                   C.c_void_p(self_len.data_ptr()), C.c_void_p(k_scale.data_ptr()), C.c_void_p(v_scale.data_ptr()),
-                                   _tensor(o), C.c_void_p(lse.data_ptr() if lse is not None else None), q.shape[1],
-                                   k_pool8.shape[1], q.shape[2], float(scale), ws_ptr, ws_bytes, C.c_void_p(_stream()))
+    rc = lib().dbsa_chunk_attn_kv8(layout.handle, _tensor(q), _tensor(k_pool8), _tensor(v_pool8), pages, self_len.data_ptr(),
+                                   k_scale.data_ptr(), v_scale.data_ptr(), _tensor(o), _at(lse), q.shape[1], k_pool8.shape[1],
+                                   q.shape[2], float(scale), ws_ptr, ws_bytes, stream)
     _check(rc, "dbsa_chunk_attn_kv8")
     return o
 
@@ -670,16 +673,14 @@ def dbsa_chunk_attn_kv8(layout: Layout, q, k_pool8, v_pool8, k_pages8, v_pages8,
 def _scales(k_scale, v_scale, n_kv_heads: int) -> None:
     import torch
     for s in (k_scale, v_scale):
-        assert s.dtype == torch.float32 and s.numel() == n_kv_heads and s.is_contiguous(), "expected float32 scales, one per KV head"
-    _here(k_scale, v_scale)
+        assert s.dtype == torch.float32 and s.shape == (n_kv_heads,) and s.is_contiguous(), "expected float32 scales, one per KV head"
 
 
-def _rope_args(table, positions, first_id, n_tokens):
-    if positions is not None:
-        assert positions.element_size() == 4 and positions.is_contiguous() and positions.numel() == n_tokens
-    _here(table, positions)
-    return (C.c_void_p(positions.data_ptr() if positions is not None else None), int(first_id),
-            C.c_void_p(table.data_ptr() if table is not None else None), table.shape[0] if table is not None else 0)
+def _rope_args(table, positions, first_id, shape):
+    assert positions is None or (_int32(positions) and positions.numel() == shape[0])
+    assert table is None or (table.is_floating_point() and table.element_size() == 4 and table.is_contiguous() and
+                             2 * table.shape[1] == shape[2] and table.shape[2] == 2), "expected a table of dbsa_rope_table()"
+    return _at(positions), int(first_id), _at(table), 0 if table is None else table.shape[0]
 
 
 def dbsa_kv8_scales(k, v, k_scale=None, v_scale=None, running: bool = False, table=None, positions=None, first_id: int = 0):
@@ -692,31 +693,30 @@ def dbsa_kv8_scales(k, v, k_scale=None, v_scale=None, running: bool = False, tab
     if v_scale is None:
         v_scale = torch.empty(k.shape[1], dtype=torch.float32, device=k.device)
     _scales(k_scale, v_scale, k.shape[1])
-    _here(k, v)
-    rc = lib().dbsa_kv8_scales(_tensor(k), _tensor(v), k.shape[0], k.shape[1], k.shape[2], _dtype_code(k),
-                               *_rope_args(table, positions, first_id, k.shape[0]), int(running), C.c_void_p(k_scale.data_ptr()),
-                               C.c_void_p(v_scale.data_ptr()), C.c_void_p(_stream()))
+    stream = _here(k, v, k_scale, v_scale, table, positions)
+    rc = lib().dbsa_kv8_scales(_tensor(k), _tensor(v), *k.shape, _dtype_code(k), *_rope_args(table, positions, first_id, k.shape),
+                               running, k_scale.data_ptr(), v_scale.data_ptr(), stream)
     _check(rc, "dbsa_kv8_scales")
     return k_scale, v_scale
 
 
 def _cache_rows(k8, v8, rows, n_tokens):
     assert k8.shape == v8.shape and k8.element_size() == 1 and v8.element_size() == 1
-    assert rows is None or (rows.element_size() == 4 and not rows.is_floating_point() and rows.is_contiguous() and rows.numel() == n_tokens)
-    _here(k8, v8, rows)
-    return C.c_void_p(rows.data_ptr() if rows is not None else None)
+    assert rows is None or (_int32(rows) and rows.numel() == n_tokens)
+    return _at(rows)
 
 
 def dbsa_kv8_write(k, v, k8, v8, k_scale, v_scale, rows=None, first_row: int = 0, table=None, positions=None, first_id: int = 0):
     """Quantises k, v [T, Hkv, D] into rows ``rows`` (int32 [T] on the device; outside the cache = not written) or first_row + t
     of the 8-bit caches k8, v8 [rows, Hkv, D]; k is rotated by ``table`` at ``positions`` or first_id + t if one is given."""
-    assert k.shape == v.shape and k.dtype == v.dtype and k.shape[1:] == k8.shape[1:]
-    _scales(k_scale, v_scale, k.shape[1])
-    _here(k, v)
-    rows_ptr = _cache_rows(k8, v8, rows, k.shape[0])
-    rc = lib().dbsa_kv8_write(_tensor(k), _tensor(v), k.shape[0], rows_ptr, int(first_row), _tensor(k8), _tensor(v8), k8.shape[0],
-                              C.c_void_p(k_scale.data_ptr()), C.c_void_p(v_scale.data_ptr()), k.shape[1], k.shape[2],
-                              _dtype_code(k), *_rope_args(table, positions, first_id, k.shape[0]), C.c_void_p(_stream()))
+    shape = k.shape
+    assert shape == v.shape and k.dtype == v.dtype and shape[1:] == k8.shape[1:]
+    _scales(k_scale, v_scale, shape[1])
+    rows_ptr = _cache_rows(k8, v8, rows, shape[0])
+    stream = _here(k, v, k8, v8, k_scale, v_scale, rows, table, positions)
+    rc = lib().dbsa_kv8_write(_tensor(k), _tensor(v), shape[0], rows_ptr, int(first_row), _tensor(k8), _tensor(v8), k8.shape[0],
+                              k_scale.data_ptr(), v_scale.data_ptr(), shape[1], shape[2], _dtype_code(k),
+                              *_rope_args(table, positions, first_id, shape), stream)
     _check(rc, "dbsa_kv8_write")
 
 
@@ -725,16 +725,16 @@ def dbsa_kv8_read(k8, v8, k_scale, v_scale, rows=None, first_row: int = 0, n_tok
     """-> (k, v) [T, Hkv, D]: rows ``rows`` (int32 [T]) or first_row .. first_row + n_tokens - 1 of an 8-bit cache, in ``dtype``
     (bf16 unless given) or in the type of ``k_out``."""
     import torch
-    n = rows.numel() if rows is not None else k8.shape[0] - first_row if n_tokens is None else n_tokens
-    shape = (n, k8.shape[1], k8.shape[2])
+    n_rows, heads, dim = k8.shape
+    n = rows.numel() if rows is not None else n_rows - first_row if n_tokens is None else n_tokens
+    shape = (n, heads, dim)
     k = torch.empty(shape, dtype=dtype or torch.bfloat16, device=k8.device) if k_out is None else k_out
     v = torch.empty(shape, dtype=k.dtype, device=k8.device) if v_out is None else v_out
-    assert tuple(k.shape) == shape and tuple(v.shape) == shape and k.dtype == v.dtype
-    _scales(k_scale, v_scale, k8.shape[1])
-    _here(k, v)
+    assert k.shape == shape and v.shape == shape and k.dtype == v.dtype
+    _scales(k_scale, v_scale, heads)
     rows_ptr = _cache_rows(k8, v8, rows, n)
-    rc = lib().dbsa_kv8_read(_tensor(k8), _tensor(v8), k8.shape[0], rows_ptr, int(first_row), n, C.c_void_p(k_scale.data_ptr()),
-                             C.c_void_p(v_scale.data_ptr()), _tensor(k), _tensor(v), k8.shape[1], k8.shape[2], _dtype_code(k),
-                             C.c_void_p(_stream()))
+    stream = _here(k, v, k8, v8, k_scale, v_scale, rows)
+    rc = lib().dbsa_kv8_read(_tensor(k8), _tensor(v8), n_rows, rows_ptr, int(first_row), n, k_scale.data_ptr(), v_scale.data_ptr(),
+                             _tensor(k), _tensor(v), heads, dim, _dtype_code(k), stream)
     _check(rc, "dbsa_kv8_read")
     return k, v
