@@ -153,7 +153,8 @@ __device__ DBSA_INLINE int lane_here() {
 }
 
 template <typename T, int kD, int kNW, int kBN>
-__global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) {
+// (fp32 workgroups of one or two waves have a compute unit's registers for themselves: their stages fill it)
+__global__ __launch_bounds__(64 * kNW, Kind<T>::kBytes == 4 && kNW <= 2 ? 1 : 2) void chunk_attn_kernel(ChunkParams p) {
   typedef Chunk<T, kD, kNW, kBN> C;
   typedef typename C::Q Q;
   constexpr bool kF32 = C::kF32;
@@ -262,8 +263,8 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     const int pool_steps = n_ent * kSteps, steps = pool_steps + own_steps;
 
     // ---- the stream of steps ----
-    // What a step hangs off: its list entry, or the pages of its keys (scalar loads, requested one step before its rows).
-    // Own steps never straddle a page of kBN tokens or more; smaller pages are at most kPages to a step.
+    // What a step hangs off: its list entry, or the pages of its keys.  Own steps never straddle a page of kBN tokens or more;
+    // smaller pages are at most kPages to a step.
     constexpr int kPages = kBN / 16;
     struct Ahead {
       int start, len;
@@ -323,10 +324,37 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     };
     bool again;           // the quick walk does not do for this record (see there)
     uint32_t partly;      // bit s % 32: some row does not see some key of step s (kept until its product is done)
-    Ahead next;
-    auto request = [&](int s) DBSA_INLINE {  // s < steps: what it hangs off is in `next`
-      const Ahead x = next;
-      next = fetch(min(s + 1, steps - 1));
+    // That of 64 steps, one per lane.  (Scalar loads in every step would be waited for by its first LDS read, which cannot
+    // tell them from its own: they come back in no order.)
+    int window, hung[kPages];
+    auto look_ahead = [&](int s) DBSA_INLINE {
+      window = s;
+      const int at = s + lane_here();
+#pragma unroll
+      for (int i = 0; i < kPages; ++i) hung[i] = 0;
+      if (at < pool_steps) {
+        const int32_t* const e = p.ent + 2 * (static_cast<int64_t>(ent_begin) + at / kSteps);
+        hung[0] = e[0];
+        hung[1] = e[1];
+      } else if (at < steps) {
+        const int first = (own_first + (at - pool_steps) * kBN) >> page_log2;
+        const int32_t* const table = p.page_table + static_cast<int64_t>(own_u) * table_stride;
+        hung[0] = table[min(first, table_stride - 1)];
+        if (page_mask < kBN - 1) {
+#pragma unroll
+          for (int i = 1; i < kPages; ++i) hung[i] = table[min(first + i, table_stride - 1)];
+        }
+      }
+      // (not left in flight: the waits for rows count)
+      wait_vmcnt<0>();
+    };
+    auto request = [&](int s) DBSA_INLINE {  // s < steps, one after the other
+      if (__builtin_expect(s == window + 64, 0)) look_ahead(s);
+      Ahead x;
+#pragma unroll
+      for (int i = 0; i < kPages; ++i) x.page[i] = __builtin_amdgcn_readlane(hung[i], s - window);
+      x.start = x.page[0];
+      x.len = x.page[1];
       const bool own = s >= pool_steps;
       uint64_t kt = kpool, vt = vpool;
       int ks = kpool_stride, vs = vpool_stride, off, len, row;
@@ -688,7 +716,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[ob][i] = 0.f;
       partly = 0;
-      next = fetch(0);
+      look_ahead(0);
     };
     // Step n is put, and the one kFlight behind it requested.  One barrier per step: behind it, step n has landed for all
     // waves, and all have read what they read before it, whose stages the step requested now takes (8 bits: whose stages the
