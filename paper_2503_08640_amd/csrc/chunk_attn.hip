@@ -124,7 +124,7 @@ struct Chunk {
   // Steps requested ahead of the one that is about to be read.  16-bit and fp32 rows go from memory straight into their
   // stage; 8-bit rows into a ring of the wave's own, from where the same lanes widen them into the stages.
   static constexpr bool kDirect = Kind<T>::kStoredBytes != 1;
-  static constexpr int kFlight = kDirect ? (kNW == 8 || (kNW == 4 && !kF32) ? 3 : kF32 ? 1 : 2) : (kNW == 8 ? 3 : kNW == 4 ? 4 : 6);
+  static constexpr int kFlight = kDirect ? (kNW == 8 || !kF32 ? 3 : 1) : kNW == 8 ? 3 : 4;
   // Eight waves of 16-bit operands run as a pipeline over half steps (walk): V is read one step behind K.
   static constexpr bool kPipelined = kNW == 8 && !kF32;
   static constexpr int kKStages = kDirect ? kFlight + 1 : 2, kVStages = kKStages + (kPipelined ? 1 : 0);
@@ -153,8 +153,7 @@ __device__ DBSA_INLINE int lane_here() {
 }
 
 template <typename T, int kD, int kNW, int kBN>
-// (fp32 workgroups of one or two waves have a compute unit's registers for themselves: their stages fill it)
-__global__ __launch_bounds__(64 * kNW, Kind<T>::kBytes == 4 && kNW <= 2 ? 1 : 2) void chunk_attn_kernel(ChunkParams p) {
+__global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) {
   typedef Chunk<T, kD, kNW, kBN> C;
   typedef typename C::Q Q;
   constexpr bool kF32 = C::kF32;
@@ -795,7 +794,7 @@ __global__ __launch_bounds__(64 * kNW, Kind<T>::kBytes == 4 && kNW <= 2 ? 1 : 2)
       }
     };
     if (steps > 0) {
-      if (kNW == 1 || wave * 32 < n_tok * r) walk();
+      if (wave * 32 < n_tok * r) walk();
       else walk_idle();
       // (behind this barrier every wave is done with the stages: the next walk's first steps may land)
       uint32_t* const votes = reinterpret_cast<uint32_t*>(smem + C::kVotesAt);
@@ -931,9 +930,7 @@ template <typename T, int kD>
 hipError_t launch_kind(const ChunkParams& p, hipStream_t stream) {
   constexpr int kWide = Kind<T>::kBytes == 4 ? 32 : 64;
   hipError_t e = hipErrorInvalidValue;
-  if (p.rows == 32) e = launch_shape<T, kD, 1, 32>(p, stream);
-  else if (p.rows == 64) e = launch_shape<T, kD, 2, 32>(p, stream);
-  else if (p.rows == 128) e = launch_shape<T, kD, 4, 32>(p, stream);
+  if (p.rows == 128) e = launch_shape<T, kD, 4, 32>(p, stream);
   else if (p.rows == 256) e = launch_shape<T, kD, 8, kWide>(p, stream);
   if (e != hipSuccess || p.n_merge == 0) return e;
   const int64_t pairs = static_cast<int64_t>(p.n_merge) * p.n_q_heads;

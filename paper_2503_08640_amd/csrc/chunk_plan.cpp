@@ -17,6 +17,11 @@
 
 namespace {
 
+// workgroups of rows rows, per_cu to a compute unit, and what a tile costs one
+struct ChunkShape {
+  int32_t rows, per_cu, tile_cost;
+};
+
 struct Unit {
   int32_t tok_begin, n_tok;  // in ck_toks
   int32_t ent_begin, n_ent;  // pool tiles, in ck_ent
@@ -30,15 +35,6 @@ constexpr int64_t kRecordCost = 3;
 constexpr int64_t kShortUnit = 3;
 
 }  // namespace
-
-ChunkShape dbsa_chunk_shape(int32_t rows) {
-  // workgroups of one wave (32 rows) sit on a compute unit in fours, of two waves in threes, of four in pairs; those with
-  // two row blocks per wave fill it
-  if (rows <= 32) return {32, 4};
-  if (rows <= 64) return {64, 3};
-  if (rows <= 128) return {128, 2};
-  return {256, 1};
-}
 
 int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t n_q_heads, int32_t n_kv_heads,
                            const int32_t* own_tokens, dbsa_layout* L) {
@@ -73,32 +69,6 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
     for (int32_t e = sel->sel_ptr[u]; e < sel->sel_ptr[u + 1]; ++e) users[sel->sel_idx[e] + 1].push_back(u);
   auto seg_tiles = [&](int32_t s) { return lists.gm_seg_ptr[s + 1] - lists.gm_seg_ptr[s]; };
 
-  // Rows of a workgroup: what the walks over the pool want, weighted by their tiles.  A question with a long chunk counts by
-  // itself, the others by what they bring to the segments they share.
-  constexpr int32_t kMostRows = 256;
-  double wanted = 0.0, weight = 0.0;
-  for (int32_t s = 0; s < n_seg; ++s) {
-    int64_t rows = 0;
-    for (int32_t u : users[s]) {
-      const int64_t own = int64_t{new_tokens(u)} * r;
-      if (own >= kMostRows) {
-        wanted += static_cast<double>(seg_tiles(s)) * kMostRows;
-        weight += static_cast<double>(seg_tiles(s));
-      } else {
-        rows += own;
-      }
-    }
-    if (rows > 0) {
-      wanted += static_cast<double>(seg_tiles(s)) * static_cast<double>(std::min<int64_t>(rows, kMostRows));
-      weight += static_cast<double>(seg_tiles(s));
-    }
-  }
-  for (int32_t u = 0; u < B; ++u) {  // own keys
-    const double tiles = own_tokens ? own_tokens[u] / static_cast<double>(kChunkTile) : 0.0;
-    wanted += tiles * static_cast<double>(std::min<int64_t>(int64_t{new_tokens(u)} * r, kMostRows));
-    weight += tiles;
-  }
-  const int32_t typical = weight > 0.0 ? static_cast<int32_t>(wanted / weight + 0.999) : std::min(kMostRows, new_tokens(0) * r);
   // ---- units ----
   std::vector<Unit> units;
   int32_t per_block = 1;  // tokens of a unit
@@ -164,22 +134,29 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
     for (const Unit& x : units) tiles += x.cost();
     return tiles;
   };
-  // Fewer tiles than there are compute units for them: smaller blocks bring in more of those (three questions in fp32, 99
-  // tokens and 60 tiles of 256 rows: 66 us, in blocks of 128 rows 51).
-  const int64_t units_of_head = std::max<int64_t>(1, L->compute_units / n_kv_heads);
-  ChunkShape shape = dbsa_chunk_shape(std::max(typical, r));
-  int64_t tiles = make_units(shape.rows);
-  while (shape.rows > 32 && tiles < units_of_head) {
-    shape = dbsa_chunk_shape(shape.rows / 2);
-    tiles = make_units(shape.rows);
+  // The shape whose longest worker is done first.  Two workgroups of four waves share a compute unit's bandwidths and take 4/3 of
+  // the time of one of eight for a tile (2.9 to 3.4 us and 2.1 to 2.5 with all rows filled), but come in twice the number and
+  // leave fewer rows empty.  16 questions of 8 tokens over 90k: 120 us with 256 rows, 126 with 128; 5 of 37 over 23k and
+  // 26k own keys each: 142 and 119; one token over 2k, where it is the fetching waves that count: 18.5 and 19.6.  (Workgroups
+  // of one or two waves were slower everywhere: 23.5 us there, 321 and 173 for the 16 questions.)
+  const ChunkShape shapes[2] = {{256, 1, 3}, {128, 2, 4}};
+  ChunkShape shape = shapes[0];
+  int64_t tiles = 0, workers = 0;
+  auto longest = [&](const ChunkShape& x) {
+    tiles = make_units(x.rows);
+    workers = std::max<int64_t>(1, std::min<int64_t>(tiles, int64_t{L->compute_units} * x.per_cu / n_kv_heads));
+    return static_cast<double>(tiles + kRecordCost * static_cast<int64_t>(units.size())) / static_cast<double>(workers) * x.tile_cost;
+  };
+  const double four_waves = longest(shapes[1]);
+  if (longest(shapes[0]) > four_waves) {
+    shape = shapes[1];
+    longest(shape);
   }
   L->ck_rows = shape.rows;
 
   // ---- dealing ----
   int64_t total = 0;
   for (const Unit& x : units) total += x.cost() + kRecordCost;
-  const int64_t places = std::max<int64_t>(1, int64_t{L->compute_units} * shape.per_cu / n_kv_heads);
-  const int64_t workers = std::max<int64_t>(1, std::min(places, tiles));
   // one dealing at a share: records (unit, first tile, tiles) worker by worker; true if every tile found a worker
   struct Record {
     int32_t unit, lo, n;

@@ -237,12 +237,8 @@ bool dbsa_crowd_worth(const dbsa_layout* L, int64_t classes, bool cuts);
 int dbsa_build_host_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t first_group, int32_t block_m, int32_t block_n,
                           dbsa_layout* L);
 
-// Chunk attention: keys of a tile, rows of a workgroup and workgroups a compute unit holds for a number of rows wanted,
-// and the plan (fills the ck_* members; own_tokens: expected own keys per question or null).
+// Chunk attention: keys of a tile, words of a record, and the plan (fills the ck_* members; own_tokens: expected own keys per
+// question or null).
 constexpr int32_t kChunkTile = 64, kChunkWords = 12;
-struct ChunkShape {
-  int32_t rows, per_cu;
-};
-ChunkShape dbsa_chunk_shape(int32_t rows);
 int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t n_q_heads, int32_t n_kv_heads,
                            const int32_t* own_tokens, dbsa_layout* L);
