@@ -323,6 +323,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     };
     bool again;           // the quick walk does not do for this record (see there)
     uint32_t partly;      // bit s % 32: some row does not see some key of step s (kept until its product is done)
+    uint32_t lacking;     // the same: some key of step s is not there
     // That of 64 steps, one per lane.  (Scalar loads in every step would be waited for by its first LDS read, which cannot
     // tell them from its own: they come back in no order.)
     int window, hung[kPages];
@@ -347,17 +348,23 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       // (not left in flight: the waits for rows count)
       wait_vmcnt<0>();
     };
-    auto request = [&](int s) DBSA_INLINE {  // s < steps, one after the other
-      if (__builtin_expect(s == window + 64, 0)) look_ahead(s);
+    auto hangs_off = [&](int s) DBSA_INLINE {  // s in the window
       Ahead x;
 #pragma unroll
       for (int i = 0; i < kPages; ++i) x.page[i] = __builtin_amdgcn_readlane(hung[i], s - window);
       x.start = x.page[0];
       x.len = x.page[1];
+      return x;
+    };
+    auto recall = [&](int s) DBSA_INLINE { return s >= window ? hangs_off(s) : fetch(s); };  // s was requested
+    auto request = [&](int s) DBSA_INLINE {  // s < steps, one after the other
+      if (__builtin_expect(s == window + 64, 0)) look_ahead(s);
+      const Ahead x = hangs_off(s);
       const bool own = s >= pool_steps;
       uint64_t kt = kpool, vt = vpool;
       int ks = kpool_stride, vs = vpool_stride, off, len, row;
-      bool whole, in_line;  // in_line: kBN rows one after the other
+      bool whole, in_line;  // every row sees every key; kBN rows one after the other
+      bool lacks = false;   // some key is not there
       if (!own) {
         off = kSteps == 1 ? 0 : (s % kSteps) * kBN;
         len = min((x.len & 0xFFFF) - off, kBN);
@@ -371,10 +378,11 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         in_line = false;
         if (page_mask >= kBN - 1) {
           in_line = len == kBN && page_there(x.page[0]);
-          whole = whole && in_line;
-        } else if (whole) {
-          whole = keys_there(x, off) == kAllKeys;
+          lacks = !in_line;
+        } else {
+          lacks = keys_there(x, off) != kAllKeys;
         }
+        whole = whole && !lacks;
         kt = kown + x.page[0] * page_bytes;
         vt = vown + x.page[0] * page_bytes;
         ks = kown_stride;
@@ -382,6 +390,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       }
       const uint32_t bit = 1u << (s % 32);
       partly = whole ? partly & ~bit : partly | bit;
+      lacking = lacks ? lacking | bit : lacking & ~bit;
       if (__builtin_expect(in_line && narrow, 1)) {
         kt += static_cast<int64_t>(row) * ks;
         vt += static_cast<int64_t>(row) * vs;
@@ -420,25 +429,28 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     // 0 * NaN: keys that are not there, and rows of V with a non-finite value, are staged as zeros, the latter's keys added
     // one by one to the rows that see them.
     uint64_t* const poison = reinterpret_cast<uint64_t*>(smem + C::kPoisonAt);
-    auto clean = [&](int s, uintx4 (&raw)[C::kLoads]) DBSA_INLINE {
+    auto clean = [&](int s, uintx4 (&raw)[C::kLoads]) DBSA_INLINE {  // -> whether it changed any
       uint64_t mask = 0;
       constexpr uint64_t kRowLanes = (1ull << C::kPieces) - 1;
       const int ln = lane_here();
       const int first = own_first + (s - pool_steps) * kBN;
-      const uint64_t there = keys_there(fetch(s), first);
+      const bool lacks = (lacking >> (s % 32)) & 1;
+      const uint64_t there = lacks ? keys_there(recall(s), first) : kAllKeys;
 #pragma unroll
       for (int i = 0; i < C::kLoads; ++i) {
         const bool missing = !((there >> piece_row(i, 64 * wave + ln)) & 1);
         uint64_t bad = 0;
         if (is_v(i)) {
           bad = __builtin_amdgcn_ballot_w64(!missing && not_finite<T>(raw[i]));
-          for (int rr = 0; rr < 64 / C::kPieces; ++rr)
-            if ((bad >> (rr * C::kPieces)) & kRowLanes) mask |= 1ull << (wave_row(i) + rr);
+          if (__builtin_expect(bad != 0, 0))
+            for (int rr = 0; rr < 64 / C::kPieces; ++rr)
+              if ((bad >> (rr * C::kPieces)) & kRowLanes) mask |= 1ull << (wave_row(i) + rr);
         }
         if (missing || ((bad >> (ln / C::kPieces * C::kPieces)) & kRowLanes)) raw[i] = uintx4{0, 0, 0, 0};
       }
       if (ln == 0) poison[(arrived.v - start.v) / C::kTileBytes * kNW + wave] = mask;
       again |= mask != 0;
+      return lacks || mask != 0;
     };
     // What this wave does to its landed pieces of step s before the others read them.
     auto put = [&](int s) DBSA_INLINE {
@@ -449,9 +461,10 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           const int ln = lane_here();
 #pragma unroll
           for (int i = 0; i < C::kLoads; ++i) raw[i] = *reinterpret_cast<const lds_piece*>(static_cast<uintptr_t>(landing(arrived, i) + ln * 16));
-          clean(s, raw);
+          if (clean(s, raw)) {
 #pragma unroll
-          for (int i = 0; i < C::kLoads; ++i) *reinterpret_cast<lds_piece*>(static_cast<uintptr_t>(landing(arrived, i) + ln * 16)) = raw[i];
+            for (int i = 0; i < C::kLoads; ++i) *reinterpret_cast<lds_piece*>(static_cast<uintptr_t>(landing(arrived, i) + ln * 16)) = raw[i];
+          }
         }
         arrived.next_k();
         arrived.next_v();
@@ -488,12 +501,11 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       const int ln = lane_here();
       uint64_t there = ~0ull;
       int last;
-      const Ahead x = fetch(st);
       if (st < pool_steps) {
-        last = (x.len & 0xFFFF) - (st % kSteps) * kBN - 1;
+        last = (recall(st).len & 0xFFFF) - (st % kSteps) * kBN - 1;
       } else {
         const int first = own_first + (st - pool_steps) * kBN;
-        there = keys_there(x, first);
+        if ((lacking >> (st % 32)) & 1) there = keys_there(recall(st), first);
         last = row_pos - first;
       }
       last -= 4 * (ln / 32);
@@ -714,7 +726,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       for (int ob = 0; ob < kO; ++ob)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[ob][i] = 0.f;
-      partly = 0;
+      partly = lacking = 0;
       look_ahead(0);
     };
     // Step n is put, and the one kFlight behind it requested.  One barrier per step: behind it, step n has landed for all
