@@ -380,7 +380,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           in_line = len == kBN && page_there(x.page[0]);
           lacks = !in_line;
         } else {
-          lacks = keys_there(x, off) != kAllKeys;
+          lacks = len < kBN;
+#pragma unroll
+          for (int i = 0; i < kPages; ++i) lacks |= i << page_log2 < kBN && !page_there(x.page[i]);
         }
         whole = whole && !lacks;
         kt = kown + x.page[0] * page_bytes;
@@ -400,6 +402,15 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           const int row0 = i * C::kThreads % C::kOperand / C::kPieces;  // (whole rows per pass of the threads)
           dma16(uniform64((is_v(i) ? vt : kt) + static_cast<unsigned>(row0 * stride)),
                 static_cast<unsigned>(piece_row(0, tid) * stride + fetched_col(i, tid)), landing(wanted, i));
+        }
+      } else if (own && !lacks && narrow) {
+        // smaller pages: the rows a wave fetches in one pass, at most 16, lie in one
+        static_assert(64 / C::kPieces <= 16, "no page is smaller");
+#pragma unroll
+        for (int i = 0; i < C::kLoads; ++i) {
+          const int row0 = __builtin_amdgcn_readfirstlane(wave_row(i)), stride = is_v(i) ? vs : ks;
+          dma16(uniform64((is_v(i) ? vown : kown) + page_of(x, row0) * page_bytes + static_cast<unsigned>(((off + row0) & page_mask) * stride)),
+                static_cast<unsigned>(lane / C::kPieces * stride + fetched_col(i, tid)), landing(wanted, i));
         }
       } else {
         const int t = 64 * wave + lane_here();
