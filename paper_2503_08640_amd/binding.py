@@ -210,6 +210,7 @@ class Layout:
         self.handle = C.c_void_p(handle)
         self.query_stage = query_stage
         self.block_m, self.block_n = block_m, block_n
+        self.chunk_needs = None  # of a chunk layout: new tokens, questions, rows of the pool
 
     def destroy(self) -> None:
         if self.handle:
@@ -397,7 +398,12 @@ def dbsa_layout_build_chunk(sink_len: int, demo_offsets, group_demo_offsets, *, 
     rc = lib().dbsa_layout_build_chunk(C.byref(pool), C.byref(sel), int(n_q_heads), int(n_kv_heads), _p32(own),
                                        DBSA_LAYOUT_HOST_ONLY if host_only else 0, C.c_void_p(stream), C.byref(out))
     _check(rc, "dbsa_layout_build_chunk")
-    return Layout(out.value, False, 0, 64)
+    lay = Layout(out.value, False, 0, 64)
+    ends = np.concatenate([[0], do[gdo]]).astype(np.int64)  # of the sink and the groups, as the pool lays them
+    at = ends[:-1] if ps is None else ps.astype(np.int64)
+    rows = (at + np.diff(ends))[at >= 0]
+    lay.chunk_needs = int(cu[-1]), len(cu) - 1, int(rows.max()) if len(rows) else 0
+    return lay
 
 
 # ---------------------------------------------------------------------------
@@ -633,6 +639,10 @@ def _chunk_args(layout: Layout, q, k_pool, v_pool, k_pages, v_pages, page_table,
     o = torch.empty_like(q) if out is None else out
     assert o.shape == q.shape and o.dtype == q.dtype
     assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous())
+    if layout.chunk_needs is not None:  # (the library refuses other layouts)
+        tokens, questions, rows = layout.chunk_needs
+        assert q.shape[0] >= tokens and ask[0] >= questions and k_pool.shape[0] >= rows, "fewer rows than the layout names"
+        assert lse is None or lse.numel() >= tokens * q.shape[1], "fewer rows than the layout names"
     ws, ws_ptr, ws_bytes = _workspace(layout, q, workspace)
     stream = _here(q, k_pool, v_pool, k_pages, v_pages, page_table, self_len, o, lse, ws, *scales)
     pages = Pages(Tensor(k_pages.data_ptr(), s[1], s[2]), Tensor(v_pages.data_ptr(), s[1], s[2]), s[0], page_table.data_ptr(),

@@ -372,6 +372,54 @@ def test_page_offsets_beyond_32_bits():
     c.check(o, want=want)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "kv8", "f32"])
+@pytest.mark.parametrize("lens,own,sink", [([130], [4500], 70), ([3], [300], 4400)])
+def test_walks_of_many_tiles(dtype, lens, own, sink):
+    """256 KV heads leave a head one or two workers: more steps to a walk than lanes to a wave, own ones and the sink's.  Checked
+    on two of the heads."""
+    c = Case((dtype, 256, 256, 64), lens=lens, own=own, sels=[[0, 1]], page=16 if sink == 70 else 64, seed=21, sink=sink)
+    assert len(c.layout().export_chunk(lens[0])["worker_ptr"]) <= 3
+    o = c.call(c.layout())
+    some = [3, 255]
+    c.q, c.k, c.v = (x[:, some] for x in (c.q, c.k, c.v))
+    c.kp, c.vp = c.kp[:, :, some], c.vp[:, :, some]
+    if dtype == "kv8":
+        c.ks, c.vs = c.ks[some], c.vs[some]
+    c.check(o[:, some])
+
+
+@pytest.mark.parametrize("kind", [KINDS[0], KINDS[8]], ids=["bf16", "kv8"])
+def test_tokens_far_apart(kind):
+    """Token strides of 2^22 elements, in pool and pages: 64 rows do not lie within 32 bits of bytes."""
+    c = Case(kind, lens=[4, 50], own=[60, 90], sels=[[1], [0]], page=32, seed=22)
+    want = c.oracle()
+    bits = torch.uint8 if c.dtype == "kv8" else c.k.dtype
+
+    def apart(x):
+        flat = x.view(bits).reshape(-1, c.hkv, c.d)
+        room = torch.empty((flat.shape[0], 2 ** 22), dtype=bits, device="cuda")
+        view = room[:, :c.hkv * c.d].unflatten(1, (c.hkv, c.d))
+        view.copy_(flat)
+        return (view if x.dim() == 3 else view.unflatten(0, x.shape[:2])).view(x.dtype)
+
+    c.k, c.v, c.kp, c.vp = (apart(x) for x in (c.k, c.v, c.kp, c.vp))
+    c.check(c.call(c.layout()), want=want)
+
+
+def test_tensors_with_fewer_rows_than_the_layout_names_are_refused():
+    c = Case(KINDS[0], lens=[5, 3], own=[60, 30], sels=[[0, 4], [1]], page=16, seed=23)
+    lay, (table, own) = c.layout(), c.device_tables()
+    args = [lay, c.q, c.k, c.v, c.kp, c.vp, table, own, c.scale]
+    B.dbsa_chunk_attn(*args)
+    for change in ({1: c.q[:7]}, {2: c.k[:-1], 3: c.v[:-1]}, {3: c.v[:-1]}, {6: table[:1], 7: own[:1]}, {7: own[:1]}):
+        with pytest.raises(AssertionError):
+            B.dbsa_chunk_attn(*[change.get(i, x) for i, x in enumerate(args)])
+    with pytest.raises(AssertionError):
+        B.dbsa_chunk_attn(*args, lse=torch.empty((c.hq, 7), device="cuda"))
+    with pytest.raises(AssertionError):
+        B.dbsa_chunk_attn(*[x.cpu() if i == 6 else x for i, x in enumerate(args)])
+
+
 def test_a_layout_of_other_heads_is_refused():
     c = Case(KINDS[0], lens=[5], own=[60], sels=[[0, 1]], page=16, seed=20)
     lay = B.dbsa_layout_build_chunk(*c.pool, cu_qlens=c.cu, sel_ptr=[0, 2], sel_idx=[0, 1], n_q_heads=16, n_kv_heads=2)
