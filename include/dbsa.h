@@ -602,8 +602,8 @@ int dbsa_kv8_scales(dbsa_tensor k, dbsa_tensor v, int32_t n_tokens, int32_t n_kv
 /*
  * Quantises rows as they enter a cache: cache row rows[t] (device int32 [n_tokens]; or first_row + t when rows is NULL) of
  * k_cache8 / v_cache8 (e4m3 bytes [n_rows, n_kv_heads, D], strides in bytes, multiples of 16) receives the nearest
- * e4m3 values, ties to even, of k[t] * (1 / k_scale) and v[t] * (1 / v_scale), both operations in fp32; what lies beyond the
- * format becomes +-448, NaN stays NaN, and under a scale whose inverse is not finite (0) every finite element becomes 0.
+ * e4m3 values, ties to even, of the fp32 quotients k[t] / k_scale and v[t] / v_scale; what lies beyond the format becomes
+ * +-448, NaN stays NaN, and under a scale that is not finite or has no finite inverse (0) every finite element becomes 0.
  * K is rotated first as in dbsa_kv8_scales.  A token whose row is outside [0, n_rows) is not written (padding); rows the call
  * does not name stay as they are.  Rows have to differ: one named twice ends up with 16-byte pieces of either token.
  * With rows == NULL: INVALID_ARG unless first_row >= 0 and first_row + n_tokens <= n_rows.  Errors as dbsa_kv8_scales.

@@ -69,28 +69,36 @@ __device__ inline const float* table_row(const Kv8Params& p, int tok) {
   return p.table + static_cast<int64_t>(id) * p.head_dim;
 }
 
-// x * inv to the nearest e4m3 value, ties to even; what lies beyond the format becomes its largest value, NaN stays NaN
-__device__ inline uintx4 quantise16(const float (&x)[kPart], float inv) {
+// What the quotients by a scale are made from.  A scale without a finite inverse (0, or so small that nothing divided by it
+// is) quantises to zeros.
+struct Divisor {
+  float scale, inv;
+};
+__device__ inline Divisor divisor(float scale) {
+  const float inv = 1.f / scale;
+  return inv - inv == 0.f && scale - scale == 0.f ? Divisor{scale, inv} : Divisor{0.f, 0.f};
+}
+
+// x / scale to the nearest e4m3 value, ties to even; what lies beyond the format becomes its largest value, NaN stays NaN.  The
+// quotient is x * inv (off by one step of fp32 or so) corrected by its exact remainder.  Without the correction values near a
+// tie land on its other side: the bytes of a 90k pool differed from the formula's by 2.9e-3 (relative 2-norm), with it by
+// 3e-5, for 197 us instead of 191.
+__device__ inline uintx4 quantise16(const float (&x)[kPart], Divisor d) {
   uintx4 out;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float z = x[4 * i + e] * inv;
-      y[e] = z > kTop ? kTop : z < -kTop ? -kTop : z;
+      const float z = x[4 * i + e] * d.inv;
+      // (the sign from z: the correction turns -0 into 0)
+      y[e] = z >= kTop ? kTop : z <= -kTop ? -kTop : copysignf(fmaf(fmaf(-z, d.scale, x[4 * i + e]), d.inv, z), z);
     }
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
     out[i] = static_cast<unsigned>(w);
   }
   return out;
-}
-
-// 1 / scale; a scale without a finite inverse (0, or so small that nothing divided by it is) quantises to zeros
-__device__ inline float inverse(float scale) {
-  const float inv = 1.f / scale;
-  return inv - inv == 0.f ? inv : 0.f;
 }
 
 // largest finite magnitude
@@ -166,7 +174,7 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8Params p) {
   load16(vp, c);
   load16(vp + half_dim, d);
   if (p.table) rotate16(table_row(p, static_cast<int>(tok)), part * kPart, a, b);
-  const float ki = inverse(p.k_scale[head]), vi = inverse(p.v_scale[head]);
+  const Divisor ki = divisor(p.k_scale[head]), vi = divisor(p.v_scale[head]);
   unsigned char* const ko = static_cast<unsigned char*>(const_cast<void*>(p.k8.ptr)) + row * p.k8.stride_tok + head * p.k8.stride_head + part * kPart;
   unsigned char* const vo = static_cast<unsigned char*>(const_cast<void*>(p.v8.ptr)) + row * p.v8.stride_tok + head * p.v8.stride_head + part * kPart;
   *reinterpret_cast<uintx4*>(ko) = quantise16(a, ki);

@@ -22,10 +22,9 @@ def normal(seed, *shape, dtype=torch.bfloat16):
 
 
 def as_8bit(x, scale):
-    """The definition: x * (1 / scale) in fp32, clamped, to the nearest value."""
-    inv = 1.0 / scale
-    inv = torch.where(torch.isfinite(inv), inv, torch.zeros_like(inv))
-    return (x.float() * inv[:, None]).clamp(-448, 448).to(F8)
+    """The definition: x / scale in fp32, clamped, to the nearest value; zeros where the scale has no finite inverse."""
+    none = ~torch.isfinite(1.0 / scale) | ~torch.isfinite(scale)
+    return torch.where(none[:, None], torch.zeros_like(x.float()), (x.float() / scale[:, None]).clamp(-448, 448)).to(F8)
 
 
 def top(x):
@@ -104,7 +103,7 @@ def test_every_bf16_value_is_rounded_to_the_nearest():
 
 def test_scales_without_an_inverse_give_zeros():
     x = normal(7, 20, 4, 64)
-    scale = torch.tensor([0.0, 1e-39, 2.0, 0.0], device="cuda")
+    scale = torch.tensor([0.0, 1e-39, 2.0, torch.inf], device="cuda")
     k8, v8 = (torch.full((20, 4, 64), 1.0, device="cuda").to(F8) for _ in range(2))
     B.dbsa_kv8_write(x, x, k8, v8, scale, scale)
     assert not k8.float()[:, [0, 1, 3]].any() and same_bytes(k8[:, 2], as_8bit(x, scale)[:, 2])
