@@ -29,9 +29,10 @@ struct Unit {
   int64_t cost() const { return int64_t{n_ent} + own_tiles; }
 };
 
-// What starting and finishing a record costs, in tiles: its rows of Q, the first tiles' latency, the partial states.
+// What starting and finishing a record costs, in tiles: its rows of Q, the first tiles' latency, the partial states.  (128 questions
+// of 4 tokens, 7 records to a worker: 376 us with 2, 372 with 3, 375 with 4, 391 with 6.)
 constexpr int64_t kRecordCost = 3;
-// tiles of a unit that is not worth cutting
+// Tiles of a unit that is not worth cutting: the merge's launch costs 6 us, a tile of a lone workgroup 2.
 constexpr int64_t kShortUnit = 3;
 
 }  // namespace
@@ -188,7 +189,7 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
   };
   // Units stay whole where that costs no worker more than a sixteenth above its share: a cut costs two partial states and the
   // merge of them (2048 tokens behind 90k, 32 units of nearly equal length: 1960 us cut into equal shares, 1830 whole).
-  // And where they are so short that the merge's launch (4 us) would cost more than their few tiles one behind the other (1.3 us each).
+  // And where they are short.
   const int64_t fair = std::max<int64_t>((total + workers - 1) / workers, 1 + kRecordCost);
   if (!deal(std::max(fair + fair / 16, kShortUnit + kRecordCost), true))
     for (int64_t share = fair; !deal(share, false);) share += std::max<int64_t>(1, share / 64);
