@@ -135,12 +135,13 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
     for (const Unit& x : units) tiles += x.cost();
     return tiles;
   };
-  // The shape whose longest worker is done first.  Two workgroups of four waves share a compute unit's bandwidths and take 4/3 of
-  // the time of one of eight for a tile (2.9 to 3.4 us and 2.1 to 2.5 with all rows filled), but come in twice the number and
-  // leave fewer rows empty.  16 questions of 8 tokens over 90k: 120 us with 256 rows, 126 with 128; 5 of 37 over 23k and
-  // 26k own keys each: 142 and 119; one token over 2k, where it is the fetching waves that count: 18.5 and 19.6.  (Workgroups
-  // of one or two waves were slower everywhere: 23.5 us there, 321 and 173 for the 16 questions.)
-  const ChunkShape shapes[2] = {{256, 1, 3}, {128, 2, 4}};
+  // The shape whose longest worker is done first.  Two workgroups of four waves share a compute unit's bandwidths and take about
+  // 3/2 of the time of one of eight for a tile, but come in twice the number and leave fewer rows empty.  12 questions of 229
+  // tokens: 1234 us with 256 rows, 1520 with 128; 122 of 14 behind 13k own keys: 891 and 658; 16 of 8 over 90k: 120 and 126.  46
+  // batches drawn from one token to 1668 came to 2 % above the better shape on average by this ratio, 5.5 % by a ratio of 1,
+  // 7.6 % by 2.  (Workgroups of one or two waves fetch and widen too slowly: one token over 2k 23.5 us, 18.5 with eight
+  // waves; the 16 questions 321 and 173.)
+  const ChunkShape shapes[2] = {{256, 1, 2}, {128, 2, 3}};
   ChunkShape shape = shapes[0];
   int64_t tiles = 0, workers = 0;
   auto longest = [&](const ChunkShape& x) {
@@ -195,10 +196,8 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
     for (int64_t share = fair; !deal(share, false);) share += std::max<int64_t>(1, share / 64);
 
   // ---- records, and where each token's partial states lie ----
-  std::vector<int32_t> pieces(units.size(), 0);
   std::vector<int32_t> parts_of(L->n_query_tokens, 0);  // records that carry the token
   for (const Record& x : recs) {
-    ++pieces[x.unit];
     for (int32_t t = 0; t < units[x.unit].n_tok; ++t) ++parts_of[L->ck_toks[units[x.unit].tok_begin + t]];
   }
   std::vector<std::vector<int32_t>> parts(L->n_query_tokens);
