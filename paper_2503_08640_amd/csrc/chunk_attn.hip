@@ -17,9 +17,9 @@
 //
 // What bounds it.  Many rows: a tile of 256 rows and 64 keys of 128 channels is 2048 cycles of the matrix pipes, 2300 of LDS
 // reads and 2000 of vector work (exponentials above all) on a compute unit; one barrier per step keeps the two waves of a
-// SIMD side by side, and what does not overlap brings a tile to 1.9 us.  2048 tokens behind 90k and 30k own keys: 1851 us, 1085
+// SIMD side by side, and what does not overlap brings a tile to 1.9 us.  2048 tokens behind 90k and 30k own keys: 1860 us, 1080
 // TFLOP/s (the library's product of 8192^3: 1212).  Few rows: memory, and the start of a record, a chain of loads (record,
-// token, row of Q, list, first rows) of 3 us.  16 questions of 8 tokens over 30 % of 90k: 124 us, 3.2 TB/s of unique bytes; one
+// token, row of Q, list, first rows) of 3 us.  16 questions of 8 tokens over 30 % of 90k: 118 us, 3.4 TB/s of unique bytes; one
 // token over 1200 keys: 17 us, 6 of them the merge.  Two row blocks per wave with one wave to a SIMD, which halves the LDS
 // reads, were slower (2203 us for the 2048 tokens, 2028 then): nothing fills the waits of a lone wave.
 #include <atomic>
