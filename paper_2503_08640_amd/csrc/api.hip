@@ -1241,7 +1241,7 @@ int kv8_common(Kv8Params& p, dbsa_tensor k, dbsa_tensor v, const dbsa_tensor* k8
   if (dtype != DBSA_BF16 && dtype != DBSA_F32) return DBSA_ERR_UNSUPPORTED;
   if (head_dim != 64 && head_dim != 128) return DBSA_ERR_UNSUPPORTED;
   if (n_tokens < 0 || n_kv_heads < 1 || !k_scale || !v_scale) return DBSA_ERR_INVALID_ARG;
-  // (a launch counts its threads, at most 8 per token and head, in workgroups of 256)
+  // (a launch has at most 32 threads per token and head)
   if (int64_t{n_tokens} * n_kv_heads > (int64_t{1} << 34)) return DBSA_ERR_UNSUPPORTED;
   if (n_tokens > 0 && (!tensor_ok(k, dtype) || !tensor_ok(v, dtype))) return DBSA_ERR_INVALID_ARG;
   if (k8) {

@@ -3,7 +3,7 @@
 // kv8_scales finds the scales (largest magnitude at the top of the format, 448), kv8_write quantises rows as they enter the
 // cache, with the encoding-time rotation of the keys on the way, kv8_read brings rows back.  All three are bound by memory:
 // one pass, 16-byte accesses, a thread keeps the two channel ranges that the rotation pairs.  90k tokens of 8 heads of 128
-// channels in bf16: scales 88 us (4.2 TB/s), write 105 (5.3 TB/s read and written); 27100 rows back to bf16: 38 us (4.4 TB/s);
+// channels in bf16: scales 88 us (4.2 TB/s), write 105 (5.3 TB/s read and written); 27100 rows back to bf16: 36 us (4.6 TB/s);
 // small calls are bound by the host's launch (an append of 16 tokens 10.6 us, the kernel 6.6).  Walking the write backwards,
 // so that it begins with what the scales' pass left in the last-level cache, changed nothing.
 #include <cstdint>
@@ -37,20 +37,6 @@ __device__ inline void load16(const float* p, float (&x)[kPart]) {
     for (int e = 0; e < 4; ++e) x[4 * i + e] = v[e];
   }
 }
-__device__ inline void store16(__bf16* p, const float (&x)[kPart]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    bf16x8 v;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(x[8 * i + e]);
-    reinterpret_cast<bf16x8*>(p)[i] = v;
-  }
-}
-__device__ inline void store16(float* p, const float (&x)[kPart]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) reinterpret_cast<floatx4*>(p)[i] = floatx4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-}
-
 // channels i .. i+15 (lo) and their partners at + D/2 (hi), rotated by table row `row` in fp32
 __device__ inline void rotate16(const float* row, int i, float (&lo)[kPart], float (&hi)[kPart]) {
   const floatx4* const cs = reinterpret_cast<const floatx4*>(row + 2 * i);
@@ -65,6 +51,8 @@ __device__ inline void rotate16(const float* row, int i, float (&lo)[kPart], flo
     }
   }
 }
+
+__device__ inline int64_t thread_index() { return (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 256 + threadIdx.x; }
 
 __device__ inline const float* table_row(const Kv8Params& p, int tok) {
   int id = p.positions ? p.positions[tok] : p.first_id + tok;
@@ -162,7 +150,7 @@ __global__ __launch_bounds__(256) void kv8_scales_kernel(Kv8Params p) {
 template <typename T>
 __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8Params p) {
   const int half_dim = p.head_dim / 2, parts = half_dim / kPart;
-  const int64_t idx = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t idx = thread_index();
   const int part = static_cast<int>(idx % parts);
   const int head = static_cast<int>((idx / parts) % p.n_kv_heads);
   const int64_t tok = idx / (static_cast<int64_t>(parts) * p.n_kv_heads);
@@ -186,43 +174,59 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8Params p) {
   *reinterpret_cast<uintx4*>(vo + half_dim) = quantise16(d, vi);
 }
 
-// One thread: sixteen channels of K and of V.
+// One thread: as many channels of K and of V as make sixteen bytes of the result, so that a wave's stores fill whole lines
+// (16 channels to a thread, two or four stores of it 16 bytes apart: 41 us for 27100 rows, so 36.4).
 template <typename T>
 __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8Params p) {
-  const int parts = p.head_dim / kPart;
-  const int64_t idx = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  constexpr int kCh = 16 / sizeof(T);
+  typedef T out_t __attribute__((ext_vector_type(kCh)));
+  typedef unsigned raw_t __attribute__((ext_vector_type(2)));
+  const int parts = p.head_dim / kCh;
+  const int64_t idx = thread_index();
   const int part = static_cast<int>(idx % parts);
   const int head = static_cast<int>((idx / parts) % p.n_kv_heads);
   const int64_t tok = idx / (static_cast<int64_t>(parts) * p.n_kv_heads);
   if (tok >= p.n_tokens) return;
   const int64_t row = p.rows ? p.rows[tok] : p.first_row + tok;
   const bool there = row >= 0 && row < p.n_cache_rows;  // (a row that is not gives zeros)
-  auto bring = [&](const TensorView& from, const TensorView& to, float scale) {
-    uintx4 raw{0, 0, 0, 0};
-    if (there)
-      raw = *reinterpret_cast<const uintx4*>(static_cast<const unsigned char*>(from.ptr) + row * from.stride_tok + head * from.stride_head + part * kPart);
-    float x[kPart];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(raw[i]), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(raw[i]), true);
-      x[4 * i] = lo[0] * scale;
-      x[4 * i + 1] = lo[1] * scale;
-      x[4 * i + 2] = hi[0] * scale;
-      x[4 * i + 3] = hi[1] * scale;
+  auto stored = [&](const TensorView& from) {
+    raw_t raw{0, 0};
+    if (there) {
+      const unsigned* const at = reinterpret_cast<const unsigned*>(static_cast<const unsigned char*>(from.ptr) + row * from.stride_tok + head * from.stride_head + part * kCh);
+      if constexpr (kCh == 8) raw = *reinterpret_cast<const raw_t*>(at);
+      else raw[0] = *at;
     }
-    store16(static_cast<T*>(const_cast<void*>(to.ptr)) + tok * to.stride_tok + head * to.stride_head + part * kPart, x);
+    return raw;
   };
-  bring(p.k8, p.k, p.k_scale[head]);
-  bring(p.v8, p.v, p.v_scale[head]);
+  auto bring = [&](const raw_t& raw, const TensorView& to, float scale) {
+    out_t x;
+#pragma unroll
+    for (int i = 0; i < kCh / 4; ++i) {
+      const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(raw[i]), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(raw[i]), true);
+      x[4 * i] = static_cast<T>(lo[0] * scale);
+      x[4 * i + 1] = static_cast<T>(lo[1] * scale);
+      x[4 * i + 2] = static_cast<T>(hi[0] * scale);
+      x[4 * i + 3] = static_cast<T>(hi[1] * scale);
+    }
+    *reinterpret_cast<out_t*>(static_cast<T*>(const_cast<void*>(to.ptr)) + tok * to.stride_tok + head * to.stride_head + part * kCh) = x;
+  };
+  const raw_t k8 = stored(p.k8), v8 = stored(p.v8);  // (both, before the stores that they may not pass)
+  const float k_scale = p.k_scale[head], v_scale = p.v_scale[head];
+  bring(k8, p.k, k_scale);
+  bring(v8, p.v, v_scale);
 }
 
-unsigned blocks(int64_t threads) { return static_cast<unsigned>((threads + 255) / 256); }
+// A grid counts its threads per dimension in 32 bits.
+dim3 grid_of(int64_t threads) {
+  const int64_t blocks = (threads + 255) / 256, wide = int64_t{1} << 23;
+  return blocks <= wide ? dim3(static_cast<unsigned>(blocks)) : dim3(static_cast<unsigned>(wide), static_cast<unsigned>((blocks + wide - 1) / wide));
+}
 
 }  // namespace
 
 hipError_t launch_kv8_scales(const Kv8Params& p, bool bf16, bool running, hipStream_t stream) {
   if (!running) {
-    kv8_zero_scales_kernel<<<dim3(blocks(p.n_kv_heads)), dim3(256), 0, stream>>>(p.k_scale, p.v_scale, p.n_kv_heads);
+    kv8_zero_scales_kernel<<<grid_of(p.n_kv_heads), dim3(256), 0, stream>>>(p.k_scale, p.v_scale, p.n_kv_heads);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (p.n_tokens == 0) return hipSuccess;
@@ -237,7 +241,7 @@ hipError_t launch_kv8_scales(const Kv8Params& p, bool bf16, bool running, hipStr
 
 hipError_t launch_kv8_write(const Kv8Params& p, bool bf16, hipStream_t stream) {
   if (p.n_tokens == 0) return hipSuccess;
-  const dim3 grid(blocks(static_cast<int64_t>(p.n_tokens) * p.n_kv_heads * (p.head_dim / 2 / kPart)));
+  const dim3 grid = grid_of(static_cast<int64_t>(p.n_tokens) * p.n_kv_heads * (p.head_dim / 2 / kPart));
   if (bf16) kv8_write_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(p);
   else kv8_write_kernel<float><<<grid, dim3(256), 0, stream>>>(p);
   return hipGetLastError();
@@ -245,7 +249,7 @@ hipError_t launch_kv8_write(const Kv8Params& p, bool bf16, hipStream_t stream) {
 
 hipError_t launch_kv8_read(const Kv8Params& p, bool bf16, hipStream_t stream) {
   if (p.n_tokens == 0) return hipSuccess;
-  const dim3 grid(blocks(static_cast<int64_t>(p.n_tokens) * p.n_kv_heads * (p.head_dim / kPart)));
+  const dim3 grid = grid_of(static_cast<int64_t>(p.n_tokens) * p.n_kv_heads * (p.head_dim / (bf16 ? 8 : 4)));
   if (bf16) kv8_read_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(p);
   else kv8_read_kernel<float><<<grid, dim3(256), 0, stream>>>(p);
   return hipGetLastError();
