@@ -4,7 +4,7 @@
 // cache, with the encoding-time rotation of the keys on the way, kv8_read brings rows back.  All three are bound by memory:
 // one pass, 16-byte accesses, a thread keeps the two channel ranges that the rotation pairs.  90k tokens of 8 heads of 128
 // channels in bf16: scales 88 us (4.2 TB/s), write 105 (5.3 TB/s read and written); 27100 rows back to bf16: 36 us (4.6 TB/s);
-// small calls are bound by the host's launch (an append of 16 tokens 10.6 us, the kernel 6.6).  Walking the write backwards,
+// small calls are bound by the host's launch (an append of 16 tokens 10.4 us, the kernel 6.6).  Walking the write backwards,
 // so that it begins with what the scales' pass left in the last-level cache, changed nothing.
 #include <cstdint>
 
