@@ -220,3 +220,9 @@ def test_refusals_of_the_8bit_calls(which):
                 (dict(table=64, n_pos=9, first_id=-1), B.DBSA_ERR_INVALID_ARG), (dict(table=72, n_pos=9), B.DBSA_ERR_INVALID_ARG)]
     for change, code in bad:
         assert kv8_call(which, **change) == code, change
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_workgroups_have_four_or_eight_waves(seed):
+    p, lens, sels, hq, hkv, own = random_case(seed)
+    assert build(p, lens, sels, hq, hkv, own).export_chunk(int(sum(lens)))["rows"] in (128, 256)
