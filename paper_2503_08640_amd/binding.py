@@ -636,6 +636,7 @@ def _chunk_args(layout: Layout, q, k_pool, v_pool, k_pages, v_pages, page_table,
     assert len(shape) == 4 and s[3] == 1 and v_pages.stride() == s and v_pages.shape == shape
     assert len(ask) == 2 and _int32(page_table), "expected a contiguous int32 page table"
     assert _int32(self_len) and self_len.shape == ask[:1] and k_pool.shape[1:] == shape[2:] and v_pool.shape == k_pool.shape
+    assert q.shape[2:] == shape[3:], "q and the caches have different channels"
     o = torch.empty_like(q) if out is None else out
     assert o.shape == q.shape and o.dtype == q.dtype
     assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous())
