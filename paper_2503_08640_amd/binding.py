@@ -643,7 +643,7 @@ def _chunk_args(layout: Layout, q, k_pool, v_pool, k_pages, v_pages, page_table,
     if layout.chunk_needs is not None:  # (the library refuses other layouts)
         tokens, questions, rows = layout.chunk_needs
         assert q.shape[0] >= tokens and ask[0] >= questions and k_pool.shape[0] >= rows, "fewer rows than the layout names"
-        assert lse is None or lse.numel() >= tokens * q.shape[1], "fewer rows than the layout names"
+        assert lse is None or lse.shape == (q.shape[1], tokens), "expected an lse [Hq, sum T], fewer rows than q where q has more"
     ws, ws_ptr, ws_bytes = _workspace(layout, q, workspace)
     stream = _here(q, k_pool, v_pool, k_pages, v_pages, page_table, self_len, o, lse, ws, *scales)
     pages = Pages(Tensor(k_pages.data_ptr(), s[1], s[2]), Tensor(v_pages.data_ptr(), s[1], s[2]), s[0], page_table.data_ptr(),
@@ -655,7 +655,7 @@ def dbsa_chunk_attn(layout: Layout, q, k_pool, v_pool, k_pages, v_pages, page_ta
                     workspace=None):
     """Stage 2 for the new tokens q [sum T, Hq, D] of every question: pool part as the layout lists it, own keys (older ones
     and the new tokens', self_len int32 [B] on the device) in pages k_pages / v_pages [pages, page tokens, Hkv, D] by page_table
-    int32 [B, pages of a question].  Returns O [sum T, Hq, D]."""
+    int32 [B, pages of a question].  Returns O [sum T, Hq, D]; lse, if given, is float32 [Hq, sum T]."""
     o, ws, pages, ws_ptr, ws_bytes, stream = _chunk_args(layout, q, k_pool, v_pool, k_pages, v_pages, page_table, self_len, out, lse,
                                                          workspace)
     assert q.dtype == k_pool.dtype == v_pool.dtype == k_pages.dtype == v_pages.dtype

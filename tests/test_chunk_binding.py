@@ -30,3 +30,11 @@ def test_queries_of_other_channels_than_the_caches_are_refused(kv8):
     for d in (128, 32):
         with pytest.raises(AssertionError, match="channels"):
             call(kv8, q=torch.zeros((3, 4, d), dtype=BF16))
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+def test_an_lse_of_other_rows_is_refused(kv8):
+    """Its rows are sum T long, also where q has more."""
+    for shape in ((4, 5), (4, 2), (5, 3), (3, 4), (12,)):
+        with pytest.raises(AssertionError, match="lse"):
+            call(kv8, spare=2, lse=torch.zeros(shape))
