@@ -8,7 +8,6 @@
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
-#include <functional>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -807,8 +806,13 @@ const char* dbsa_strerror(int code) {
 }
 
 namespace {
-// build_lists(L): fills the host lists, returns a DBSA_* code
-int build_layout_with(int32_t flags, void* stream, dbsa_layout** out, const std::function<int(dbsa_layout*)>& build_lists) {
+// what a chunk layout is built from besides the pool and the selection
+struct ChunkBatch {
+  int32_t n_q_heads, n_kv_heads;
+  const int32_t* own_tokens;
+};
+int build_layout(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t first_group, int32_t block_m,
+                 int32_t block_n, int32_t flags, void* stream, dbsa_layout** out, const ChunkBatch* chunk = nullptr) {
   if (!out || (flags & ~DBSA_LAYOUT_HOST_ONLY)) return DBSA_ERR_INVALID_ARG;
   dbsa_layout* L = new (std::nothrow) dbsa_layout();
   if (!L) return DBSA_ERR_INVALID_ARG;
@@ -816,7 +820,8 @@ int build_layout_with(int32_t flags, void* stream, dbsa_layout** out, const std:
   // the decode chunking and the split / persistent prefill launches are sized for the current device
   if (!(flags & DBSA_LAYOUT_HOST_ONLY)) L->compute_units = device_compute_units();
   try {
-    rc = build_lists(L);
+    rc = chunk ? dbsa_build_chunk_lists(pool, sel, chunk->n_q_heads, chunk->n_kv_heads, chunk->own_tokens, L)
+               : dbsa_build_host_lists(pool, sel, first_group, block_m, block_n, L);
   } catch (...) {
     rc = DBSA_ERR_INVALID_ARG;
   }
@@ -835,13 +840,6 @@ int build_layout_with(int32_t flags, void* stream, dbsa_layout** out, const std:
   *out = L;
   return DBSA_OK;
 }
-
-int build_layout(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t first_group, int32_t block_m,
-                 int32_t block_n, int32_t flags, void* stream, dbsa_layout** out) {
-  return build_layout_with(flags, stream, out, [&](dbsa_layout* L) {
-    return dbsa_build_host_lists(pool, sel, first_group, block_m, block_n, L);
-  });
-}
 }  // namespace
 
 int dbsa_layout_build(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t block_m, int32_t block_n,
@@ -857,9 +855,8 @@ int dbsa_layout_build_append(const dbsa_pool_desc* pool, int32_t first_group, in
 
 int dbsa_layout_build_chunk(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t n_q_heads, int32_t n_kv_heads,
                             const int32_t* own_tokens, int32_t flags, void* stream, dbsa_layout** out) {
-  return build_layout_with(flags, stream, out, [&](dbsa_layout* L) {
-    return dbsa_build_chunk_lists(pool, sel, n_q_heads, n_kv_heads, own_tokens, L);
-  });
+  const ChunkBatch chunk{n_q_heads, n_kv_heads, own_tokens};
+  return build_layout(pool, sel, -1, 0, 0, flags, stream, out, &chunk);
 }
 
 int dbsa_layout_export_chunk(const dbsa_layout* L, int32_t* rows, const int32_t** worker_ptr, int32_t* n_workers,
