@@ -211,7 +211,8 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8Params p) {
     *reinterpret_cast<out_t*>(static_cast<T*>(const_cast<void*>(to.ptr)) + tok * to.stride_tok + head * to.stride_head + part * kCh) = x;
   };
   const raw_t k8 = stored(p.k8), v8 = stored(p.v8);  // (both, before the stores that they may not pass)
-  const float k_scale = p.k_scale[head], v_scale = p.v_scale[head];
+  // (a scale may be infinite or no number, and zero times it is none)
+  const float k_scale = there ? p.k_scale[head] : 0.f, v_scale = there ? p.v_scale[head] : 0.f;
   bring(k8, p.k, k_scale);
   bring(v8, p.v, v_scale);
 }

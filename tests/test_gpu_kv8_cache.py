@@ -285,3 +285,12 @@ def test_a_question_answered_from_an_8bit_cache(hq, hkv):
                           sel["sel_ptr"], np.asarray(sel["sel_idx"]), pc.scale)
     assert_close(to_f64(step), ref, "decode over the same caches")
     assert_close(to_f64(o), ref, "one-token chunk over the same caches")
+
+
+def test_absent_rows_are_read_as_zeros_under_any_scale():
+    k8 = torch.full((5, 4, 64), 3.0, device="cuda").to(F8)
+    scale = torch.tensor([torch.inf, torch.nan, -torch.inf, -2.0], device="cuda")
+    rows = torch.tensor([-1, 5, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    for dtype in (torch.bfloat16, torch.float32):
+        for x in B.dbsa_kv8_read(k8, k8, scale, scale, rows=rows, dtype=dtype):
+            assert (x == 0).all()
