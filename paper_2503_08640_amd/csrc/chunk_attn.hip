@@ -175,12 +175,15 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
   const int hk = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x) % p.n_kv_heads);
   const int worker = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x) / p.n_kv_heads);
   const int r = p.n_q_heads / p.n_kv_heads;
-  // scores in log2 units: scale * log2 e (and the keys' scale) goes onto them in fp32.  A negative key scale turns the
-  // rows of Q around; a scale of nothing stays above zero, so that a masked -inf stays one.
-  float c2 = p.scale_log2e;
-  if (p.k_scale) c2 *= p.k_scale[hk];
-  const bool negate = c2 < 0.f;
-  c2 = fmaxf(fabsf(c2), 1e-30f);
+  // scores in log2 units: scale * log2 e (and the keys' scale) goes onto them in fp32.  The softmax takes a positive factor
+  // (a masked -inf stays one, the largest score the largest): the sign of a negative key scale goes onto the rows of Q, and so
+  // do a factor of nothing and one that is no number.
+  float c2 = p.scale_log2e, on_rows = 1.f;
+  if constexpr (kEs == 1) {
+    const float c = c2 * p.k_scale[hk];
+    on_rows = c > 0.f ? 1.f : c < 0.f ? -1.f : c;
+    c2 = c == 0.f || c != c ? 1.f : fabsf(c);
+  }
 
   const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_byte*)smem));
   // What the step loop reads of the arguments, in registers of its own: the compiler otherwise picks the ADDRESS of the
@@ -254,7 +257,12 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
         qf[c] = *reinterpret_cast<const Piece*>(qp + (2 * c + half) * (16 / static_cast<int>(sizeof(Q))));
-        if (negate) qf[c] = -qf[c];
+        if constexpr (kEs == 1) {
+          if (on_rows != 1.f) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) qf[c][e] = static_cast<Q>(static_cast<float>(qf[c][e]) * on_rows);
+          }
+        }
       }
     }
     // own tiles of this record: its share of those up to the last token's own key

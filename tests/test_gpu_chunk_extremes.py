@@ -1,0 +1,63 @@
+"""Chunk attention and 8-bit caches at the edge of what they accept: scales that are not finite, nothing, tiny or huge, values near
+the top of their type, infinities that a row does see.  Against the fp64 oracle, with the tolerances of test_gpu_chunk.py."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_chunk import Case
+
+pytestmark = pytest.mark.gpu
+
+# heads, KV heads; lens, own: one question whose tokens walk by themselves, some that share their groups' tiles, and (128 KV heads)
+# workgroups with many records
+BATCHES = {
+    "alone": dict(lens=[300], own=[420], sels=[[4, 2]]),
+    "shared": dict(lens=[3, 1, 9], own=[90, 200, 9], sels=[[0, 1], [1], [3, 0]]),
+    "one": dict(lens=[1], own=[70], sels=[[1]]),
+}
+
+
+def case(dtype, d, batch, seed, heads=(8, 2), **kw):
+    return Case((dtype, *heads, d), page=32, seed=seed, **dict(BATCHES[batch], **kw))
+
+
+def run(c):
+    lse = torch.zeros((c.hq, int(c.cu[-1])), device="cuda")
+    return c.call(c.layout(), lse=lse), lse
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("batch", sorted(BATCHES))
+def test_a_scale_that_is_no_number_gives_no_numbers(batch, d):
+    for which in ("ks", "vs"):
+        c = case("kv8", d, batch, seed=50, heads=(8, 4))
+        want = c.oracle()
+        getattr(c, which)[1] = torch.nan
+        o = run(c)[0]
+        assert torch.isnan(o[:, 2:4]).all()
+        rest = [0, 1, 4, 5, 6, 7]
+        c.hq, c.hkv = 6, 3
+        c.check(o[:, rest], want={k: v if k == "keys" else v[rest] if k == "lse" else v[:, rest] for k, v in want.items()})
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("batch", sorted(BATCHES))
+def test_a_tiny_softmax_scale(dtype, d, batch):
+    c = case(dtype, d, batch, seed=51)
+    c.q, c.k, c.kp = (x * 1e16 for x in (c.q, c.k, c.kp))
+    c.scale = 1e-32 / np.sqrt(d)
+    o, lse = run(c)
+    c.check(o, lse)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("batch", sorted(BATCHES))
+def test_tiny_key_scales_and_none(batch, d):
+    """Factors far below 1 against queries far above it, of either sign; under a scale of zero all keys weigh the same, and a
+    product of queries and bytes beyond fp32 does not matter."""
+    c = case("kv8", d, batch, seed=52, heads=(8, 4))
+    c.ks = torch.tensor([1e-34, -3e-35, 0.0, -0.0], device="cuda")
+    c.q[:, :4] *= 1e32
+    c.q[:, 4:] *= 1e37
+    o, lse = run(c)
+    c.check(o, lse)
