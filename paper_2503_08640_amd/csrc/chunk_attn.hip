@@ -871,8 +871,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
               floatx4{acc[ob][4 * g], acc[ob][4 * g + 1], acc[ob][4 * g + 2], acc[ob][4 * g + 3]};
       if (half == 0) *reinterpret_cast<floatx2*>(out + kD) = floatx2{m, sum};
     } else {
-      // (a row that saw no key is zero)
-      const float inv = sum > 0.f || sum != sum ? (p.v_scale ? p.v_scale[hk] : 1.f) / sum : 0.f;
+      // (A row that saw no key is zero.  The values' scale comes behind the division: over a large sum a small one would lose its bits.)
+      const bool any_key = sum > 0.f || sum != sum;
+      const float inv = any_key ? 1.f / sum : 0.f, v_scale = kEs == 1 && any_key ? p.v_scale[hk] : 1.f;
       Q* const out = static_cast<Q*>(const_cast<void*>(p.o.ptr)) + row_tok * p.o.stride_tok + row_head * p.o.stride_head;
 #pragma unroll
       for (int ob = 0; ob < kO; ++ob)
@@ -880,8 +881,8 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         for (int g = 0; g < 4; ++g) {
           typedef Q four __attribute__((ext_vector_type(4)));
           *reinterpret_cast<four*>(out + 32 * ob + 8 * g + 4 * half) =
-              four{static_cast<Q>(acc[ob][4 * g] * inv), static_cast<Q>(acc[ob][4 * g + 1] * inv),
-                   static_cast<Q>(acc[ob][4 * g + 2] * inv), static_cast<Q>(acc[ob][4 * g + 3] * inv)};
+              four{static_cast<Q>(acc[ob][4 * g] * inv * v_scale), static_cast<Q>(acc[ob][4 * g + 1] * inv * v_scale),
+                   static_cast<Q>(acc[ob][4 * g + 2] * inv * v_scale), static_cast<Q>(acc[ob][4 * g + 3] * inv * v_scale)};
         }
       if (p.lse && half == 0) p.lse[static_cast<int64_t>(row_head) * p.n_rows + row_tok] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     }
@@ -941,14 +942,14 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
   }
 #pragma unroll
   for (int o = kTeam / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kTeam);
-  const float v_scale = p.v_scale ? p.v_scale[head / (p.n_q_heads / p.n_kv_heads)] : 1.f;
-  const float inv = sum > 0.f || sum != sum ? v_scale / sum : 0.f;
+  const bool any_key = sum > 0.f || sum != sum;
+  const float inv = any_key ? 1.f / sum : 0.f, v_scale = any_key && p.v_scale ? p.v_scale[head / (p.n_q_heads / p.n_kv_heads)] : 1.f;
   Q* const out = static_cast<Q*>(const_cast<void*>(p.o.ptr)) + tok * p.o.stride_tok + head * p.o.stride_head + in * kPer;
   typedef Q four __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int e = 0; e < kPer / 4; ++e)
-    *reinterpret_cast<four*>(out + 4 * e) = four{static_cast<Q>(acc[e][0] * inv), static_cast<Q>(acc[e][1] * inv),
-                                                 static_cast<Q>(acc[e][2] * inv), static_cast<Q>(acc[e][3] * inv)};
+    *reinterpret_cast<four*>(out + 4 * e) = four{static_cast<Q>(acc[e][0] * inv * v_scale), static_cast<Q>(acc[e][1] * inv * v_scale),
+                                                 static_cast<Q>(acc[e][2] * inv * v_scale), static_cast<Q>(acc[e][3] * inv * v_scale)};
   if (p.lse && in == 0) p.lse[static_cast<int64_t>(head) * p.n_rows + tok] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 

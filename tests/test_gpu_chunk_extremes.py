@@ -26,6 +26,28 @@ def run(c):
     return c.call(c.layout(), lse=lse), lse
 
 
+def second_half_higher(c, by):
+    """Scores of about 0 for the first 32 keys of every 64, `by` (log2 units) for the others: in the sink, in every group, in the
+    own keys."""
+    sign = torch.sign(torch.randn(c.d, generator=torch.Generator().manual_seed(1))).cuda()
+    size = by * np.log(2) / np.sqrt(c.d)  # (q = sign: the product is size * D, the scale 1 / sqrt D)
+    bounds = np.concatenate([[0], c.pool[1][c.pool[2]]])
+    at = np.concatenate([np.arange(b - a) for a, b in zip(bounds, bounds[1:])])
+    own = np.arange(c.kp.shape[0] * c.page).reshape(c.kp.shape[:2]) % c.page
+    for u in range(len(c.lens)):
+        for i, page in enumerate(c.table[u]):
+            if page >= 0:
+                own[page] = i * c.page + np.arange(c.page)
+
+    def keys(x):
+        high = torch.from_numpy((x % 64 >= 32).astype(np.float32)).cuda()[..., None, None] * size * sign
+        high = high.expand(*x.shape, c.hkv, c.d)
+        return high if c.ks is None else high / c.ks[:, None]
+
+    c.k, c.kp = keys(at).to(c.k.dtype).contiguous(), keys(own).to(c.k.dtype).contiguous()
+    c.q = sign.expand(c.q.shape).to(c.q.dtype).contiguous()
+
+
 @pytest.mark.parametrize("d", [128, 64])
 @pytest.mark.parametrize("batch", sorted(BATCHES))
 def test_a_scale_that_is_no_number_gives_no_numbers(batch, d):
@@ -61,3 +83,14 @@ def test_tiny_key_scales_and_none(batch, d):
     c.q[:, 4:] *= 1e37
     o, lse = run(c)
     c.check(o, lse)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("batch", sorted(BATCHES))
+def test_tiny_and_huge_value_scales(batch, d):
+    for size in (1.2e-38, 1e35):
+        c = case("kv8", d, batch, seed=55)
+        second_half_higher(c, 18)
+        c.vs = torch.full((c.hkv,), size, device="cuda")
+        o, lse = run(c)
+        c.check(o, lse)
