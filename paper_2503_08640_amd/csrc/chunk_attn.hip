@@ -65,15 +65,20 @@ __device__ inline void dma16_wide(uint64_t address, unsigned lds_addr) {
 
 // O += V P, as statements that change the accumulators where they are (left to itself the compiler keeps two sets of them and
 // copies one to the other in every step).  It does not know what these are, so the spacing rules are kept by the order of the
-// code: an accumulator's next product is at least two matrix instructions away, and the vector ALU reads one only behind
-// product_fence().
+// code: an accumulator's next product is at least two matrix instructions away, and the vector ALU reads or writes one only
+// behind product_fence(), which passes the accumulators on, so that no use of them can be moved in front of its waits.
 __device__ DBSA_INLINE void product_bf16(floatx16& o, const bf16x8& v, const bf16x8& p) {
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
 }
 __device__ DBSA_INLINE void product_f32(floatx16& o, float v, float p) {
   asm volatile("v_mfma_f32_32x32x2_f32 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
 }
-__device__ DBSA_INLINE void product_fence() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+template <int kO>
+__device__ DBSA_INLINE void product_fence(floatx16 (&acc)[kO]) {
+  static_assert(kO == 2 || kO == 4, "head_dim 64 or 128");
+  if constexpr (kO == 2) asm volatile("s_nop 15\n\ts_nop 15" : "+v"(acc[0]), "+v"(acc[1])::"memory");
+  else asm volatile("s_nop 15\n\ts_nop 15" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3])::"memory");
+}
 
 // sixteen e4m3 bytes as bf16
 __device__ DBSA_INLINE void widen16(const uintx4& raw, uintx4& lo, uintx4& hi) {
@@ -803,6 +808,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           read.next_v();
         }
       }
+      product_fence(acc);
     };
     // a wave without rows brings its pieces
     auto walk_idle = [&]() DBSA_INLINE {
@@ -824,9 +830,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         static_for<kB>([&](auto KB) DBSA_INLINE { run(KB, kNone, kNone); });
         softmax(std::true_type{}, st);
         if (st >= pool_steps && ((partly >> (st % 32)) & 1)) add_poison(st);
-        product_fence();
+        product_fence(acc);
         static_for<kB>([&](auto KB) DBSA_INLINE { run(kNone, KB, kNone); });
-        product_fence();
+        product_fence(acc);
         read.next_k();
         read.next_v();
         barrier();
@@ -856,7 +862,6 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         for (int i = 0; i < 16; ++i) acc[ob][i] = 0.f;
     }
 
-    product_fence();
     // ---- what the record leaves ----
     const float sum = half_swap_sum(l);
     const int row_head = hk * r + row_index % r;
