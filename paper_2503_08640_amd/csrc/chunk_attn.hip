@@ -32,7 +32,8 @@
 namespace {
 using namespace dbsa_mfma;
 
-constexpr float kRoom = 24.f;  // log2 units a row's scores may exceed its reference maximum by
+constexpr float kRoom = 24.f;    // log2 units a row's scores may exceed its reference maximum by
+constexpr float kShrink = 24.f;  // log2 units that probabilities stay below 1 by where values are huge
 
 struct E4m3 {};  // storage of 8-bit caches; q and o are bf16 then
 
@@ -343,6 +344,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       return (C::kDirect ? col ^ (is_v(i) ? C::v_swizzle(row) : C::k_swizzle(row)) : col) * 16;
     };
     bool again;           // the quick walk does not do for this record (see there)
+    bool beyond;          // its sums of values left fp32
     uint32_t partly;      // bit s % 32: some row does not see some key of step s (kept until its product is done)
     uint32_t lacking;     // the same: some key of step s is not there
     // That of 64 steps, one per lane.  (Scalar loads in every step would be waited for by its first LDS read, which cannot
@@ -524,6 +526,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     // ---- softmax state ----
     floatx16 acc[kO];
     float m, l;                       // l: this lane's keys' share
+    float shrink = 1.f;               // on the probabilities of the careful walk (see there)
     floatx16 s[kB];                   // scores, then (fp32) probabilities
     bf16x8 pf[kF32 ? 1 : kB][2];      // probabilities as operands of the product
 
@@ -589,7 +592,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
           prepare(st, KB);
         } else {
           if ((partly >> (st % 32)) & 1) mask(st, KB);
-          const float bigger = fmaxf(m, row_max(KB));
+          const float top = row_max(KB), bigger = fmaxf(m, shrink == 1.f ? top : ceilf(top));
           const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - bigger);
           m = bigger;
           l *= alpha;
@@ -605,6 +608,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           s[kb][i] = probability(s[kb][i], less);
+          if constexpr (decltype(CAREFUL)::value) s[kb][i] *= shrink;
           sum += s[kb][i];
         }
         l += sum;
@@ -747,13 +751,16 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
     constexpr std::integral_constant<int, kB - 1> k1{};  // the second half of a step, where it has one
     // All steps of the record.  The quick walk never touches the accumulators but in the product (a block that sometimes
     // scales them costs a copy of all of them in every step): a row's reference maximum is that of the first step in which it
-    // sees a key, and later scores may exceed it by kRoom, where probabilities, their sums and the accumulators are still far
-    // inside fp32 and bf16.  Rows whose scores grow further, and values that are not finite under a mask, send the
-    // workgroup through the record once more, carefully: with the running maximum, and the poisoned keys one by one.
+    // sees a key, and later scores may exceed it by kRoom, where probabilities and their sums are still far inside fp32 and
+    // bf16.  Rows whose scores grow further, values that are not finite under a mask, and accumulators that are not finite
+    // send the workgroup through the record once more, carefully: with the running maximum, and the poisoned keys one by
+    // one.  Where it was the accumulators, the probabilities are held 2^kShrink times smaller, so that 2^kShrink of the largest
+    // values add up to no more than one of them; the maximum is then kept to whole numbers, which take kShrink without a
+    // rounding.  (Only there: next to huge values a channel of tiny ones, 2^-102 and below, loses bits by it.)
     auto begin_walk = [&]() DBSA_INLINE {
       m = -INFINITY;
       l = 0.f;
-      again = false;
+      again = beyond = false;
 #pragma unroll
       for (int ob = 0; ob < kO; ++ob)
 #pragma unroll
@@ -809,6 +816,15 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         }
       }
       product_fence(acc);
+      if constexpr (kEs != 1) {  // (sums of bytes stay far inside fp32)
+        float nothing[kO] = {};  // 0, or NaN
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int ob = 0; ob < kO; ++ob) nothing[ob] = fmaf(acc[ob][i], 0.f, nothing[ob]);
+#pragma unroll
+        for (int ob = 0; ob < kO; ++ob) beyond |= nothing[ob] != 0.f;
+      }
     };
     // a wave without rows brings its pieces
     auto walk_idle = [&]() DBSA_INLINE {
@@ -843,15 +859,18 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       else walk_idle();
       // (behind this barrier every wave is done with the stages: the next walk's first steps may land)
       uint32_t* const votes = reinterpret_cast<uint32_t*>(smem + C::kVotesAt);
-      const bool any = __builtin_amdgcn_ballot_w64(again) != 0;
-      if (lane == 0) votes[wave] = any ? 1 : 0;
+      const uint32_t any = __builtin_amdgcn_ballot_w64(again) != 0, far = __builtin_amdgcn_ballot_w64(beyond) != 0;
+      if (lane == 0) votes[wave] = any | 2 * far;
       barrier();
       uint32_t all = 0;
 #pragma unroll
       for (int i = 0; i < kNW; ++i) all |= votes[i];
-      if (__builtin_expect(__builtin_amdgcn_readfirstlane(static_cast<int>(all)) != 0, 0)) {
+      all = __builtin_amdgcn_readfirstlane(static_cast<int>(all));
+      if (__builtin_expect(all != 0, 0)) {
         barrier();
+        if (all & 2) shrink = __builtin_exp2f(-kShrink);
         walk_carefully();
+        if (all & 2) m += kShrink;
       }
     } else {
       m = -INFINITY;
@@ -913,6 +932,8 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
   for (int i = in; i < n; i += kTeam) m = fmaxf(m, base[parts[i] * stride + kD]);
 #pragma unroll
   for (int o = kTeam / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kTeam));
+  // (weights below 1 / n: n states of the largest values add up to no more than one)
+  const float below = __builtin_exp2f(static_cast<float>(__builtin_clz(n) - 32));
   float sum = 0.f;
   floatx4 acc[kPer / 4] = {};
   for (int first = 0; first < n; first += kTeam) {
@@ -920,7 +941,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
     float weight = 0.f;
     if (first + in < n) {
       const floatx2 ml = *reinterpret_cast<const floatx2*>(base + part * stride + kD);
-      weight = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m);
+      weight = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m) * below;
       sum = fmaf(ml[1], weight, sum);
     }
     const int here = min(kTeam, n - first);
@@ -955,7 +976,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
   for (int e = 0; e < kPer / 4; ++e)
     *reinterpret_cast<four*>(out + 4 * e) = four{static_cast<Q>(acc[e][0] * inv * v_scale), static_cast<Q>(acc[e][1] * inv * v_scale),
                                                  static_cast<Q>(acc[e][2] * inv * v_scale), static_cast<Q>(acc[e][3] * inv * v_scale)};
-  if (p.lse && in == 0) p.lse[static_cast<int64_t>(head) * p.n_rows + tok] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  if (p.lse && in == 0) p.lse[static_cast<int64_t>(head) * p.n_rows + tok] = (m + __builtin_amdgcn_logf(sum / below)) * 0.6931471805599453f;
 }
 
 template <typename T, int kD, int kNW, int kBN>

@@ -85,6 +85,19 @@ def test_tiny_key_scales_and_none(batch, d):
     c.check(o, lse)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("batch", sorted(BATCHES))
+def test_values_near_the_top_of_their_type(dtype, d, batch):
+    """The weighted mean of finite values is finite, however many there are, and however far the weights rise along the keys."""
+    for power, by in ((110, 20), (126, 20), (126, 0), (126, 60)):
+        c = case(dtype, d, batch, seed=54)
+        second_half_higher(c, by)
+        for x in (c.v, c.vp):
+            x.copy_((1 + torch.rand(x.shape, generator=torch.Generator("cuda").manual_seed(3), device="cuda")) * 2.0 ** (power - 1))
+        o, lse = run(c)
+        c.check(o, lse)
+
+
 @pytest.mark.parametrize("d", [128, 64])
 @pytest.mark.parametrize("batch", sorted(BATCHES))
 def test_tiny_and_huge_value_scales(batch, d):
