@@ -835,6 +835,16 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         read.next_v();
       }
     };
+    // Rows behind a pool tile's end are copies of one that is there, and 0 * inf makes NaN of an infinity that the rows do see:
+    // the quick walk's accumulators are not finite then, and the careful one takes these rows out.  (Bytes have no infinities.)
+    auto take_copies = [&](int s, unsigned v) DBSA_INLINE {
+      const int ln = lane_here(), len = (recall(s).len & 0xFFFF) - (s % kSteps) * kBN;
+#pragma unroll
+      for (int i = 0; i < C::kLoads; ++i) {
+        const int row = piece_row(i, 64 * wave + ln);
+        if (is_v(i) && row >= len) *reinterpret_cast<lds_piece*>(static_cast<uintptr_t>(v + wave_row(i) * C::kRowBytes + ln * 16)) = uintx4{0, 0, 0, 0};
+      }
+    };
     // step by step, nothing ahead
     auto walk_carefully = [&]() DBSA_INLINE {
       begin_walk();
@@ -842,6 +852,9 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         request(st);
         wait_vmcnt<0>();
         put(st);
+        if constexpr (C::kDirect) {
+          if (st < pool_steps && ((partly >> (st % 32)) & 1)) take_copies(st, read.v);
+        }
         barrier();
         static_for<kB>([&](auto KB) DBSA_INLINE { run(KB, kNone, kNone); });
         softmax(std::true_type{}, st);

@@ -86,6 +86,37 @@ def test_tiny_key_scales_and_none(batch, d):
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("heads", [(8, 2), (128, 128), (256, 128)])
+def test_an_infinite_value_that_is_seen_stays_infinite(dtype, d, heads):
+    """In the last row of segments that end inside a tile, and inside a tile."""
+    c = case(dtype, d, "shared" if heads == (8, 2) else "alone", seed=53, heads=heads, **({} if heads == (8, 2) else {"lens": [300], "own": [300]}))
+    bounds = c.pool[1][c.pool[2]]
+    want, some = c.oracle() if heads == (8, 2) else None, [0, 1]
+    r = c.hq // c.hkv
+    sign, channels = [1, -1, 1], [5, d - 1, 0]
+    rows = [c.pool[0] - 1, int(bounds[c.sels[0][0] + 1]) - 1, int(bounds[c.sels[0][1]]) + 10]
+    sees = [np.ones(int(c.cu[-1]), bool)] + [np.concatenate([np.full(n, c.sels[0][i] in s) for n, s in zip(c.lens, c.sels)]) for i in (0, 1)]
+    near = c.v.clone()
+    for row, s, ch in zip(rows, sign, channels):
+        c.v[row, :, ch] = s * torch.inf
+    o = run(c)[0]
+    c.v = near
+    if want is None:
+        heads = [h * r + i for h in some for i in range(r)]
+        o = o[:, heads]
+        c.q, c.k, c.v, c.kp, c.vp = c.q[:, heads], c.k[:, some], c.v[:, some], c.kp[:, :, some], c.vp[:, :, some]
+        want = c.oracle()
+    got = o.clone()
+    for s, ch, see in zip(sign, channels, sees):
+        see = torch.from_numpy(see).cuda()
+        assert see.any() and (got[see][:, :, ch] == s * torch.inf).all()
+        place = torch.zeros_like(got, dtype=torch.bool)
+        place[:, :, ch] = see[:, None]
+        got = torch.where(place, torch.from_numpy(want["o"]).cuda().to(got.dtype), got)
+    c.check(got, want=want)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
 @pytest.mark.parametrize("batch", sorted(BATCHES))
 def test_values_near_the_top_of_their_type(dtype, d, batch):
     """The weighted mean of finite values is finite, however many there are, and however far the weights rise along the keys."""
