@@ -153,7 +153,8 @@ int dbsa_layout_build_append(const dbsa_pool_desc* pool, int32_t first_group, in
  *                balance of the launch goes by it; the keys attended are those that self_len counts at the call, so that
  *                one layout serves all layers, and later steps that bring as many new tokens.
  * Such a layout goes with dbsa_chunk_attn, dbsa_chunk_attn_kv8, dbsa_workspace_bytes (0 for another n_q_heads) and
- * dbsa_layout_export_chunk; every other call takes it for a layout of the wrong stage.
+ * dbsa_layout_export_chunk.  It has no Q tiles: dbsa_layout_export and dbsa_layout_export_order give empty lists.  Every other
+ * call takes it for a layout of the wrong stage.
  * Errors as dbsa_layout_build; UNSUPPORTED unless n_q_heads is a multiple of n_kv_heads, at most 32 times as many.
  */
 int dbsa_layout_build_chunk(const dbsa_pool_desc* pool, const dbsa_select_desc* sel, int32_t n_q_heads, int32_t n_kv_heads,

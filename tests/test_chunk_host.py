@@ -226,3 +226,13 @@ def test_refusals_of_the_8bit_calls(which):
 def test_workgroups_have_four_or_eight_waves(seed):
     p, lens, sels, hq, hkv, own = random_case(seed)
     assert build(p, lens, sels, hq, hkv, own).export_chunk(int(sum(lens)))["rows"] in (128, 256)
+
+
+def test_a_chunk_layout_has_no_lists_of_the_other_stages():
+    chunk = build(pool(4, [10, 20], 1), [2], [[0]], 2, 2)
+    tab, ptr, ent = chunk.export()
+    assert tab.shape == (0, 4) and ptr.tolist() == [0] and ent.shape == (0, 2) and chunk.export_order().shape == (0,)
+    for export in (lambda: chunk.export_decode(1), lambda: chunk.export_decode_groups(2, 1), lambda: chunk.export_positions(1),
+                   chunk.export_matrix_records, lambda: chunk.export_matrix_plan(1), lambda: chunk.export_schedule(4),
+                   lambda: chunk.export_cut_schedule(4, 8)):
+        refused(B.DBSA_ERR_INVALID_ARG, export)
