@@ -9,7 +9,8 @@
 // holds 16 keys of ONE row per block of 32 keys: maxima and sums need one exchange between the two half-waves and no LDS,
 // and the probabilities are in place as the operand of O^T = V^T P^T.  bf16 products (8-bit caches are widened as they are
 // staged, exactly: every e4m3 value is a bf16 value), fp32 products for fp32 tensors; the only rounding to fewer bits besides
-// the output's is that of the probabilities to bf16, relative 2^-9 each and unbiased, while l sums them unrounded.
+// the output's is that of the probabilities to bf16, half a step (2^-8) at most and unbiased, while l sums them unrounded.  (Dividing
+// by the sum of the rounded ones changed nothing, 2.332e-3 to 2.330e-3 of the result's norm, for 3 % of the time.)
 //
 // Work.  Workers and their records come from the host's plan (chunk_plan.cpp).  A record is a block of rows and a run of
 // 64-key tiles: pool tiles from the lists, then a part of the question's own keys, whose number the device knows
@@ -17,10 +18,12 @@
 //
 // What bounds it.  Many rows: a tile of 256 rows and 64 keys of 128 channels is 2048 cycles of the matrix pipes, 2300 of LDS
 // reads and 2000 of vector work (exponentials above all) on a compute unit; one barrier per step keeps the two waves of a
-// SIMD side by side, and what does not overlap brings a tile to 1.9 us.  2048 tokens behind 90k and 30k own keys: 1860 us, 1080
+// SIMD side by side, and what does not overlap brings a tile to 2.0 us.  2048 tokens behind 90k and 30k own keys: 1860 us, 1080
 // TFLOP/s (the library's product of 8192^3: 1212).  Few rows: memory, and the start of a record, a chain of loads (record,
-// token, row of Q, list, first rows) of 3 us.  16 questions of 8 tokens over 30 % of 90k: 118 us, 3.4 TB/s of unique bytes; one
-// token over 1200 keys: 17 us, 6 of them the merge.  Two row blocks per wave with one wave to a SIMD, which halves the LDS
+// token, row of Q, list, first rows) of 3 us; a workgroup's waves without rows only fetch.  16 questions of 8 tokens over 30 % of
+// 90k: 120 us, 3.3 TB/s of unique bytes; one token over 1200 keys: 17 us, 6 of them the merge.  8-bit caches of 64 channels:
+// each wave fetches K or V alone, the choice ends up as pointers in scratch memory, and every request waits for the rows in
+// flight (172 us for 6 prompts of 16 heads, 123 for the same in bf16).  Two row blocks per wave with one wave to a SIMD, which halves the LDS
 // reads, were slower (2203 us for the 2048 tokens, 2028 then): nothing fills the waits of a lone wave.
 #include <atomic>
 #include <cstdint>
@@ -616,7 +619,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
       });
       static_for<kB>([&](auto KB) DBSA_INLINE { pack(KB); });
     };
-    // the keys that take_poison kept out of the product
+    // the keys that clean() kept out of the product
     auto add_poison = [&](int st) DBSA_INLINE {
       uint64_t keys = 0;
       for (int i = 0; i < kNW; ++i) keys |= poison[(read.v - start.v) / C::kTileBytes * kNW + i];
@@ -785,7 +788,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void chunk_attn_kernel(ChunkParams p) 
         // Half steps of 32 keys in three stages, one apart: while the probabilities of a half are made, the scores of the next
         // half and the product of the one before it run on the matrix pipe; no instruction waits for one of its own half.
         // (One barrier per step keeps the two waves of a SIMD side by side, so that each has to mix its matrix and vector
-        // instructions itself: with the two kinds one after the other a step of eight waves took 2.2 us, so 1.4.)
+        // instructions itself.)
         for (int n = -C::kFlight; n <= 0; ++n) advance(n);
         run(k0, kNone, kNone);
         prepare(0, k0);

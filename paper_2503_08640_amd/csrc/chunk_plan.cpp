@@ -137,10 +137,12 @@ int dbsa_build_chunk_lists(const dbsa_pool_desc* pool, const dbsa_select_desc* s
   };
   // The shape whose longest worker is done first.  Two workgroups of four waves share a compute unit's bandwidths and take about
   // 3/2 of the time of one of eight for a tile, but come in twice the number and leave fewer rows empty.  12 questions of 229
-  // tokens: 1234 us with 256 rows, 1520 with 128; 122 of 14 behind 13k own keys: 891 and 658; 16 of 8 over 90k: 120 and 126.  46
-  // batches drawn from one token to 1668 came to 2 % above the better shape on average by this ratio, 5.5 % by a ratio of 1,
-  // 7.6 % by 2.  (Workgroups of one or two waves fetch and widen too slowly: one token over 2k 23.5 us, 18.5 with eight
-  // waves; the 16 questions 321 and 173.)
+  // tokens: 1234 us with 256 rows, 1520 with 128; 122 of 14 behind 13k own keys: 891 and 658; 16 of 8 over 90k: 120 and 126.  The
+  // ratio is one for all calls, because a layout knows neither the type nor the channels: over 72 batches drawn from one token to
+  // 1668 it came to 3.6 % above the better shape on average (eight waves always: 7.1 %, four always: 5.7 %).  By type: bf16
+  // 1.6 % with 128 channels and 8 % with 64, 8 bits 2 %, where eight waves always would be as good, and fp32 9 %, where
+  // four always would be better.  (Workgroups of one or two waves fetch and widen too slowly: one token over 2k 23.5 us, 18.5 with
+  // eight waves; the 16 questions 321 and 173.)
   const ChunkShape shapes[2] = {{256, 1, 2}, {128, 2, 3}};
   ChunkShape shape = shapes[0];
   int64_t tiles = 0, workers = 0;

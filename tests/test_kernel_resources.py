@@ -38,3 +38,14 @@ def test_no_pipelined_kernel_keeps_registers_in_scratch(tmp_path):
     spilled = {name: (f[".vgpr_spill_count"], f[".private_segment_fixed_size"]) for name, f in found
                if f[".vgpr_spill_count"] != "0" or f[".private_segment_fixed_size"] != "0"}
     assert not spilled
+
+
+@pytest.mark.skipif(not (os.path.exists(READELF) and os.path.exists(build.LIB_PATH)), reason="needs the built library and llvm-readelf")
+def test_chunk_kernels_with_scratch_are_the_known_ones(tmp_path):
+    """Twelve instances of the chunk attention.  Both of 8-bit caches with 64 channels keep pointers in scratch that the step loop
+    reads (72 bytes), two with 128 channels and eight waves a few registers outside the quick walk's loop; no other, and no more."""
+    found = {re.search(r"chunk_attn_kernelI(DF16b|f|NS_4E4m3E)Li(\d+)ELi(\d)E", name).groups(): int(f[".private_segment_fixed_size"])
+             for name, f in kernels(tmp_path) if "chunk_attn_kernel" in name}
+    assert len(found) == 12
+    room = {("NS_4E4m3E", "64", "4"): 72, ("NS_4E4m3E", "64", "8"): 72, ("DF16b", "128", "8"): 24, ("NS_4E4m3E", "128", "8"): 16}
+    assert {name: n for name, n in found.items() if n > room.get(name, 0)} == {}
