@@ -23,7 +23,7 @@
 // token, row of Q, list, first rows) of 3 us; a workgroup's waves without rows only fetch.  16 questions of 8 tokens over 30 % of
 // 90k: 120 us, 3.3 TB/s of unique bytes; one token over 1200 keys: 17 us, 6 of them the merge.  8-bit caches of 64 channels:
 // each wave fetches K or V alone, the choice ends up as pointers in scratch memory, and every request waits for the rows in
-// flight (172 us for 6 prompts of 16 heads, 123 for the same in bf16).  Two row blocks per wave with one wave to a SIMD, which halves the LDS
+// flight (178 us for 6 prompts of 16 heads, 113 for the same in bf16).  Two row blocks per wave with one wave to a SIMD, which halves the LDS
 // reads, were slower (2203 us for the 2048 tokens, 2028 then): nothing fills the waits of a lone wave.
 #include <atomic>
 #include <cstdint>
