@@ -41,7 +41,7 @@ enum {
   DBSA_ERR_HIP = -6            /* a HIP runtime call failed; hipGetLastError() holds the cause */
 };
 
-enum { DBSA_BF16 = 0, DBSA_F32 = 1 };
+enum { DBSA_BF16 = 0, DBSA_F32 = 1, DBSA_E4M3 = 2 /* bytes of 8-bit caches: dbsa_pages_copy alone */ };
 
 /* dbsa_layout_build flag: build the host lists only and touch no GPU.  Such a
  * layout can be exported and destroyed but not passed to an attention call. */
@@ -622,6 +622,131 @@ int dbsa_kv8_write(dbsa_tensor k, dbsa_tensor v, int32_t n_tokens, const int32_t
 int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, const int32_t* rows, int64_t first_row,
                   int32_t n_tokens, const float* k_scale, const float* v_scale, dbsa_tensor k, dbsa_tensor v,
                   int32_t n_kv_heads, int32_t head_dim, int32_t dtype, void* stream);
+
+/*
+ * ---- which of several proposed tokens stay ------------------------------------------------------
+ * A chunk of T_u tokens of question u goes through dbsa_chunk_attn and the model around it: its first token is the last one
+ * that is settled, the T_u - 1 behind it were proposed (by a smaller model, or looked up in the prompt).  Row a of the
+ * target's scores then checks token a + 1.  With p_a and q_a the distributions of the target and of what proposed,
+ *   token a + 1 stands   iff all before it do and uniform_a * q_a(token) < p_a(token);
+ *   behind n that stand one more token is drawn, with weights w = max(p_n - q_n, 0) if proposal n was refused and
+ *   w = p_n if there was none: the first i with  sum_{j <= i} w_j > uniform_last * sum_j w_j.
+ * What comes out is distributed as if the target had drawn every token.  T_u = 1 draws a token without proposals.
+ *
+ *   target     : device [n_tokens, vocab] of dtype, rows target_stride elements apart (any alignment), packed by cu_qlens.
+ *   draft      : rows of the same form and dtype that the proposals were drawn from: that of proposal a of question u begins at
+ *                element u * stride_query + a * stride_step, a < n_steps.  NULL, or ptr NULL: the proposals were not drawn at
+ *                random (q = 1 at the proposal).
+ *   tokens     : device int32 [n_tokens], the chunk's tokens.  One that is no token of the vocabulary (-1), or has no row
+ *                in draft, ends the proposals: nothing is taken from p_n there.
+ *   cu_qlens   : device int32 [n_queries + 1], ascending from 0, each at most n_tokens; a question may have no rows.
+ *   form       : DBSA_LOGITS: p = softmax(row / T), T = temperature[u]; a value that is no number counts as -infinity, values of
+ *                +infinity share everything.  T that is not above 0: p is 1 at the largest value, the lowest index of equal
+ *                ones, and draft is not read.
+ *                DBSA_PROBABILITIES: rows hold p and q themselves (temperature NULL); values that are negative, infinite or no
+ *                number count as 0, and a row need not sum to 1.
+ *   temperature: device float [n_queries], or NULL for 1.
+ *   uniform    : device float [n_tokens] in [0, 1): that of row a decides on proposal a, that of the question's last row
+ *                draws.  (Where it is outside, the draw takes the last token with a weight.)
+ *   out_tokens : device int32 [n_tokens]: the tokens that stand, the drawn one, then -1, from the question's first row on; rows
+ *                of no question are left alone.  A row without any probability draws -1; where w is 0 throughout (p nowhere above
+ *                q) the draw is from p_n.  Not the same array as tokens.
+ *   accepted   : device int32 [n_queries]: how many stand.
+ *   logp       : optional device float [n_tokens]: log p of each token of out_tokens (where T is not above 0: of T = 1), 0 in
+ *                rows without one.
+ *   self_len, new_len : optional device int32 [n_queries], both or none: the own keys at the chunk's attention call, and those
+ *                of the tokens that stand: self_len - (T_u - 1 - accepted).  May be the same array.
+ *   workspace  : device memory of >= dbsa_draft_verify_workspace_bytes() bytes, 16-byte aligned; calls that overlap need one
+ *                each.  Its contents need not be set.
+ * Distributions, sums and prefixes are held in 64 bits.  The call only launches kernels and may be recorded into a HIP graph;
+ * all device arrays may change between replays.
+ * Errors: INVALID_ARG; UNSUPPORTED (other dtypes or forms, more than 2^30 words, rows or questions whose pieces of 4096 values
+ * number more than 2^23); WORKSPACE; HIP.
+ */
+enum { DBSA_LOGITS = 0, DBSA_PROBABILITIES = 1 };
+typedef struct {
+  const void* ptr;
+  int64_t stride_query, stride_step; /* elements */
+  int32_t n_steps;
+} dbsa_draft;
+size_t dbsa_draft_verify_workspace_bytes(int32_t n_tokens, int32_t n_queries, int32_t vocab);
+int dbsa_draft_verify(const void* target, int64_t target_stride, const dbsa_draft* draft, const int32_t* tokens,
+                      const int32_t* cu_qlens, int32_t n_tokens, int32_t n_queries, int32_t vocab, int32_t dtype, int32_t form,
+                      const float* temperature, const float* uniform, int32_t* out_tokens, int32_t* accepted, float* logp,
+                      const int32_t* self_len, int32_t* new_len, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- the pages that caches lie in -----------------------------------------------------------------
+ * The books of an arena of pages, kept by the caller on the device and changed in place by the calls below.  An entry of the
+ * table names a page or, outside [0, n_pages), none; refs counts the entries (of this table and of others) that name a
+ * page, and a page is free while its count is not above 0.  Row u of the table names the pages of question u in order, those
+ * of its first self_len[u] tokens and perhaps some behind, as dbsa_pages describes them to dbsa_chunk_attn.
+ * The calls only launch kernels and may be recorded into a HIP graph; calls on one set of books have to follow one
+ * another.  Their results do not depend on what runs beside them or on the order of atomics.
+ */
+typedef struct {
+  int32_t* table;      /* device [n_queries][table_stride]                                   */
+  int32_t* refs;       /* device [n_pages]                                                   */
+  int32_t* self_len;   /* device [n_queries], counted from 0 to what a row of the table holds */
+  int32_t n_queries;   /* at most 8192                                                       */
+  int32_t table_stride;/* at most 2^24                                                       */
+  int32_t page_tokens; /* a power of two, at least 16                                        */
+  int32_t n_pages;
+} dbsa_page_book;
+
+/*
+ * Question u becomes a copy of question source[u] as it was before the call, sharing its pages: answers that branch, a beam that
+ * is reordered.  Row u then names the pages of the first self_len[source[u]] tokens and none behind them, self_len follows,
+ * and so do the counts.  source[u] == u or outside [0, n_queries): question u stays as it is.  source: device int32 [n_queries].
+ * A shared last page is not to be written to before dbsa_pages_reserve has replaced it.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+int dbsa_pages_fork(const dbsa_page_book* book, const int32_t* source, void* stream);
+
+/*
+ * Room for add[u] (device int32) more tokens of each question, which self_len then counts.  In the order of the questions:
+ *   - a last page that is partly used and that, after the questions before, more than one entry names is replaced by a free
+ *     one, and (old page, new page, rows in use) is added to the copies: the caller passes them to dbsa_pages_copy for its caches
+ *     before it writes the new tokens' keys;
+ *   - entries the new tokens reach into that name no page get free ones.
+ * Free pages are taken from the lowest up.  From the first question on that they do not suffice for, questions are left as they
+ * are.  A question whose row of the table is too short, or whose partly used last page is not there, is left as it is.
+ *   got      : device int32 [n_queries], written: add[u], or 0 for a question that is left as it is.
+ *   copies   : device int32 [n_queries][3]; n_copies: device int32, how many were written (the rest is left alone).
+ *   workspace: device memory of >= 4 * n_pages bytes, 4-byte aligned.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ */
+int dbsa_pages_reserve(const dbsa_page_book* book, const int32_t* add, int32_t* got, int32_t* copies, int32_t* n_copies,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gives back the pages behind the first self_len[u] tokens of each question (0: all of them, the question has ended): their
+ * entries become -1, their counts go down.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+int dbsa_pages_trim(const dbsa_page_book* book, void* stream);
+
+/*
+ * Puts the pages in use to the front of the arena.  With L of them, the k-th page in use at L or behind becomes the k-th
+ * free page before L; counts and table entries follow.  The caller passes the copies to dbsa_pages_copy for its caches.
+ * book->self_len is not looked at (may be NULL); n_queries may be 0 (table NULL): other tables are renamed by new_place.
+ *   copies    : device int32 [max(1, n_pages / 2)][3], as those of dbsa_pages_reserve, with rows = page_tokens.
+ *   counts    : device int32 [2], written: copies, L.
+ *   new_place : device int32 [n_pages], written: where each page is now, -1 for a free one.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+int dbsa_pages_compact(const dbsa_page_book* book, int32_t* copies, int32_t* counts, int32_t* new_place, void* stream);
+
+/*
+ * Carries out copies: rows 0 .. rows - 1 of page `from` become those of page `to`, keys and values, in every layer.  Pages written
+ * to are not read by the same call.  A copy that names a page that is not there is left out.
+ *   pages      : k, v, stride_page, page_tokens and n_pages count; table is not looked at.
+ *   n_layers, stride_layer: layer l lies l * stride_layer elements behind the first (1 and 0: one layer).
+ *   copies, n_copies: as written by dbsa_pages_reserve or dbsa_pages_compact; at most max_copies are carried out.
+ *   dtype      : DBSA_BF16, DBSA_F32, or DBSA_E4M3 (strides multiples of 16); head_dim in {64, 128}.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+int dbsa_pages_copy(const dbsa_pages* pages, int32_t n_layers, int64_t stride_layer, const int32_t* copies, const int32_t* n_copies,
+                    int32_t max_copies, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, void* stream);
 
 #ifdef __cplusplus
 }

@@ -37,6 +37,9 @@ DBSA_ERR_WORKSPACE = -5
 DBSA_ERR_HIP = -6
 DBSA_BF16 = 0
 DBSA_F32 = 1
+DBSA_E4M3 = 2
+DBSA_LOGITS = 0
+DBSA_PROBABILITIES = 1
 DBSA_LAYOUT_HOST_ONLY = 1
 
 EXPORTED_SYMBOLS = (
@@ -47,7 +50,8 @@ EXPORTED_SYMBOLS = (
     "dbsa_layout_export_matrix_plan",
     "dbsa_layout_export_schedule", "dbsa_layout_export_cut_schedule",
     "dbsa_layout_build_chunk", "dbsa_layout_export_chunk", "dbsa_chunk_attn", "dbsa_chunk_attn_kv8", "dbsa_kv8_scales",
-    "dbsa_kv8_write", "dbsa_kv8_read",
+    "dbsa_kv8_write", "dbsa_kv8_read", "dbsa_draft_verify_workspace_bytes", "dbsa_draft_verify", "dbsa_pages_fork",
+    "dbsa_pages_reserve", "dbsa_pages_trim", "dbsa_pages_compact", "dbsa_pages_copy",
 )
 DBSA_STATIC_SCRATCH_BYTES = 32 << 20
 
@@ -75,6 +79,15 @@ class Tensor(C.Structure):
 class Pages(C.Structure):
     _fields_ = [("k", Tensor), ("v", Tensor), ("stride_page", C.c_int64), ("table", C.c_void_p), ("table_stride", C.c_int32),
                 ("page_tokens", C.c_int32), ("n_pages", C.c_int32)]
+
+
+class Draft(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("stride_query", C.c_int64), ("stride_step", C.c_int64), ("n_steps", C.c_int32)]
+
+
+class PageBook(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("refs", C.c_void_p), ("self_len", C.c_void_p), ("n_queries", C.c_int32),
+                ("table_stride", C.c_int32), ("page_tokens", C.c_int32), ("n_pages", C.c_int32)]
 
 
 _lib = None
@@ -182,6 +195,21 @@ def lib() -> C.CDLL:
     L.dbsa_kv8_read.restype = C.c_int
     L.dbsa_kv8_read.argtypes = [Tensor, Tensor, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, Tensor,
                                 Tensor] + [C.c_int32] * 3 + [C.c_void_p]
+    L.dbsa_draft_verify_workspace_bytes.restype = C.c_size_t
+    L.dbsa_draft_verify_workspace_bytes.argtypes = [C.c_int32] * 3
+    ptr = C.c_void_p
+    L.dbsa_draft_verify.restype = C.c_int
+    L.dbsa_draft_verify.argtypes = [ptr, C.c_int64, C.POINTER(Draft), ptr, ptr] + [C.c_int32] * 5 + [ptr] * 8 + [C.c_size_t, ptr]
+    L.dbsa_pages_fork.restype = C.c_int
+    L.dbsa_pages_fork.argtypes = [C.POINTER(PageBook), ptr, ptr]
+    L.dbsa_pages_reserve.restype = C.c_int
+    L.dbsa_pages_reserve.argtypes = [C.POINTER(PageBook), ptr, ptr, ptr, ptr, ptr, C.c_size_t, ptr]
+    L.dbsa_pages_trim.restype = C.c_int
+    L.dbsa_pages_trim.argtypes = [C.POINTER(PageBook), ptr]
+    L.dbsa_pages_compact.restype = C.c_int
+    L.dbsa_pages_compact.argtypes = [C.POINTER(PageBook), ptr, ptr, ptr, ptr]
+    L.dbsa_pages_copy.restype = C.c_int
+    L.dbsa_pages_copy.argtypes = [C.POINTER(Pages), C.c_int32, C.c_int64, ptr, ptr] + [C.c_int32] * 4 + [ptr]
     _lib = L
     return L
 
@@ -749,3 +777,122 @@ def dbsa_kv8_read(k8, v8, k_scale, v_scale, rows=None, first_row: int = 0, n_tok
                              _tensor(k), _tensor(v), heads, dim, _dtype_code(k), stream)
     _check(rc, "dbsa_kv8_read")
     return k, v
+
+
+# ---------------------------------------------------------------------------
+# proposed tokens, pages of the caches
+# ---------------------------------------------------------------------------
+
+def _ints(t, n: int) -> bool:
+    return t.dim() == 1 and t.shape[0] == n and _int32(t)
+
+
+def dbsa_draft_verify_workspace_bytes(n_tokens: int, n_queries: int, vocab: int) -> int:
+    return int(lib().dbsa_draft_verify_workspace_bytes(int(n_tokens), int(n_queries), int(vocab)))
+
+
+def dbsa_draft_verify(target, tokens, cu_qlens, uniform, draft=None, temperature=None, probs: bool = False, out=None, accepted=None,
+                      logp=None, self_len=None, new_len=None, workspace=None):
+    """-> (tokens int32 [sum T], accepted int32 [B]): which of the tokens [sum T] of a chunk, packed by cu_qlens int32 [B + 1] on
+    the device, stand before the target's scores [sum T, V], and the one drawn behind them, from uniform float32 [sum T] in
+    [0, 1).  ``draft`` [B, steps, V] holds the scores the proposals were drawn from (None: they were not drawn).  Scores are logits
+    at ``temperature`` float32 [B] (None: 1; 0: greedy), or probabilities if ``probs``.  ``logp`` float32 [sum T] receives the log
+    probabilities, ``new_len`` int32 [B] the own keys of ``self_len`` that stay."""
+    import torch
+    shape, n, b = target.shape, tokens.shape[0], cu_qlens.shape[0] - 1
+    assert len(shape) == 2 and shape[0] == n and target.stride(1) == 1, "expected scores [sum T, V], V contiguous"
+    assert b >= 1 and _ints(tokens, n) and _ints(cu_qlens, b + 1), "expected contiguous int32 tokens [sum T] and cu_qlens [B + 1]"
+    for t, m in ((uniform, n), (temperature, b), (logp, n)):
+        assert t is None or (t.dtype == torch.float32 and t.shape == (m,) and t.is_contiguous()), "expected contiguous float32 numbers"
+    out = torch.empty_like(tokens) if out is None else out
+    accepted = torch.empty_like(cu_qlens[1:]) if accepted is None else accepted
+    assert _ints(out, n) and _ints(accepted, b)
+    assert (self_len is None) == (new_len is None) and (self_len is None or (_ints(self_len, b) and _ints(new_len, b)))
+    d = None
+    if draft is not None and draft.shape[1] > 0:
+        s = draft.stride()
+        assert draft.dtype == target.dtype and draft.shape[0] == b and draft.shape[2] == shape[1] and s[2] == 1, "expected draft scores [B, steps, V]"
+        d = C.byref(Draft(draft.data_ptr(), s[0], s[1], draft.shape[1]))
+    if workspace is None:
+        workspace = torch.empty(max(16, dbsa_draft_verify_workspace_bytes(n, b, shape[1])), dtype=torch.uint8, device=target.device)
+    stream = _here(target, tokens, cu_qlens, uniform, draft, temperature, out, accepted, logp, self_len, new_len, workspace)
+    rc = lib().dbsa_draft_verify(target.data_ptr(), target.stride(0), d, tokens.data_ptr(), cu_qlens.data_ptr(), n, b, shape[1],
+                                 _dtype_code(target), DBSA_PROBABILITIES if probs else DBSA_LOGITS, _at(temperature), uniform.data_ptr(),
+                                 out.data_ptr(), accepted.data_ptr(), _at(logp), _at(self_len), _at(new_len), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), stream)
+    _check(rc, "dbsa_draft_verify")
+    return out, accepted
+
+
+def _book(page_table, refs, self_len, page_tokens: int):
+    """The books of an arena: page_table int32 [B, pages of a question], refs int32 [pages], self_len int32 [B]."""
+    b, columns = page_table.shape
+    assert _int32(page_table) and refs.dim() == 1 and _int32(refs), "expected a contiguous int32 page table and counts"
+    assert self_len is None or _ints(self_len, b), "expected contiguous int32 lengths [B]"
+    return C.byref(PageBook(page_table.data_ptr(), refs.data_ptr(), _at(self_len), b, columns, int(page_tokens), refs.shape[0]))
+
+
+def dbsa_pages_fork(page_table, refs, self_len, source, page_tokens: int) -> None:
+    """Question u becomes a copy of question source[u] (int32 [B] on the device) that shares its pages; in place."""
+    book = _book(page_table, refs, self_len, page_tokens)
+    assert _ints(source, page_table.shape[0]), "expected contiguous int32 sources [B]"
+    stream = _here(page_table, refs, self_len, source)
+    _check(lib().dbsa_pages_fork(book, source.data_ptr(), stream), "dbsa_pages_fork")
+
+
+def dbsa_pages_reserve(page_table, refs, self_len, add, page_tokens: int, got=None, copies=None, n_copies=None, workspace=None):
+    """-> (got int32 [B], copies int32 [B, 3], n_copies int32 [1]): room for add int32 [B] more tokens of each question, counted by
+    self_len from then on; the copies are for dbsa_pages_copy.  The books change in place."""
+    import torch
+    book, b = _book(page_table, refs, self_len, page_tokens), page_table.shape[0]
+    got = torch.empty_like(add) if got is None else got
+    copies = torch.empty((b, 3), dtype=torch.int32, device=add.device) if copies is None else copies
+    n_copies = torch.empty(1, dtype=torch.int32, device=add.device) if n_copies is None else n_copies
+    workspace = torch.empty_like(refs) if workspace is None else workspace
+    assert _ints(add, b) and _ints(got, b) and _ints(n_copies, 1) and copies.shape == (b, 3) and _int32(copies)
+    stream = _here(page_table, refs, self_len, add, got, copies, n_copies, workspace)
+    rc = lib().dbsa_pages_reserve(book, add.data_ptr(), got.data_ptr(), copies.data_ptr(), n_copies.data_ptr(), workspace.data_ptr(),
+                                  workspace.numel() * workspace.element_size(), stream)
+    _check(rc, "dbsa_pages_reserve")
+    return got, copies, n_copies
+
+
+def dbsa_pages_trim(page_table, refs, self_len, page_tokens: int) -> None:
+    """Gives back the pages behind the first self_len[u] tokens of each question; in place."""
+    book = _book(page_table, refs, self_len, page_tokens)
+    stream = _here(page_table, refs, self_len)
+    _check(lib().dbsa_pages_trim(book, stream), "dbsa_pages_trim")
+
+
+def dbsa_pages_compact(refs, page_table, page_tokens: int, copies=None, counts=None, new_place=None):
+    """-> (copies int32 [n, 3], counts int32 [2] = (copies, pages in use), new_place int32 [pages]): the pages in use move to the front of
+    the arena; refs and page_table (None: the caller renames its tables) change in place, the caches by dbsa_pages_copy."""
+    import torch
+    n = refs.shape[0]
+    if page_table is None:
+        assert refs.dim() == 1 and _int32(refs), "expected contiguous int32 counts"
+        book = C.byref(PageBook(None, refs.data_ptr(), None, 0, 0, int(page_tokens), n))
+    else:
+        book = _book(page_table, refs, None, page_tokens)
+    copies = torch.empty((max(1, n // 2), 3), dtype=torch.int32, device=refs.device) if copies is None else copies
+    counts = torch.empty(2, dtype=torch.int32, device=refs.device) if counts is None else counts
+    new_place = torch.empty_like(refs) if new_place is None else new_place
+    assert copies.shape == (max(1, n // 2), 3) and _int32(copies) and _ints(counts, 2) and _ints(new_place, n)
+    stream = _here(refs, page_table, copies, counts, new_place)
+    _check(lib().dbsa_pages_compact(book, copies.data_ptr(), counts.data_ptr(), new_place.data_ptr(), stream), "dbsa_pages_compact")
+    return copies, counts, new_place
+
+
+def dbsa_pages_copy(k_pages, v_pages, copies, n_copies) -> None:
+    """Carries out the copies [n, 3] = (from, to, rows), of which n_copies[0] count, in k_pages and v_pages [pages, page tokens, Hkv,
+    D], or [layers, pages, page tokens, Hkv, D]; bf16, float32 or 8 bits."""
+    s, shape = k_pages.stride(), k_pages.shape
+    assert len(shape) in (4, 5) and s[-1] == 1 and v_pages.stride() == s and v_pages.shape == shape and v_pages.dtype == k_pages.dtype
+    assert copies.dim() == 2 and copies.shape[1] == 3 and _int32(copies) and _int32(n_copies) and n_copies.numel() >= 1
+    layers, apart = (shape[0], s[0]) if len(shape) == 5 else (1, 0)
+    pages = Pages(Tensor(k_pages.data_ptr(), s[-3], s[-2]), Tensor(v_pages.data_ptr(), s[-3], s[-2]), s[-4], None, 0, shape[-3], shape[-4])
+    dtype = DBSA_E4M3 if k_pages.element_size() == 1 else _dtype_code(k_pages)
+    stream = _here(k_pages, v_pages, copies, n_copies)
+    rc = lib().dbsa_pages_copy(C.byref(pages), layers, apart, copies.data_ptr(), n_copies.data_ptr(), copies.shape[0], shape[-2], shape[-1],
+                               dtype, stream)
+    _check(rc, "dbsa_pages_copy")

@@ -1318,6 +1318,138 @@ int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, co
   return launch_kv8_read(p, dtype == DBSA_BF16, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
 }
 
+size_t dbsa_draft_verify_workspace_bytes(int32_t n_tokens, int32_t n_queries, int32_t vocab) {
+  if (n_tokens < 0 || n_queries < 1 || vocab < 1 || vocab > 1 << 30) return 0;
+  return verify_workspace_bytes(n_tokens, n_queries, vocab);
+}
+
+int dbsa_draft_verify(const void* target, int64_t target_stride, const dbsa_draft* draft, const int32_t* tokens,
+                      const int32_t* cu_qlens, int32_t n_tokens, int32_t n_queries, int32_t vocab, int32_t dtype, int32_t form,
+                      const float* temperature, const float* uniform, int32_t* out_tokens, int32_t* accepted, float* logp,
+                      const int32_t* self_len, int32_t* new_len, void* workspace, size_t workspace_bytes, void* stream) {
+  if (dtype != DBSA_BF16 && dtype != DBSA_F32) return DBSA_ERR_UNSUPPORTED;
+  if (form != DBSA_LOGITS && form != DBSA_PROBABILITIES) return DBSA_ERR_UNSUPPORTED;
+  if (!target || !tokens || !cu_qlens || !uniform || !out_tokens || !accepted || n_tokens < 0 || n_queries < 1 || vocab < 1)
+    return DBSA_ERR_INVALID_ARG;
+  if (out_tokens == tokens || !self_len != !new_len) return DBSA_ERR_INVALID_ARG;
+  if (form == DBSA_PROBABILITIES && temperature) return DBSA_ERR_INVALID_ARG;
+  const uintptr_t size = dtype == DBSA_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(target) % size != 0 || target_stride < 0) return DBSA_ERR_INVALID_ARG;
+  const bool drawn = draft && draft->ptr;
+  if (drawn && (reinterpret_cast<uintptr_t>(draft->ptr) % size != 0 || draft->stride_query < 0 || draft->stride_step < 0 || draft->n_steps < 1))
+    return DBSA_ERR_INVALID_ARG;
+  const int64_t pieces = (int64_t{vocab} + 8 + 4095) / 4096;  // (a grid counts its threads in 32 bits)
+  if (vocab > 1 << 30 || std::max<int64_t>(n_tokens, n_queries) * pieces > 1 << 23) return DBSA_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < verify_workspace_bytes(n_tokens, n_queries, vocab) || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
+    return DBSA_ERR_WORKSPACE;
+  VerifyParams p{};
+  p.target = target;
+  p.target_stride = target_stride;
+  if (drawn) {
+    p.draft = draft->ptr;
+    p.draft_query = draft->stride_query;
+    p.draft_step = draft->stride_step;
+    p.draft_steps = draft->n_steps;
+  }
+  p.tokens = tokens;
+  p.cu = cu_qlens;
+  p.uniform = uniform;
+  p.heat = temperature;
+  p.self_len = self_len;
+  p.out = out_tokens;
+  p.accepted = accepted;
+  p.new_len = new_len;
+  p.logp = logp;
+  p.n_queries = n_queries;
+  p.n_tokens = n_tokens;
+  p.vocab = vocab;
+  p.workspace = workspace;
+  return launch_verify(p, dtype == DBSA_BF16, form == DBSA_LOGITS, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
+}
+
+namespace {
+// What the calls on a set of books share.  rows: the call needs questions with lengths.
+int book_common(BookParams& p, const dbsa_page_book* book, bool rows) {
+  if (!book || !book->refs || book->n_pages < 1 || book->n_queries < (rows ? 1 : 0)) return DBSA_ERR_INVALID_ARG;
+  if (book->n_queries > 0 && (!book->table || book->table_stride < 1)) return DBSA_ERR_INVALID_ARG;
+  if (rows && !book->self_len) return DBSA_ERR_INVALID_ARG;
+  if (book->page_tokens < 16 || (book->page_tokens & (book->page_tokens - 1)) != 0) return DBSA_ERR_UNSUPPORTED;
+  if (book->n_queries > kBookQuestions || book->table_stride > 1 << 24) return DBSA_ERR_UNSUPPORTED;
+  p.table = book->table;
+  p.refs = book->refs;
+  p.self_len = book->self_len;
+  p.n_queries = book->n_queries;
+  p.table_stride = book->table_stride;
+  p.page_log2 = __builtin_ctz(static_cast<unsigned>(book->page_tokens));
+  p.n_pages = book->n_pages;
+  return DBSA_OK;
+}
+}  // namespace
+
+int dbsa_pages_fork(const dbsa_page_book* book, const int32_t* source, void* stream) {
+  BookParams p{};
+  if (int rc = book_common(p, book, true)) return rc;
+  if (!source) return DBSA_ERR_INVALID_ARG;
+  return launch_pages_fork(p, source, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
+}
+
+int dbsa_pages_reserve(const dbsa_page_book* book, const int32_t* add, int32_t* got, int32_t* copies, int32_t* n_copies,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  BookParams p{};
+  if (int rc = book_common(p, book, true)) return rc;
+  if (!add || !got || !copies || !n_copies) return DBSA_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < static_cast<size_t>(p.n_pages) * 4 || reinterpret_cast<uintptr_t>(workspace) % 4 != 0) return DBSA_ERR_WORKSPACE;
+  return launch_pages_reserve(p, add, got, copies, n_copies, static_cast<int32_t*>(workspace), static_cast<hipStream_t>(stream)) == hipSuccess
+             ? DBSA_OK
+             : DBSA_ERR_HIP;
+}
+
+int dbsa_pages_trim(const dbsa_page_book* book, void* stream) {
+  BookParams p{};
+  if (int rc = book_common(p, book, true)) return rc;
+  return launch_pages_trim(p, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
+}
+
+int dbsa_pages_compact(const dbsa_page_book* book, int32_t* copies, int32_t* counts, int32_t* new_place, void* stream) {
+  BookParams p{};
+  if (int rc = book_common(p, book, false)) return rc;
+  if (!copies || !counts || !new_place) return DBSA_ERR_INVALID_ARG;
+  return launch_pages_compact(p, copies, counts, new_place, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
+}
+
+int dbsa_pages_copy(const dbsa_pages* pages, int32_t n_layers, int64_t stride_layer, const int32_t* copies, const int32_t* n_copies,
+                    int32_t max_copies, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, void* stream) {
+  if (dtype != DBSA_BF16 && dtype != DBSA_F32 && dtype != DBSA_E4M3) return DBSA_ERR_UNSUPPORTED;
+  if (head_dim != 64 && head_dim != 128) return DBSA_ERR_UNSUPPORTED;
+  if (!pages || !copies || !n_copies || n_layers < 1 || max_copies < 0 || n_kv_heads < 1 || pages->n_pages < 1) return DBSA_ERR_INVALID_ARG;
+  for (const dbsa_tensor& t : {pages->k, pages->v})
+    if (!(dtype == DBSA_E4M3 ? cache_ok(t) : tensor_ok(t, dtype))) return DBSA_ERR_INVALID_ARG;
+  const int bytes = dtype == DBSA_E4M3 ? 1 : dtype == DBSA_BF16 ? 2 : 4;
+  if (pages->stride_page <= 0 || pages->stride_page * bytes % 16 != 0 || stride_layer < 0 || stride_layer * bytes % 16 != 0 ||
+      (n_layers > 1 && stride_layer == 0))
+    return DBSA_ERR_INVALID_ARG;
+  if (pages->page_tokens < 16 || (pages->page_tokens & (pages->page_tokens - 1)) != 0) return DBSA_ERR_UNSUPPORTED;
+  const int64_t units = int64_t{pages->page_tokens} * n_kv_heads * (head_dim * bytes / 16);
+  if (units > 1 << 30) return DBSA_ERR_UNSUPPORTED;  // 16 GB a page
+  PagesCopyParams p{};
+  p.k = view(pages->k);
+  p.v = view(pages->v);
+  p.stride_page = pages->stride_page;
+  p.stride_layer = stride_layer;
+  p.copies = copies;
+  p.n_copies = n_copies;
+  p.max_copies = max_copies;
+  p.n_layers = n_layers;
+  p.n_pages = pages->n_pages;
+  p.page_tokens = pages->page_tokens;
+  p.heads = n_kv_heads;
+  p.row_log2 = __builtin_ctz(static_cast<unsigned>(head_dim * bytes / 16));
+  p.elem_bytes = bytes;
+  p.flat = pages->k.stride_head == head_dim && pages->v.stride_head == head_dim &&
+           pages->k.stride_tok == int64_t{n_kv_heads} * head_dim && pages->v.stride_tok == int64_t{n_kv_heads} * head_dim;
+  return launch_pages_copy(p, static_cast<hipStream_t>(stream)) == hipSuccess ? DBSA_OK : DBSA_ERR_HIP;
+}
+
 }  // extern "C"
 
 namespace {

@@ -162,3 +162,44 @@ struct Kv8Params {
 hipError_t launch_kv8_scales(const Kv8Params& p, bool bf16, bool running, hipStream_t stream);
 hipError_t launch_kv8_write(const Kv8Params& p, bool bf16, hipStream_t stream);
 hipError_t launch_kv8_read(const Kv8Params& p, bool bf16, hipStream_t stream);
+
+// Verification of proposed tokens (verify.hip).  Row t of target checks the token behind it; T_u rows of question u lie at
+// cu[u] .. cu[u+1]-1.
+struct VerifyParams {
+  const void* target;   // [n_tokens][vocab]
+  int64_t target_stride;
+  const void* draft;    // null, or step a of question u at u * draft_query + a * draft_step
+  int64_t draft_query, draft_step;
+  int32_t draft_steps;
+  const int32_t *tokens, *cu;   // device [n_tokens], [n_queries + 1]
+  const float *uniform, *heat;  // device [n_tokens]; [n_queries] or null
+  const int32_t* self_len;      // device [n_queries] or null
+  int32_t *out, *accepted, *new_len;
+  float* logp;
+  int32_t n_queries, n_tokens, vocab;
+  void* workspace;
+};
+size_t verify_workspace_bytes(int64_t n_tokens, int64_t n_queries, int64_t vocab);
+hipError_t launch_verify(const VerifyParams& p, bool bf16, bool logits, hipStream_t stream);
+
+// Page tables (pages.hip): the caller's arrays, all on the device and changed in place.
+struct BookParams {
+  int32_t *table, *refs, *self_len;
+  int32_t n_queries, table_stride, page_log2, n_pages;
+};
+constexpr int kBookQuestions = 8192;  // most rows of a table
+hipError_t launch_pages_fork(const BookParams& p, const int32_t* source, hipStream_t stream);
+hipError_t launch_pages_reserve(const BookParams& p, const int32_t* add, int32_t* got, int32_t* copies, int32_t* n_copies, int32_t* spare,
+                                hipStream_t stream);
+hipError_t launch_pages_trim(const BookParams& p, hipStream_t stream);
+hipError_t launch_pages_compact(const BookParams& p, int32_t* copies, int32_t* counts, int32_t* new_place, hipStream_t stream);
+
+struct PagesCopyParams {
+  TensorView k, v;  // a page: [page tokens, heads, D]
+  int64_t stride_page, stride_layer;
+  const int32_t *copies, *n_copies;  // device [max_copies][3] = (from, to, rows); how many of them count
+  int32_t max_copies, n_layers, n_pages, page_tokens, heads, row_log2;  // rows of 16 << row_log2 bytes
+  int32_t elem_bytes;
+  int32_t flat;  // a page's rows lie end to end
+};
+hipError_t launch_pages_copy(const PagesCopyParams& p, hipStream_t stream);

@@ -1,0 +1,276 @@
+"""Verification of proposed tokens against the fp64 oracle.  Tokens and counts have to be the oracle's: kernel and oracle hold weights
+and their running sums in 64 bits, 2e-12 apart, so that the choice among V tokens differs with a probability of about V * 4e-12.
+Log probabilities: one rounding to fp32, half a step (2^-24 of the value), and what 64 bits leave (1e-10)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import steps_oracle as orc
+from paper_2503_08640_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def make(seed, rows, vocab, dtype="bf16", form="logits", draft=True, heat=None, spread=2.0):
+    """A batch on the host, values as the type holds them."""
+    rng = np.random.default_rng(seed)
+    b, n, steps = len(rows), sum(rows), max(max(rows) - 1, 0)
+    cu = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+    x = spread * rng.standard_normal((n, vocab)) + 8.0 * (rng.random((n, vocab)) < 2.0 / vocab)
+    y = np.zeros((b, steps, vocab))
+    tokens = rng.integers(0, vocab, n).astype(np.int32)
+    for u in range(b):
+        for a in range(rows[u] - 1):
+            near = x[cu[u] + a] + 0.7 * rng.standard_normal(vocab)
+            y[u, a] = near
+            t = 1.0 if heat is None else heat[u]
+            noise = rng.gumbel(size=vocab) * (t if 0 < t < 100 else 0.0) if draft else 0.0
+            tokens[cu[u] + a + 1] = int(np.argmax(near + noise))
+    if form == "probs":
+        x, y = (np.exp(z - z.max(-1, keepdims=True)) for z in (x, y))
+        x, y = (np.where(z < 1e-3, 0, z) / np.where(z < 1e-3, 0, z).sum(-1, keepdims=True) for z in (x, y))
+    c = dict(x=torch.from_numpy(x).to(TYPES[dtype]), y=torch.from_numpy(y).to(TYPES[dtype]) if draft and steps else None, tokens=tokens, cu=cu,
+             uniform=rng.random(n).astype(np.float32), heat=None if heat is None else np.asarray(heat, np.float32), form=form)
+    return c
+
+
+def wanted(c):
+    f = lambda t: None if t is None else t.double().numpy()  # noqa: E731
+    return orc.draft_verify(f(c["x"]), c["tokens"], c["cu"], c["uniform"].astype(np.float64), draft=f(c["y"]),
+                            temperature=None if c["heat"] is None else c["heat"].astype(np.float64), probabilities=c["form"] == "probs")
+
+
+def dev(x):
+    return None if x is None else torch.from_numpy(x).cuda() if isinstance(x, np.ndarray) else x.cuda()
+
+
+def call(c, x=None, y=None, spare=3, **more):
+    """Through buffers with rows behind the last question's, which have to stay as they are."""
+    x = dev(c["x"]) if x is None else x
+    y = dev(c["y"]) if y is None else y
+    n, b = c["x"].shape[0], len(c["cu"]) - 1
+    full = torch.full((n + spare,), -77, dtype=torch.int32, device="cuda")
+    logp = torch.full((n + spare,), float("nan"), device="cuda")
+    tokens = torch.cat([dev(c["tokens"]), torch.zeros(spare, dtype=torch.int32, device="cuda")])
+    uniform = torch.cat([dev(c["uniform"]), torch.zeros(spare, device="cuda")])
+    if spare:
+        x = torch.cat([x, x.new_zeros((spare, x.shape[1]))])
+    self_len = torch.arange(100, 100 + b, dtype=torch.int32, device="cuda")
+    kept = torch.zeros(b, dtype=torch.int32, device="cuda")
+    need = B.dbsa_draft_verify_workspace_bytes(n + spare, b, c["x"].shape[1])
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")  # (no number in any of its words)
+    out, accepted = B.dbsa_draft_verify(x, tokens, dev(c["cu"]), uniform, draft=y, temperature=dev(c["heat"]), probs=c["form"] == "probs",
+                                        out=full, logp=logp, self_len=self_len, new_len=kept, workspace=ws, **more)
+    torch.cuda.synchronize()
+    assert (full[n:] == -77).all() and torch.isnan(logp[n:]).all()
+    return dict(out=out[:n].cpu().numpy(), accepted=accepted.cpu().numpy(), logp=logp[:n].double().cpu().numpy(), kept=kept.cpu().numpy())
+
+
+def same(got, want, c, what=""):
+    print(f"[verify] {what}: stands {got['accepted'].tolist()[:8]} tokens {got['out'].tolist()[:8]}", flush=True)
+    assert (got["accepted"] == want["accepted"]).all(), what
+    assert (got["out"] == want["out"]).all(), what
+    off = np.abs(got["logp"] - want["logp"])
+    assert (off <= 2.0 ** -24 * np.abs(want["logp"]) + 1e-10).all(), (what, off.max())
+    rows = np.diff(c["cu"])
+    assert (got["kept"] == 100 + np.arange(len(rows)) - np.where(rows > 0, rows - 1 - want["accepted"], 0)).all(), what
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 7, 64, 1000, 4095, 4096, 4097, 8183, 8192, 8193, 50257])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_vocabularies(vocab, dtype):
+    for draft in (True, False):
+        c = make(vocab + draft, [5, 1, 3], vocab, dtype, draft=draft)
+        same(call(c), wanted(c), c, f"vocab {vocab} {dtype} draft {draft}")
+
+
+@pytest.mark.parametrize("form", ["logits", "probs"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("rows", [[1], [2], [1, 1, 1], [9, 4, 1, 12, 7], [70], [0, 3, 0, 0, 5, 0]])
+def test_chunks(form, dtype, draft, rows):
+    for seed in range(3):
+        c = make(100 * seed + sum(rows), rows, 1777, dtype, form, draft)
+        same(call(c), wanted(c), c, f"{form} {dtype} draft {draft} rows {rows}")
+
+
+def test_more_questions_than_threads():
+    rng = np.random.default_rng(1)
+    rows = [int(x) for x in rng.integers(0, 4, 700)]
+    for form in ("logits", "probs"):
+        c = make(5, rows, 33, "bf16", form)
+        same(call(c), wanted(c), c, f"700 questions {form}")
+
+
+def test_large_vocabulary():
+    c = make(77, [4, 6], 300001, "bf16", heat=[0.8, 0.0], spread=0.5)  # (more pieces than a wave has lanes)
+    same(call(c), wanted(c), c, "300001 words")
+    c = make(78, [3], 530000, "f32", spread=0.1)
+    same(call(c), wanted(c), c, "530000 words")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("draft", [True, False])
+def test_temperatures(dtype, draft):
+    heat = [0.0, 0.3, 1.0, 1.7, -1.0, float("nan"), float("inf"), 1e-30, 1e30]
+    c = make(9, [4] * len(heat), 3001, dtype, draft=draft, heat=heat)
+    same(call(c), wanted(c), c, f"temperatures {dtype} draft {draft}")
+
+
+def test_greedy_takes_the_first_of_equal_values():
+    for dtype in ("bf16", "f32"):
+        c = make(3, [3, 2, 1, 2], 20000, dtype, heat=[0.0] * 4)
+        c["x"] = torch.zeros_like(c["x"])
+        c["x"][0, 15000], c["x"][0, 9000], c["x"][0, 19999] = 3, 3, 3
+        c["x"][1, 5] = -2
+        c["tokens"][1], c["tokens"][2] = 9000, 0
+        want = wanted(c)
+        assert list(want["out"][:2]) == [9000, 0]
+        same(call(c), want, c, f"ties {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heat", [None, 0.0, 0.7])
+def test_values_that_are_no_numbers(dtype, heat):
+    inf, nan = float("inf"), float("nan")
+    for seed in range(4):
+        c = make(40 + seed, [3, 3, 3, 2, 2, 1, 1], 9001, dtype, heat=None if heat is None else [heat] * 7)
+        rng = np.random.default_rng(seed)
+        hide = torch.from_numpy(rng.random(c["x"].shape) < 0.999)
+        c["x"][hide] = -inf                     # nearly everything is masked
+        c["y"][1, :] = nan                      # what proposed has no distribution
+        c["x"][6] = nan
+        c["x"][7, 100], c["x"][7, 8999] = inf, inf
+        c["x"][9] = -inf
+        c["x"][11] = nan
+        c["x"][13, 4], c["y"][4, 0, 4] = inf, inf
+        c["x"][14] = -inf
+        c["x"][14, 8192] = -3.0
+        same(call(c), wanted(c), c, f"no numbers {dtype} {heat} {seed}")
+    c = make(50, [3, 3], 500, dtype, "probs")
+    c["x"][0, :100], c["x"][1, 7], c["x"][2] = -1.0, inf, nan
+    c["x"][3], c["y"][1, 0, 9] = 0.0, nan
+    same(call(c), wanted(c), c, f"no probabilities {dtype}")
+
+
+def test_proposals_that_are_none():
+    """-1, words outside the vocabulary, more tokens than what proposed has rows for: the chain ends, the target is drawn from."""
+    for dtype in ("bf16", "f32"):
+        for form in ("logits", "probs"):
+            for draft in (True, False):
+                c = make(60, [6, 6, 6, 6], 999, dtype, form, draft)
+                c["tokens"][[1, 8, 15]] = [-1, 999, 2 ** 31 - 1]
+                c["tokens"][20] = -2 ** 31
+                same(call(c), wanted(c), c, f"padding {dtype} {form} {draft}")
+                if draft:
+                    c = make(61, [6, 6], 999, dtype, form)
+                    c["y"] = c["y"][:, :2].contiguous()
+                    same(call(c), wanted(c), c, f"two rows of five {dtype} {form}")
+
+
+def test_random_numbers_at_their_ends():
+    for form in ("logits", "probs"):
+        for u in (0.0, 1.0 - 2.0 ** -24, 1.0, 7.0, -1.0):
+            c = make(70, [4, 4, 1], 2500, "f32", form)
+            c["uniform"][:] = u
+            same(call(c), wanted(c), c, f"uniform {u} {form}")
+
+
+def test_equal_distributions():
+    """Target and proposer agree: everything stands; a refusal (a number of 1) leaves no weight, and the target is drawn from."""
+    c = make(80, [5, 5], 4000, "f32")
+    for u in range(2):
+        c["y"][u] = c["x"][5 * u:5 * u + 4]
+    got = call(c)
+    assert (got["accepted"] == 4).all()
+    same(got, wanted(c), c, "equal")
+    c["uniform"][1] = 1.0
+    got = call(c)
+    assert got["accepted"][0] == 1
+    same(got, wanted(c), c, "equal, refused")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", ["logits", "probs"])
+def test_strides_and_alignments(dtype, form):
+    """Rows off 16-byte addresses, wider than the vocabulary, every one at an offset of its own; the proposer's rows step by step
+    instead of question by question."""
+    for vocab, wide in ((1000, 1003), (8192, 8199), (777, 781)):
+        for off in range(0, 8, 3):
+            c = make(90 + off, [4, 5, 2], vocab, dtype, form)
+            n = c["x"].shape[0]
+            flat = torch.full((off + (n + 1) * wide,), float("nan"), dtype=TYPES[dtype], device="cuda")
+            x = torch.as_strided(flat, (n, vocab), (wide, 1), off)
+            x.copy_(c["x"])
+            b, k = c["y"].shape[:2]
+            steps = torch.full((k, b, vocab + 5), float("nan"), dtype=TYPES[dtype], device="cuda")
+            y = steps[:, :, 3:3 + vocab].transpose(0, 1)
+            y.copy_(c["y"])
+            same(call(c, x, y, spare=0), wanted(c), c, f"stride {wide} offset {off} {dtype} {form}")
+
+
+def test_lengths_may_be_changed_in_place():
+    c = make(95, [4, 3], 500)
+    n = torch.tensor([40, 50], dtype=torch.int32, device="cuda")
+    out, accepted = B.dbsa_draft_verify(dev(c["x"]), dev(c["tokens"]), dev(c["cu"]), dev(c["uniform"]), draft=dev(c["y"]), self_len=n, new_len=n)
+    want = wanted(c)
+    assert (out.cpu().numpy() == want["out"]).all()
+    assert n.tolist() == [40 - 3 + want["accepted"][0], 50 - 2 + want["accepted"][1]]
+
+
+def test_two_graphs_with_one_workspace():
+    """Captured on a stream of its own, replayed in turn with eager calls between, inputs changed before each replay."""
+    batches = [make(200, [5, 3], 20000, "bf16"), make(201, [2, 7, 1], 9999, "f32", heat=[0.0, 0.7, 1.0]), make(202, [3], 5000, "f32", "probs")]
+    need = max(B.dbsa_draft_verify_workspace_bytes(c["x"].shape[0], len(c["cu"]) - 1, c["x"].shape[1]) for c in batches)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    made = []
+    for c in batches:
+        t = dict(x=dev(c["x"]), y=dev(c["y"]), tokens=dev(c["tokens"]), cu=dev(c["cu"]), uniform=dev(c["uniform"]), heat=dev(c["heat"]))
+        t["out"] = torch.empty_like(t["tokens"])
+        t["acc"] = torch.empty_like(t["cu"][1:])
+        run = lambda t=t, c=c: B.dbsa_draft_verify(t["x"], t["tokens"], t["cu"], t["uniform"], draft=t["y"], temperature=t["heat"],  # noqa: E731
+                                                   probs=c["form"] == "probs", out=t["out"], accepted=t["acc"], workspace=ws)
+        run()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run()
+        made.append((c, t, g, run))
+    for turn in range(4):
+        for c, t, g, run in made:
+            c["uniform"] = np.random.default_rng(turn).random(len(c["uniform"])).astype(np.float32)
+            t["uniform"].copy_(torch.from_numpy(c["uniform"]))
+            t["out"].fill_(-5)
+            g.replay()
+            want = wanted(c)
+            torch.cuda.synchronize()
+            assert (t["out"].cpu().numpy() == want["out"]).all() and (t["acc"].cpu().numpy() == want["accepted"]).all()
+            t["out"].fill_(-5)
+            run()
+            torch.cuda.synchronize()
+            assert (t["out"].cpu().numpy() == want["out"]).all()
+
+
+def test_on_another_stream():
+    c = make(300, [4, 4, 4], 30000, "bf16")
+    want, stream = wanted(c), torch.cuda.Stream()
+    x, y = dev(c["x"]), dev(c["y"])
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        out, accepted = B.dbsa_draft_verify(x, dev(c["tokens"]), dev(c["cu"]), dev(c["uniform"]), draft=y)
+    stream.synchronize()
+    assert (out.cpu().numpy() == want["out"]).all() and (accepted.cpu().numpy() == want["accepted"]).all()
+
+
+def test_bounds_that_do_not_ascend_stay_inside():
+    """cu_qlens lies on the device: whatever it holds, nothing outside the arrays is touched (and questions that are in order among
+    the others need not come out right)."""
+    c = make(310, [3, 3], 600)
+    for cu in ([0, 50, 6], [-4, 3, 6], [5, 2, 100000], [0, 6, 2]):
+        full = torch.full((10,), -77, dtype=torch.int32, device="cuda")
+        B.dbsa_draft_verify(dev(c["x"]), dev(c["tokens"]), torch.tensor(cu, dtype=torch.int32, device="cuda"), dev(c["uniform"]),
+                            draft=dev(c["y"]), out=full[2:8], logp=torch.zeros(6, device="cuda"))
+        torch.cuda.synchronize()
+        assert (full[:2] == -77).all() and (full[8:] == -77).all()
