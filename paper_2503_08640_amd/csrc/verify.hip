@@ -7,10 +7,12 @@
 // A choice among 10^5 tokens lies next to a border often enough that 32 bits would choose another one now and then: weights,
 // sums and their prefixes are held in 64 bits throughout.
 //
-// verify_stats_kernel   logits only: largest value, sum of exponentials around it and place of the largest, of each piece of
-//                       every row (the one pass over all of them)
-// verify_weigh_kernel   which proposals stand; sums of w over pieces of the row that decides
-// verify_pick_kernel    the piece in which the running sum passes its share, the token in it, what is written
+// verify_stats_kernel   logits only: the sum of exponentials (and where it is asked for, the place of the largest value) of each
+//                       piece of every row, the one pass over all of them
+// verify_decide_kernel  many questions: which proposals stand
+// verify_draw_kernel    few questions: the same, first; sums of w over shares of the row that decides; the last workgroup of a
+//                       question to be done finds the share in which the running sum passes its part, and the token in it
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 
@@ -19,58 +21,60 @@
 namespace {
 
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef uintx4 loose_uintx4 __attribute__((aligned(2)));  // rows begin where they like: 16 bytes at any address of a value
 
-constexpr int kThreads = 256;
-constexpr int kPiece = 8192;   // values of a piece of statistics
-constexpr int kShare = 4096;   // values of a piece of weights
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kPieceLeast = 2048;  // values of a wave's piece of statistics
+constexpr int kShare = 512;        // values whose weights a wave sums up as one
+constexpr int kGroup = 16;         // lanes that look at one row, the next as many at the row of what proposed
+constexpr int kRows = kThreads / (2 * kGroup);
+constexpr int kApart = 64;         // counters lie 256 bytes apart
 
+// What a row gives its weights from.
 struct Decision {
-  int32_t row, stands;  // row of the target that the token is drawn from (-1: no rows); proposals that stand
-  int32_t refused;      // 0: w = p; 1: w = max(p - q, 0); 2: w = p without the proposal
-  int32_t token;        // greedy: the token; else -1
-  int32_t proposal;
-  float top_p, top_q;
-  int32_t pad;
-  double inv_p, inv_q;  // 1 / sum of exponentials
+  int row, step;        // that the token is drawn from, and its number in the question; row -1: no rows
+  int refused;          // 0: w = p; 1: w = max(p - q, 0); 2: w = p without the proposal
+  int proposal, place;  // place: of the largest value
+  float top_p, top_q, number;
+  double log_p, inv_p, inv_q;  // logarithm and inverse of the sums of exponentials
 };
 
 // pieces of the workspace
 struct Work {
-  double* sum;      // [2 n_tokens][pieces]: target rows, then the rows of what proposed
-  float* top;
+  double* sum;   // [2 n_tokens][pieces]: target rows, then the rows of what proposed
+  float* top;    // what its weights are counted from
+  float* peak;   // greedy: largest value and its place
   int32_t* place;
-  double *weight, *plain;  // [n_queries][shares]: sums of w and of p
+  double* weight;          // [n_queries][shares]: sums of w
   Decision* decision;      // [n_queries]
+  unsigned* done;          // [n_queries][kApart]: workgroups that have left theirs
   int pieces, shares;
 };
 __host__ __device__ inline int64_t pieces_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
-__host__ __device__ inline Work work_of(void* base, int64_t n_tokens, int64_t n_queries, int64_t vocab) {
+__host__ __device__ inline Work work_of(void* base, int64_t n_tokens, int64_t n_queries, int64_t vocab, int64_t piece) {
   Work w;
-  // (a row may begin up to seven values off a 16-byte address)
-  w.pieces = static_cast<int>(pieces_of(vocab + 7, kPiece));
+  w.pieces = static_cast<int>(pieces_of(vocab, piece));
   w.shares = static_cast<int>(pieces_of(vocab, kShare));
   char* at = static_cast<char*>(base);
   w.decision = reinterpret_cast<Decision*>(at);
   at += n_queries * static_cast<int64_t>(sizeof(Decision));
   w.weight = reinterpret_cast<double*>(at);
   at += n_queries * w.shares * 8;
-  w.plain = reinterpret_cast<double*>(at);
-  at += n_queries * w.shares * 8;
   const int64_t cells = 2 * n_tokens * w.pieces;
   w.sum = reinterpret_cast<double*>(at);
   at += cells * 8;
   w.top = reinterpret_cast<float*>(at);
   at += cells * 4;
+  w.peak = reinterpret_cast<float*>(at);
+  at += cells * 4;
   w.place = reinterpret_cast<int32_t*>(at);
+  at += cells * 4;
+  w.done = reinterpret_cast<unsigned*>(at);
   return w;
 }
 
-// 2^t for t <= 0 in 64 bits, to 2e-12 of it: the nearest whole number goes to the exponent, the rest through the polynomial
-// that meets 2^f at the nine Chebyshev points of [-1/2, 1/2].  No number and what lies below 2^-1074 give 0.
-__device__ inline double exp2_below(double t) {
-  t = fmax(t, -1100.0);
-  const double shifted = t + 6755399441055744.0;  // 3 * 2^51: the sum's low bits hold the whole number
-  const double f = t - (shifted - 6755399441055744.0);
+// 2^f for f in [-1/2, 1/2], to 2e-12 of it: the polynomial that meets it at the interval's nine Chebyshev points.
+__device__ inline double exp2_part(double f) {
   double y = 0x1.63d1363930791p-20;
   y = fma(y, f, 0x1.00dc4a53395d3p-16);
   y = fma(y, f, 0x1.4308ac85a7718p-13);
@@ -79,16 +83,55 @@ __device__ inline double exp2_below(double t) {
   y = fma(y, f, 0x1.c6b08dd6fd236p-5);
   y = fma(y, f, 0x1.ebfbdff823cedp-3);
   y = fma(y, f, 0x1.62e42fef84cf0p-1);
-  y = fma(y, f, 1.0);
-  return ldexp(y, static_cast<int>(__double2loint(shifted)));
+  return fma(y, f, 1.0);
+}
+// 2^t for any t; nothing below 2^-1074, however far
+__device__ inline double exp2_of(double t) {
+#pragma clang fp contract(off)  // (f would take what the product behind a large t was rounded by)
+  const double whole = rint(t);
+  int exponent;
+  asm("v_cvt_i32_f64 %0, %1" : "=v"(exponent) : "v"(whole));  // (stays at the ends of its range)
+  return __builtin_amdgcn_ldexp(exp2_part(t - whole), exponent);
 }
 
-// e^((x - top) / T): factor = log2(e) / T.  Infinite values share everything between them; a row of none above -infinity has
-// no weight.
-__device__ inline double weight_of(float x, float top, double factor) {
-  if (top == INFINITY) return x == INFINITY ? 1.0 : 0.0;
-  if (!(top > -INFINITY)) return 0.0;
-  return exp2_below((static_cast<double>(x) - static_cast<double>(top)) * factor);
+// Weights 2^(x factor - reference), factor = log2(e) / T, are counted from the value `top`.  Where x factor stays within 2^20 the
+// reference is the nearest whole number to top factor, which then enters the exponent alone: fourteen operations of 64 bits, four
+// cycles each, which bound the statistics in bf16.  Where it does not, from top itself.
+struct Scale {
+  double factor, shift;  // shift: 3 * 2^51 less the reference: x factor + shift holds the exponent in its low bits
+  float top, least, most;  // values beyond least and most weigh nothing, and more than 64 bits hold
+  bool plain;
+};
+__device__ inline Scale scale_of(float top, double factor) {
+  Scale s{factor, 0.0, top, 0.f, 0.f, false};
+  const double reference = rint(static_cast<double>(top) * factor);
+  s.plain = fabs(reference) < 0x1p20 && factor < 0x1p100;
+  s.shift = 6755399441055744.0 - reference;
+  const double inverse = 1.0 / factor;
+  s.least = static_cast<float>((reference - 2000.0) * inverse);
+  s.most = static_cast<float>((reference + 1100.0) * inverse);
+  return s;
+}
+__device__ inline double plain_weight(float x, const Scale& s) {
+  const double v = __builtin_amdgcn_fmed3f(x, s.least, s.most);  // (what is no number becomes the least)
+  const double shifted = fma(v, s.factor, s.shift), whole = shifted - s.shift;
+  return __builtin_amdgcn_ldexp(exp2_part(fma(v, s.factor, -whole)), __double2loint(shifted));
+}
+// What is no number, and -infinity, has no weight; infinite values share everything between them; a row of none above -infinity
+// has no weight.
+__device__ inline double weight_of(float x, const Scale& s) {
+  if (s.plain) return plain_weight(x, s);
+  if (s.top == INFINITY) return x == INFINITY ? 1.0 : 0.0;
+  return x >= -FLT_MAX && s.top >= -FLT_MAX ? exp2_of((static_cast<double>(x) - static_cast<double>(s.top)) * s.factor) : 0.0;
+}
+// what weights counted from `from` are to be multiplied by to be counted from `to`, which is not lower
+__device__ inline double rescale(const Scale& from, const Scale& to) {
+  if (from.plain && to.plain) return exp2_of(to.shift - from.shift);
+  if (from.top == to.top) return 1.0;
+  if (to.top == INFINITY) return 0.0;
+  if (from.plain || to.plain) return exp2_of((from.plain ? 6755399441055744.0 - from.shift : from.top * from.factor) -
+                                             (to.plain ? 6755399441055744.0 - to.shift : to.top * to.factor));
+  return exp2_of((static_cast<double>(from.top) - static_cast<double>(to.top)) * to.factor);
 }
 
 __device__ inline float widen(float x) { return x; }
@@ -98,6 +141,17 @@ __device__ inline float at(const T* p, int64_t i) { return widen(p[i]); }
 
 // a probability that is no number, negative or infinite counts as none
 __device__ inline double clean(float p) { return p > 0.f && p < INFINITY ? static_cast<double>(p) : 0.0; }
+
+// natural logarithm of the probability of value x, from that of the sum of the weights counted from top
+constexpr double kLn2 = 0.69314718055994530942;
+template <bool kLogits>
+__device__ inline double log_of(float x, float top, double log_sum, double factor) {
+  if constexpr (!kLogits) return log(clean(x));
+  return (top == INFINITY ? 0.0 : (static_cast<double>(x) - static_cast<double>(top)) * factor * kLn2) - log_sum;
+}
+__device__ inline double log_sum_of(double sum, const Scale& s) {  // counted from top
+  return log(sum) + (s.plain ? (6755399441055744.0 - s.shift - static_cast<double>(s.top) * s.factor) * kLn2 : 0.0);
+}
 
 __device__ inline float wave_max(float v) {
 #pragma unroll
@@ -119,14 +173,19 @@ struct Span {
   int begin, end;
 };
 __device__ inline Span span_of(const VerifyParams& p, int u) {
-  const int begin = min(max(p.cu[u], 0), p.n_tokens);
-  return {begin, min(max(p.cu[u + 1], begin), p.n_tokens)};
+  const int from = p.cu[u], to = p.cu[u + 1], begin = min(max(from, 0), p.n_tokens);
+  return {begin, min(max(to, begin), p.n_tokens)};
 }
-// 1 / T as the factor of base-2 exponents; a temperature that is not above 0 is greedy, its statistics those of T = 1
-__device__ inline bool greedy_of(const VerifyParams& p, int u) { return p.heat && !(p.heat[u] > 0.f); }
-__device__ inline double factor_of(const VerifyParams& p, int u, bool greedy) {
-  const double heat = p.heat && !greedy ? static_cast<double>(p.heat[u]) : 1.0;
-  return 1.4426950408889634074 / heat;
+// A temperature that is not above 0 is greedy, its statistics those of T = 1.  (Above 1e30 it would give weight to what is masked
+// with the type's lowest value.)
+struct Heat {
+  bool greedy;
+  double factor;  // log2(e) / T
+};
+__device__ inline Heat heat_of(const VerifyParams& p, int u) {
+  const float t = p.heat ? p.heat[u] : 1.f;
+  const bool greedy = !(t > 0.f);
+  return {greedy, 1.4426950408889634074 / (greedy ? 1.0 : static_cast<double>(fminf(t, 1e30f)))};
 }
 template <typename T>
 __device__ inline const T* target_row(const VerifyParams& p, int64_t row) { return static_cast<const T*>(p.target) + row * p.target_stride; }
@@ -134,214 +193,333 @@ template <typename T>
 __device__ inline const T* draft_row(const VerifyParams& p, int64_t u, int64_t step) {
   return static_cast<const T*>(p.draft) + u * p.draft_query + step * p.draft_step;
 }
-// whether row t checks a proposal: a token of the vocabulary that a row of probabilities belongs to
-__device__ inline bool proposes(const VerifyParams& p, const Span& s, int row) {
-  if (row + 1 >= s.end) return false;
-  const int x = p.tokens[row + 1];
-  return x >= 0 && x < p.vocab && (!p.draft || row - s.begin < p.draft_steps);
+// whether row t checks proposal x: a token of the vocabulary that a row of probabilities belongs to
+__device__ inline bool proposes(const VerifyParams& p, const Span& s, int row, int x) {
+  return row + 1 < s.end && x >= 0 && x < p.vocab && (!p.draft || row - s.begin < p.draft_steps);
 }
 
-// One workgroup: a piece of a row.  Values stay in registers between the maximum and the sum.
+// 16 / sizeof(T) values from the first-th on, in two steps, so that several loads are in flight before one is waited for: the
+// load (behind the row's end: of its last 16 bytes), then the values, `none` behind the end.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p) {
-  constexpr int kWide = 16 / sizeof(T), kLoads = kPiece / kThreads / kWide;
-  const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab);
-  const int64_t cell = blockIdx.x;
-  const int piece = static_cast<int>(cell % w.pieces);
+__device__ inline uintx4 load_wide(const T* row, int first, int vocab) {
+  constexpr int n = 16 / sizeof(T);
+  return vocab < n ? uintx4{} : *reinterpret_cast<const loose_uintx4*>(row + min(first, vocab - n));
+}
+template <typename T, int n = 16 / sizeof(T)>
+__device__ inline void widen_all(uintx4 v, float (&x)[n]) {
+#pragma unroll
+  for (int e = 0; e < n; ++e)
+    x[e] = sizeof(T) == 2 ? __uint_as_float(e % 2 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16) : __uint_as_float(v[e % 4]);
+}
+template <typename T, int n = 16 / sizeof(T)>
+__device__ inline void values_of(uintx4 v, const T* row, int first, int vocab, float none, float (&x)[n]) {
+  if (first + n <= vocab) {
+    widen_all<T>(v, x);
+  } else {
+#pragma unroll
+    for (int e = 0; e < n; ++e) x[e] = first + e < vocab ? at(row, first + e) : none;
+  }
+}
+
+// One wave: a piece of a row, in chunks of kLoads times 16 bytes a lane, the next chunk on its way while one is summed up.  The
+// exponents are counted from the largest value of the first chunk that has one: 64 bits leave 2^1000 on either side, so that the
+// maximum need not be followed.  A piece that holds more than that (or +infinity) is gone through again with its own.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, int piece) {
+  constexpr int kWide = 16 / sizeof(T), kLoads = 2, kStep = 64 * kWide, kChunk = kLoads * kStep;
+  const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
+  const int lane = threadIdx.x % 64;
+  // (the counters of the kernels behind this one)
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.n_queries; i += static_cast<int64_t>(gridDim.x) * kThreads) w.done[i * kApart] = 0;
+  const int64_t cell = static_cast<int64_t>(blockIdx.x) * kWaves + threadIdx.x / 64;
   const int64_t which = cell / w.pieces;
+  if (which >= (p.draft ? 2 : 1) * static_cast<int64_t>(p.n_tokens)) return;
   const bool of_draft = which >= p.n_tokens;
   const int row = static_cast<int>(of_draft ? which - p.n_tokens : which);
-  __shared__ float top_sh[kThreads / 64];
-  __shared__ double sum_sh[kThreads / 64];
-  __shared__ int place_sh[kThreads / 64];
+  const int begin = static_cast<int>(cell - which * w.pieces) * piece, end = min(begin + piece, p.vocab);
+  const int mine = begin + lane * kWide;
+  uintx4 raw[kLoads];
+  const T* from = target_row<T>(p, row);
+  if (!of_draft) {  // (asked for before it is known what for)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) raw[i] = load_wide(from, mine + i * kStep, p.vocab);
+  }
   // the question: as many as end at or before this row
   int u = 0;
-  for (int i = 0; i < p.n_queries; i += kThreads) {
-    const int mine = i + static_cast<int>(threadIdx.x);
-    u += __syncthreads_count(mine < p.n_queries && p.cu[mine + 1] <= row);
-  }
+  for (int i = 0; i < p.n_queries; i += 64) u += __popcll(__ballot(i + lane < p.n_queries && p.cu[min(i + lane, p.n_queries - 1) + 1] <= row));
   if (u >= p.n_queries) return;
   const Span s = span_of(p, u);
+  const Heat heat = heat_of(p, u);
   if (row < s.begin || row >= s.end) return;
-  const bool greedy = greedy_of(p, u);
-  if (of_draft && (greedy || !proposes(p, s, row))) return;
-  const double factor = factor_of(p, u, greedy);
-  const T* const from = of_draft ? draft_row<T>(p, u, row - s.begin) : target_row<T>(p, row);
-  // 16-byte pieces from the address at or before the row's first value
-  const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(from) % 16 / sizeof(T));
-  float x[kLoads][kWide];
-  float top = -INFINITY;
+  if (of_draft) {
+    if (heat.greedy || row + 1 >= s.end || !proposes(p, s, row, p.tokens[row + 1])) return;
+    from = draft_row<T>(p, u, row - s.begin);
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int64_t first = static_cast<int64_t>(piece) * kPiece + (i * kThreads + threadIdx.x) * kWide - lead;
-    if (first >= 0 && first + kWide <= p.vocab) {
-      const uintx4 v = *reinterpret_cast<const uintx4*>(from + first);
+    for (int i = 0; i < kLoads; ++i) raw[i] = load_wide(from, mine + i * kStep, p.vocab);
+  }
+  const bool sums = !heat.greedy || p.logp;
+  float peak = -INFINITY;
+  double sum = 0;
+  int place = INT32_MAX;
+  Scale scale{};
+  scale.top = -INFINITY;
+  for (int chunk = begin; chunk < end; chunk += kChunk) {
+    float x[kLoads][kWide];
+    const int first = chunk + lane * kWide;
+    if (chunk + kChunk <= end) {
 #pragma unroll
-      for (int e = 0; e < kWide; ++e)
-        x[i][e] = sizeof(T) == 2 ? __uint_as_float(e % 2 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16) : __uint_as_float(v[e % 4]);
+      for (int i = 0; i < kLoads; ++i) widen_all<T>(raw[i], x[i]);
     } else {
 #pragma unroll
-      for (int e = 0; e < kWide; ++e) x[i][e] = first + e >= 0 && first + e < p.vocab ? at(from, first + e) : -INFINITY;
+      for (int i = 0; i < kLoads; ++i) values_of(raw[i], from, first + i * kStep, end, -INFINITY, x[i]);
     }
+    if (chunk + kChunk < end) {
 #pragma unroll
-    for (int e = 0; e < kWide; ++e) top = fmaxf(top, x[i][e]);  // (passes over what is no number)
+      for (int i = 0; i < kLoads; ++i) raw[i] = load_wide(from, first + kChunk + i * kStep, p.vocab);
+    }
+    if (!(scale.top > -INFINITY)) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int e = 0; e < kWide; ++e) top = fmaxf(top, x[i][e]);  // (passes over what is no number)
+      top = wave_max(top);
+      if (!(top > -INFINITY)) continue;
+      scale = scale_of(top, heat.factor);
+    }
+    if (heat.greedy) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int e = 0; e < kWide; ++e)
+          if (x[i][e] > peak) {
+            peak = x[i][e];
+            place = first + i * kStep + e;
+          }
+    }
+    if (sums) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int e = 0; e < kWide; ++e) sum += plain_weight(x[i][e], scale);
+    }
   }
-  top = wave_max(top);
-  const int wave = threadIdx.x / 64;
-  if (threadIdx.x % 64 == 0) top_sh[wave] = top;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) top = fmaxf(top, top_sh[i]);
-  double sum = 0;
-  if (top == INFINITY) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-      for (int e = 0; e < kWide; ++e) sum += x[i][e] == INFINITY ? 1.0 : 0.0;
-  } else if (top > -INFINITY) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-      for (int e = 0; e < kWide; ++e) sum += exp2_below((static_cast<double>(x[i][e]) - static_cast<double>(top)) * factor);
-  }
-  int place = p.vocab;
-  if (greedy && top > -INFINITY) {
-#pragma unroll
-    for (int i = kLoads - 1; i >= 0; --i)
-#pragma unroll
-      for (int e = kWide - 1; e >= 0; --e) {
-        const int64_t index = static_cast<int64_t>(piece) * kPiece + (i * kThreads + threadIdx.x) * kWide - lead + e;
-        if (x[i][e] == top && index >= 0 && index < p.vocab) place = static_cast<int>(index);
-      }
-  }
+  float top = scale.top;
   sum = wave_sum(sum);
-  place = wave_min(place);
-  if (threadIdx.x % 64 == 0) {
-    sum_sh[wave] = sum;
-    place_sh[wave] = place;
+  if (sums && top > -INFINITY && !(scale.plain && sum < 0x1p1000)) {
+    for (int i = begin + lane; i < end; i += 64) top = fmaxf(top, at(from, i));
+    top = wave_max(top);
+    scale = scale_of(top, heat.factor);
+    sum = 0;
+    for (int i = begin + lane; i < end; i += 64) sum += weight_of(at(from, i), scale);
+    sum = wave_sum(sum);
   }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < kThreads / 64; ++i) {
-      sum += sum_sh[i];
-      place = min(place, place_sh[i]);
-    }
+  if (heat.greedy) {
+    const float all = wave_max(peak);
+    place = wave_min(peak == all ? place : INT32_MAX);
+    peak = all;
+  }
+  if (lane == 0) {
     w.sum[cell] = sum;
     w.top[cell] = top;
+    w.peak[cell] = peak;
     w.place[cell] = place;
   }
 }
 
-// Statistics of a whole row from its pieces, by one wave.
-struct RowStats {
+__global__ void verify_clear_kernel(VerifyParams p, int piece) {
+  const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
+  const int u = blockIdx.x * kThreads + threadIdx.x;
+  if (u < p.n_queries) w.done[static_cast<int64_t>(u) * kApart] = 0;
+}
+
+// Statistics of a whole row from its pieces, by the lanes of a group.
+__device__ inline float group_max(float v) {
+#pragma unroll
+  for (int s = kGroup / 2; s > 0; s >>= 1) v = fmaxf(v, __shfl_xor(v, s));
+  return v;
+}
+struct RowSum {
+  Scale scale;
+  double sum;
+};
+// first: the lane's first piece, asked for beforehand
+struct Piece {
   float top;
   double sum;
-  int place;
 };
-__device__ inline RowStats row_stats(const Work& w, int64_t which, double factor) {
-  const int lane = threadIdx.x % 64;
-  RowStats r{-INFINITY, 0.0, INT32_MAX};
-  for (int i = lane; i < w.pieces; i += 64) r.top = fmaxf(r.top, w.top[which * w.pieces + i]);
-  r.top = wave_max(r.top);
-  for (int i = lane; i < w.pieces; i += 64) {
-    const float top = w.top[which * w.pieces + i];
-    r.sum += w.sum[which * w.pieces + i] * (top == r.top ? 1.0 : weight_of(top, r.top, factor));
-    if (top == r.top) r.place = min(r.place, w.place[which * w.pieces + i]);
+__device__ inline Piece first_piece(const Work& w, int64_t which) {
+  const int lane = threadIdx.x % kGroup;
+  const int64_t cell = which * w.pieces + min(lane, w.pieces - 1);
+  return {w.top[cell], w.sum[cell]};
+}
+__device__ inline RowSum row_sum(const Work& w, int64_t which, Piece first, double factor) {
+  const int lane = threadIdx.x % kGroup;
+  const int64_t base = which * w.pieces;
+  float top = first.top;
+  for (int i = lane + kGroup; i < w.pieces; i += kGroup) top = fmaxf(top, w.top[base + i]);
+  const Scale scale = scale_of(group_max(top), factor);
+  double sum = 0;
+  for (int i = lane; i < w.pieces; i += kGroup) {
+    if (i > lane) first = {w.top[base + i], w.sum[base + i]};
+    if (first.sum > 0) sum += first.sum * rescale(scale_of(first.top, factor), scale);
   }
-  r.sum = wave_sum(r.sum);
-  r.place = wave_min(r.place);
-  return r;
+#pragma unroll
+  for (int s = kGroup / 2; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
+  return {scale, sum};
+}
+__device__ inline int row_place(const Work& w, int64_t which) {
+  const int lane = threadIdx.x % kGroup;
+  const int64_t base = which * w.pieces;
+  float peak = -INFINITY;
+  int place = INT32_MAX;
+  for (int i = lane; i < w.pieces; i += kGroup) {
+    const float here = w.peak[base + i];
+    if (here > peak) {
+      peak = here;
+      place = w.place[base + i];
+    }
+  }
+  const float all = group_max(peak);
+  place = peak == all ? place : INT32_MAX;
+#pragma unroll
+  for (int s = kGroup / 2; s > 0; s >>= 1) place = min(place, __shfl_xor(place, s));
+  return place == INT32_MAX ? -1 : place;
 }
 __device__ inline double inverse(double sum) { return sum > 0 ? 1.0 / sum : 0.0; }
 
-// Which proposals of question u stand, by a whole workgroup: every thread gets the decision.
+// Which proposals of question u stand, by a whole workgroup, eight rows at a time: every thread gets the decision.  `tells`: this
+// workgroup writes the rows in front of the one that decides, and behind it.
 template <typename T, bool kLogits>
-__device__ Decision decide(const VerifyParams& p, const Work& w, int u, const Span& s, bool greedy, double factor) {
-  __shared__ int stop_sh;
+__device__ Decision decide(const VerifyParams& p, const Work& w, int u, const Span& s, const Heat& heat, bool tells) {
+  __shared__ unsigned falls_sh[kWaves];
   __shared__ Decision decision_sh;
-  const int wave = threadIdx.x / 64;
-  if (threadIdx.x == 0) stop_sh = s.end - 1;
-  __syncthreads();
-  for (int first = s.begin; first < s.end - 1; first += kThreads / 64) {
-    const int row = first + wave;
-    if (row < s.end - 1) {
-      bool stands = proposes(p, s, row);
-      if (stands) {
-        const int x = p.tokens[row + 1];
-        double px, qx = 1.0;
-        if constexpr (kLogits) {
-          const RowStats a = row_stats(w, row, factor);
-          if (greedy) {
-            px = x == a.place ? 1.0 : 0.0;
-            qx = 0.0;
-          } else {
-            px = weight_of(at(target_row<T>(p, row), x), a.top, factor) * inverse(a.sum);
-            if (p.draft) {
-              const RowStats b = row_stats(w, static_cast<int64_t>(p.n_tokens) + row, factor);
-              qx = weight_of(at(draft_row<T>(p, u, row - s.begin), x), b.top, factor) * inverse(b.sum);
-            }
-          }
-        } else {
-          px = clean(at(target_row<T>(p, row), x));
-          if (p.draft) qx = clean(at(draft_row<T>(p, u, row - s.begin), x));
-        }
-        stands = static_cast<double>(p.uniform[row]) * qx < px;
-      }
-      if (!stands && threadIdx.x % 64 == 0) atomicMin(&stop_sh, row);
-    }
-    __syncthreads();
-    const bool done = stop_sh < first + kThreads / 64;
-    __syncthreads();
-    if (done) break;
-  }
-  const int stop = stop_sh;
-  if (wave == 0) {
+  const int lane = threadIdx.x % (2 * kGroup), group = threadIdx.x / (2 * kGroup);
+  const bool speaks = lane == 0, of_draft = lane >= kGroup;
+  const bool sums = kLogits && (!heat.greedy || p.logp);
+  const float number = p.uniform[s.end - 1];
+  for (int first = s.begin;; first += kRows) {
+    const int row = first + group;
     Decision d{};
-    d.row = stop;
-    d.stands = stop - s.begin;
-    d.token = -1;
-    d.refused = proposes(p, s, stop) ? (p.draft ? 1 : 2) : 0;
-    d.proposal = d.refused ? p.tokens[stop + 1] : -1;
-    if constexpr (kLogits) {
-      const RowStats a = row_stats(w, stop, factor);
-      d.top_p = a.top;
-      d.inv_p = inverse(a.sum);
-      if (greedy) d.token = a.place < p.vocab ? a.place : -1;
-      else if (d.refused == 1) {
-        const RowStats b = row_stats(w, static_cast<int64_t>(p.n_tokens) + stop, factor);
-        d.top_q = b.top;
-        d.inv_q = inverse(b.sum);
+    bool stands = false;
+    int x = -1;
+    float v = 0;
+    if (row < s.end) {
+      if (row + 1 < s.end) x = p.tokens[row + 1];
+      const float number_of_row = p.uniform[row];
+      Piece piece{};
+      const int64_t which = row + (of_draft && p.draft ? static_cast<int64_t>(p.n_tokens) : 0);
+      if (sums) piece = first_piece(w, which);
+      const bool asks = proposes(p, s, row, x), drawn = asks && p.draft && !(kLogits && heat.greedy);
+      const T* const from = of_draft && drawn ? draft_row<T>(p, u, row - s.begin) : target_row<T>(p, row);
+      if (asks) v = at(from, x);
+      d.row = row;
+      d.step = row - s.begin;
+      d.number = number;
+      d.proposal = x;
+      d.refused = asks ? p.draft ? 1 : 2 : 0;
+      double mine;  // p(x), in the other half of the lanes q(x)
+      if constexpr (kLogits) {
+        mine = 0.0;
+        if (heat.greedy) d.place = row_place(w, row);
+        if (sums) {
+          const RowSum sum = row_sum(w, which, piece, heat.factor);
+          d.top_p = sum.scale.top;
+          d.inv_p = inverse(sum.sum);
+          mine = weight_of(v, sum.scale) * d.inv_p;
+          if (p.logp) d.log_p = log_sum_of(sum.sum, sum.scale);
+          d.top_q = __shfl_xor(d.top_p, kGroup);
+          d.inv_q = __shfl_xor(d.inv_p, kGroup);
+        }
+        if (heat.greedy) mine = of_draft ? 0.0 : x == d.place ? 1.0 : 0.0;
+      } else {
+        mine = clean(v);
       }
+      const double other = __shfl_xor(mine, kGroup), qx = drawn || (kLogits && heat.greedy) ? other : 1.0;
+      stands = asks && static_cast<double>(number_of_row) * qx < mine;  // (counts in the lanes that speak)
     }
-    if (threadIdx.x == 0) decision_sh = d;
+    const uint64_t mask = __ballot(!stands);
+    if (threadIdx.x % 64 == 0) falls_sh[threadIdx.x / 64] = static_cast<unsigned>((mask & 1) | (mask >> 2 * kGroup & 1) << 1) << group;
+    __syncthreads();
+    unsigned falls = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) falls |= falls_sh[i];
+    const int stop = falls ? __ffs(falls) - 1 : kRows;
+    if (group == stop && speaks) decision_sh = d;
+    if (tells && speaks && row < s.end && group != stop) {
+      p.out[row] = group < stop ? x : -1;
+      if (p.logp) p.logp[row] = group < stop ? static_cast<float>(log_of<kLogits>(v, d.top_p, d.log_p, heat.factor)) : 0.f;
+    }
+    __syncthreads();
+    if (falls) break;
   }
-  __syncthreads();
-  return decision_sh;
+  const Decision d = decision_sh;
+  if (tells) {
+    for (int row = s.begin + d.step / kRows * kRows + kRows + threadIdx.x; row < s.end; row += kThreads) {
+      p.out[row] = -1;
+      if (p.logp) p.logp[row] = 0.f;
+    }
+    if (threadIdx.x == 0) {
+      p.accepted[u] = d.step;
+      if (p.new_len) p.new_len[u] = p.self_len[u] - (s.end - 1 - d.row);
+    }
+  }
+  return d;
 }
 
-// (w, p) of value i of the row that decides.  Both products are rounded, so that equal distributions leave exactly nothing.
-struct Pair {
-  double w, p;
-};
+// A question without rows.
+__device__ inline void tell_nothing(const VerifyParams& p, int u) {
+  if (threadIdx.x == 0) {
+    p.accepted[u] = 0;
+    if (p.new_len) p.new_len[u] = p.self_len[u];
+  }
+}
 template <typename T, bool kLogits>
-__device__ inline Pair pair_at(const Decision& d, const T* target, const T* draft, int i, double factor) {
+__device__ inline void tell_token(const VerifyParams& p, const Decision& d, int token, double factor) {
+  p.out[d.row] = token;
+  if (p.logp)
+    p.logp[d.row] = token < 0 ? 0.f : static_cast<float>(log_of<kLogits>(at(target_row<T>(p, d.row), token), d.top_p, d.log_p, factor));
+}
+
+// One workgroup: question u.
+template <typename T, bool kLogits>
+__global__ __launch_bounds__(kThreads) void verify_decide_kernel(VerifyParams p, int piece) {
+  const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
+  const int u = blockIdx.x;
+  if (threadIdx.x == 0) w.done[static_cast<int64_t>(u) * kApart] = 0;
+  const Span s = span_of(p, u);
+  if (s.begin == s.end) {
+    if (threadIdx.x == 0) w.decision[u].row = -1;
+    tell_nothing(p, u);
+    return;
+  }
+  const Heat heat = heat_of(p, u);
+  Decision d = decide<T, kLogits>(p, w, u, s, heat, true);
+  if (threadIdx.x > 0) return;
+  if (kLogits && heat.greedy) {
+    tell_token<T, kLogits>(p, d, d.place, heat.factor);
+    d.row = -1;
+  }
+  w.decision[u] = d;
+}
+
+// w of value i of the row that decides.  Both products are rounded, so that equal distributions leave exactly nothing.
+template <bool kLogits>
+__device__ inline double weight_at(const Decision& d, float x, float y, int i, const Scale& of_p, const Scale& of_q) {
 #pragma clang fp contract(off)
-  const float x = at(target, i);
   double a, b = 0.0;
-  if constexpr (kLogits) a = weight_of(x, d.top_p, factor) * d.inv_p;
+  if constexpr (kLogits) a = weight_of(x, of_p) * d.inv_p;
   else a = clean(x);
   if (d.refused == 1) {
-    const float y = at(draft, i);
-    if constexpr (kLogits) b = weight_of(y, d.top_q, factor) * d.inv_q;
+    if constexpr (kLogits) b = weight_of(y, of_q) * d.inv_q;
     else b = clean(y);
   }
-  const double left = d.refused == 2 && i == d.proposal ? 0.0 : fmax(a - b, 0.0);
-  return {left, a};
+  return d.refused == 2 && i == d.proposal ? 0.0 : fmax(a - b, 0.0);
 }
 
 // Exclusive prefix of v over the workgroup, and its total.
 __device__ inline double scan(double v, double& total) {
-  __shared__ double part[kThreads / 64];
+  __shared__ double part[kWaves];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   double up = v;
 #pragma unroll
@@ -354,186 +532,226 @@ __device__ inline double scan(double v, double& total) {
   __syncthreads();
   double before = 0;
   total = 0;
-  for (int i = 0; i < kThreads / 64; ++i) {
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
     if (i < wave) before += part[i];
     total += part[i];
   }
   return before + up - v;
 }
 
-// One workgroup: a share of the row that decides for question u.
-template <typename T, bool kLogits>
-__global__ __launch_bounds__(kThreads) void verify_weigh_kernel(VerifyParams p) {
-  const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab);
-  const int share = static_cast<int>(blockIdx.x % w.shares), u = static_cast<int>(blockIdx.x / w.shares);
-  const Span s = span_of(p, u);
-  if (s.begin == s.end) {
-    if (share == 0 && threadIdx.x == 0) w.decision[u].row = -1;
-    return;
+// Sums go from workgroup to workgroup past the caches in between (stores and loads of the device's scope), and a workgroup is
+// counted once its stores have been acknowledged: nothing else is handed over, so that the count needs no fence, which
+// would write back a whole L2 for each workgroup (64 questions over 102400 words: 76 us instead of 34).
+__device__ inline double left(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline void leave(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline void wait_for_stores() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Threads hold runs of items one after the other, of sums `mine` with `front` in front of them.  The thread in whose run the
+// running sum passes `want`; where none does, the last that has any.  (By ballots: an atomic of many lanes becomes a loop over
+// them, 1.5 us each.)
+__device__ inline int passing_thread(double mine, double front, double want) {
+  __shared__ int found_sh[kWaves], last_sh[kWaves];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const uint64_t any = __ballot(mine > 0), found = __ballot(mine > 0 && front + mine > want);
+  if (lane == 0) {  // (nobody reads these of an earlier call any more: a barrier lies between)
+    found_sh[wave] = found ? wave * 64 + __builtin_ctzll(found) : -1;
+    last_sh[wave] = any ? wave * 64 + 63 - __builtin_clzll(any) : -1;
   }
-  const bool greedy = kLogits && greedy_of(p, u);
-  const double factor = kLogits ? factor_of(p, u, greedy) : 0.0;
-  const Decision d = decide<T, kLogits>(p, w, u, s, greedy, factor);
-  if (share == 0 && threadIdx.x == 0) w.decision[u] = d;
-  if (greedy) return;
-  const T* const target = target_row<T>(p, d.row);
-  const T* const draft = d.refused == 1 ? draft_row<T>(p, u, d.row - s.begin) : nullptr;
-  double weight = 0, plain = 0;
-#pragma unroll 4
-  for (int i = share * kShare + threadIdx.x; i < min((share + 1) * kShare, p.vocab); i += kThreads) {
-    const Pair x = pair_at<T, kLogits>(d, target, draft, i, factor);
-    weight += x.w;
-    plain += x.p;
-  }
-  double all_weight, all_plain;
-  scan(weight, all_weight);
-  scan(plain, all_plain);
-  if (threadIdx.x == 0) {
-    w.weight[static_cast<int64_t>(u) * w.shares + share] = all_weight;
-    w.plain[static_cast<int64_t>(u) * w.shares + share] = all_plain;
-  }
+  __syncthreads();
+  int it = -1;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) it = max(it, last_sh[i]);
+#pragma unroll
+  for (int i = kWaves - 1; i >= 0; --i) it = found_sh[i] >= 0 ? found_sh[i] : it;
+  return it;
 }
 
-// One workgroup: question u.
-template <typename T, bool kLogits>
-__global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
-  const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab);
-  const int u = blockIdx.x;
-  const Span s = span_of(p, u);
-  const int tid = threadIdx.x;
-  __shared__ int token_sh, share_sh, last_sh;
-  __shared__ double before_sh;
-  Decision d = w.decision[u];
-  if (s.begin == s.end) {
-    if (tid == 0) {
-      p.accepted[u] = 0;
-      if (p.new_len) p.new_len[u] = p.self_len[u];
+// One workgroup: shares part * each .. of the row that decides for question u, a wave a share at a time and the next one on its way.
+template <typename T, bool kLogits, bool kDecided>
+__global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, int piece, int parts, int each) {
+  constexpr int kWide = 16 / sizeof(T), kStep = 64 * kWide, kLoads = kShare / kStep;
+  constexpr float kNone = kLogits ? -INFINITY : 0.f;
+  const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
+  const int part = blockIdx.x % parts, u = blockIdx.x / parts, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  __shared__ bool last_sh;
+  __shared__ int chosen_sh;
+  __shared__ double before_sh, weight_sh[kShare];
+  const Heat heat = heat_of(p, u);
+  Decision d;
+  if constexpr (kDecided) {
+    d = w.decision[u];
+    if (d.row < 0) return;
+  } else {
+    const Span s = span_of(p, u);
+    const bool greedy = kLogits && heat.greedy;
+    if (greedy && part > 0) return;  // (nothing to weigh)
+    if (s.begin == s.end) {
+      if (part == 0) tell_nothing(p, u);
+      return;
     }
-    return;
+    d = decide<T, kLogits>(p, w, u, s, heat, part == 0);
+    if (greedy) {
+      if (tid == 0) tell_token<T, kLogits>(p, d, d.place, heat.factor);
+      return;
+    }
   }
-  const bool greedy = kLogits && greedy_of(p, u);
-  const double factor = kLogits ? factor_of(p, u, greedy) : 0.0;
-  int token = d.token;
-  if (!greedy) {
-    const double* sums = w.weight + static_cast<int64_t>(u) * w.shares;
-    double total = 0;
-    for (int i = tid; i < w.shares; i += kThreads) total += sums[i];
-    double all;
-    scan(total, all);
-    if (!(all > 0)) {  // the target lies nowhere above what proposed
-      d.refused = 0;
-      sums = w.plain + static_cast<int64_t>(u) * w.shares;
-      total = 0;
-      for (int i = tid; i < w.shares; i += kThreads) total += sums[i];
-      scan(total, all);
-    }
-    if (all > 0) {
-      const double want = static_cast<double>(p.uniform[s.end - 1]) * all;
-      // the share in which the running sum passes `want`; behind the last, the last that has any
-      if (tid == 0) {
-        share_sh = INT32_MAX;
-        last_sh = 0;
-        token_sh = p.vocab;
-      }
-      double before = 0;
-      for (int i = 0; i < w.shares; i += kThreads) {
-        const double here = i + tid < w.shares ? sums[i + tid] : 0.0;
-        double round;
-        const double mine = before + scan(here, round);  // (its barriers are behind the lines above, and the last round's)
-        if (here > 0) atomicMax(&last_sh, i + tid);
-        if (here > 0 && mine + here > want) atomicMin(&share_sh, i + tid);
-        __syncthreads();
-        if (i + tid == share_sh || (share_sh == INT32_MAX && i + tid == last_sh)) before_sh = mine;
-        before += round;
-        if (share_sh != INT32_MAX) break;
-      }
-      __syncthreads();
-      const int share = share_sh != INT32_MAX ? share_sh : last_sh;
-      const T* const target = target_row<T>(p, d.row);
-      const T* const draft = d.refused == 1 ? draft_row<T>(p, u, d.row - s.begin) : nullptr;
-      constexpr int kMine = kShare / kThreads;
-      const int first = share * kShare + tid * kMine;
-      double mine[kMine], sum = 0;
-      int last = -1;
+  const T* const target = target_row<T>(p, d.row);
+  const T* const draft = d.refused == 1 ? draft_row<T>(p, u, d.step) : target;
+  double* const sums = w.weight + static_cast<int64_t>(u) * w.shares;
+  const Scale of_p = kLogits ? scale_of(d.top_p, heat.factor) : Scale{}, of_q = kLogits ? scale_of(d.top_q, heat.factor) : Scale{};
+  // phase 0: the workgroup's shares; 1: the sums are there, and the share that the token lies in is gone through again (the same
+  // instructions: what runs for the first time waits for them); 2: the target lies nowhere above what proposed, the last workgroup
+  // goes through all of the target alone
+  int share_begin = part * each, share_end = min(share_begin + each, w.shares), phase = 0;
+  double want = 0;
+  for (;;) {
+    const bool again = phase == 1;
+    const int end = again ? share_begin + 1 : share_end;
+    int share = share_begin + wave;
+    uintx4 of_target[kLoads], of_draft[kLoads];
+    if (share < end) {
 #pragma unroll
-      for (int e = 0; e < kMine; ++e) {
-        mine[e] = first + e < p.vocab ? pair_at<T, kLogits>(d, target, draft, first + e, factor).w : 0.0;
-        sum += mine[e];
-        if (mine[e] > 0) last = first + e;
+      for (int k = 0; k < kLoads; ++k) {
+        of_target[k] = load_wide(target, share * kShare + k * kStep + lane * kWide, p.vocab);
+        of_draft[k] = load_wide(draft, share * kShare + k * kStep + lane * kWide, p.vocab);
       }
-      double unused, run = before_sh + scan(sum, unused);
-      int found = p.vocab;
-#pragma unroll
-      for (int e = 0; e < kMine; ++e) {
-        run += mine[e];
-        if (found == p.vocab && run > want && mine[e] > 0) found = first + e;
-      }
-      found = wave_min(found);
-      if (tid % 64 == 0) atomicMin(&token_sh, found);
-      __syncthreads();
-      token = token_sh;
-      if (token == p.vocab) {  // (by rounding, or a number of 1 and more)
-        __syncthreads();
-        if (tid == 0) token_sh = -1;
-        __syncthreads();
-        last = -wave_min(-last);
-        if (tid % 64 == 0) atomicMax(&token_sh, last);
-        __syncthreads();
-        token = token_sh;
-      }
-    } else {
-      token = -1;
     }
-  }
-  for (int row = s.begin + tid; row < s.end; row += kThreads)
-    p.out[row] = row < d.row ? p.tokens[row + 1] : row == d.row ? token : -1;
-  if (tid == 0) {
-    p.accepted[u] = d.stands;
-    if (p.new_len) p.new_len[u] = p.self_len[u] - (s.end - 1 - d.row);
-  }
-  if (p.logp) {
-    for (int row = s.begin + tid / 64; row < s.end; row += kThreads / 64) {
-      double lp = 0;
-      const int x = row < d.row ? p.tokens[row + 1] : row == d.row ? token : -1;
-      if (x >= 0) {
-        const float v = at(target_row<T>(p, row), x);
-        if constexpr (kLogits) {
-          const RowStats a = row_stats(w, row, factor);
-          lp = (a.top == INFINITY ? 0.0 : (static_cast<double>(v) - static_cast<double>(a.top)) * factor * 0.69314718055994530942) - log(a.sum);
-        } else {
-          lp = log(clean(v));
+    while (share < end) {
+      const int first = share * kShare + lane * kWide, next = share + kWaves;
+      float x[kLoads][kWide], y[kLoads][kWide];
+      if ((share + 1) * kShare <= p.vocab) {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+          widen_all<T>(of_target[k], x[k]);
+          widen_all<T>(of_draft[k], y[k]);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+          values_of(of_target[k], target, first + k * kStep, p.vocab, kNone, x[k]);
+          values_of(of_draft[k], draft, first + k * kStep, p.vocab, kNone, y[k]);
         }
       }
-      if (tid % 64 == 0) p.logp[row] = static_cast<float>(lp);
+      if (next < end) {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+          of_target[k] = load_wide(target, next * kShare + k * kStep + lane * kWide, p.vocab);
+          of_draft[k] = load_wide(draft, next * kShare + k * kStep + lane * kWide, p.vocab);
+        }
+      }
+      double sum = 0;
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k)
+#pragma unroll
+        for (int e = 0; e < kWide; ++e) {
+          const double here = weight_at<kLogits>(d, x[k][e], y[k][e], first + k * kStep + e, of_p, of_q);
+          sum += here;
+          if (again) weight_sh[k * kStep + lane * kWide + e] = here;
+        }
+      if (!again) {
+        sum = wave_sum(sum);
+        if (lane == 0) leave(sums + share, sum);
+      }
+      share = next;
     }
+    if (again) break;
+    wait_for_stores();
+    __syncthreads();
+    if (phase == 0) {
+      if (tid == 0)
+        last_sh = __hip_atomic_fetch_add(w.done + static_cast<int64_t>(u) * kApart, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == static_cast<unsigned>(parts - 1);
+      __syncthreads();
+      if (!last_sh) return;
+    }
+    const int run = (w.shares + kThreads - 1) / kThreads;
+    double mine = 0, all;
+    for (int i = tid * run; i < min(tid * run + run, w.shares); ++i) mine += left(sums + i);
+    const double front = scan(mine, all);
+    if (!(all > 0)) {
+      if (phase == 2 || d.refused == 0) {
+        if (tid == 0) tell_token<T, kLogits>(p, d, -1, heat.factor);
+        return;
+      }
+      d.refused = 0;
+      share_begin = 0;
+      share_end = w.shares;
+      phase = 2;
+      continue;
+    }
+    want = static_cast<double>(d.number) * all;
+    if (tid == passing_thread(mine, front, want)) {
+      double before = front, at_last = front;
+      int chosen = 0;
+      for (int i = tid * run; i < min(tid * run + run, w.shares); ++i) {
+        const double here = run == 1 ? mine : left(sums + i);
+        if (!(here > 0)) continue;
+        chosen = i;
+        at_last = before;
+        before += here;
+        if (before > want) break;
+      }
+      chosen_sh = chosen;
+      before_sh = at_last;
+    }
+    __syncthreads();
+    share_begin = chosen_sh;
+    phase = 1;
   }
+  __syncthreads();
+  constexpr int kMine = kShare / kThreads;
+  double mine = 0, all;
+#pragma unroll
+  for (int e = 0; e < kMine; ++e) mine += weight_sh[tid * kMine + e];
+  const double front = before_sh + scan(mine, all);
+  if (tid != passing_thread(mine, front, want)) return;
+  double before = front;
+  int token = 0;
+  for (int e = 0; e < kMine; ++e) {
+    const double here = weight_sh[tid * kMine + e];
+    if (!(here > 0)) continue;
+    token = share_begin * kShare + tid * kMine + e;
+    before += here;
+    if (before > want) break;
+  }
+  tell_token<T, kLogits>(p, d, token, heat.factor);
 }
 
-template <typename T>
-void launch(const VerifyParams& p, bool logits, hipStream_t stream) {
-  const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab);
+template <typename T, bool kLogits>
+void launch(const VerifyParams& p, hipStream_t stream) {
+  const int64_t rows = (p.draft ? 2 : 1) * static_cast<int64_t>(p.n_tokens);
+  const int piece = rows * p.vocab >= int64_t{1} << 25 ? 4 * kPieceLeast : kPieceLeast;
+  const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
   const dim3 threads(kThreads);
-  if (logits) {
-    const int64_t rows = (p.draft ? 2 : 1) * static_cast<int64_t>(p.n_tokens);
-    if (rows > 0) verify_stats_kernel<T><<<dim3(static_cast<unsigned>(rows * w.pieces)), threads, 0, stream>>>(p);
-    verify_weigh_kernel<T, true><<<dim3(static_cast<unsigned>(p.n_queries * w.shares)), threads, 0, stream>>>(p);
-    verify_pick_kernel<T, true><<<dim3(p.n_queries), threads, 0, stream>>>(p);
+  // shares of a workgroup, a multiple of its waves
+  const int64_t most = pieces_of(w.shares, kWaves), per = (p.n_queries * most + 2047) / 2048;
+  const int each = static_cast<int>(per * kWaves), parts = static_cast<int>(pieces_of(w.shares, each));
+  const bool apart = static_cast<int64_t>(p.n_queries) * parts > 512;
+  if (kLogits && rows > 0) {
+    const int64_t cells = rows * w.pieces;
+    verify_stats_kernel<T><<<dim3(static_cast<unsigned>((cells + kWaves - 1) / kWaves)), threads, 0, stream>>>(p, piece);
+  } else if (!apart) {
+    verify_clear_kernel<<<dim3((p.n_queries + kThreads - 1) / kThreads), threads, 0, stream>>>(p, piece);
+  }
+  const dim3 grid(static_cast<unsigned>(p.n_queries) * parts);
+  if (apart) {
+    verify_decide_kernel<T, kLogits><<<dim3(p.n_queries), threads, 0, stream>>>(p, piece);
+    verify_draw_kernel<T, kLogits, true><<<grid, threads, 0, stream>>>(p, piece, parts, each);
   } else {
-    verify_weigh_kernel<T, false><<<dim3(static_cast<unsigned>(p.n_queries * w.shares)), threads, 0, stream>>>(p);
-    verify_pick_kernel<T, false><<<dim3(p.n_queries), threads, 0, stream>>>(p);
+    verify_draw_kernel<T, kLogits, false><<<grid, threads, 0, stream>>>(p, piece, parts, each);
   }
 }
 
 }  // namespace
 
 size_t verify_workspace_bytes(int64_t n_tokens, int64_t n_queries, int64_t vocab) {
-  const Work w = work_of(nullptr, n_tokens, n_queries, vocab);
-  const size_t all = reinterpret_cast<size_t>(w.place) + static_cast<size_t>(2 * n_tokens * w.pieces) * 4;
+  const Work w = work_of(nullptr, n_tokens, n_queries, vocab, kPieceLeast);
+  const size_t all = reinterpret_cast<size_t>(w.done) + static_cast<size_t>(n_queries) * kApart * 4;
   return (all + 15) / 16 * 16;
 }
 
 hipError_t launch_verify(const VerifyParams& p, bool bf16, bool logits, hipStream_t stream) {
-  if (bf16) launch<__bf16>(p, logits, stream);
-  else launch<float>(p, logits, stream);
+  if (bf16) logits ? launch<__bf16, true>(p, stream) : launch<__bf16, false>(p, stream);
+  else logits ? launch<float, true>(p, stream) : launch<float, false>(p, stream);
   return hipGetLastError();
 }
