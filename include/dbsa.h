@@ -688,7 +688,7 @@ typedef struct {
   int32_t* table;      /* device [n_queries][table_stride]                                   */
   int32_t* refs;       /* device [n_pages]                                                   */
   int32_t* self_len;   /* device [n_queries], counted from 0 to what a row of the table holds */
-  int32_t n_queries;   /* at most 8192                                                       */
+  int32_t n_queries;   /* at most 4096                                                       */
   int32_t table_stride;/* at most 2^24                                                       */
   int32_t page_tokens; /* a power of two, at least 16                                        */
   int32_t n_pages;

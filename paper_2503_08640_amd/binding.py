@@ -783,8 +783,14 @@ def dbsa_kv8_read(k8, v8, k_scale, v_scale, rows=None, first_row: int = 0, n_tok
 # proposed tokens, pages of the caches
 # ---------------------------------------------------------------------------
 
-def _ints(t, n: int) -> bool:
-    return t.dim() == 1 and t.shape[0] == n and _int32(t)
+@functools.lru_cache(maxsize=None)
+def _i32_type():
+    import torch
+    return torch.int32
+
+
+def _ints(t, *shape) -> bool:
+    return t.shape == shape and t.dtype is _i32_type() and t.is_contiguous()
 
 
 def dbsa_draft_verify_workspace_bytes(n_tokens: int, n_queries: int, vocab: int) -> int:
@@ -799,27 +805,27 @@ def dbsa_draft_verify(target, tokens, cu_qlens, uniform, draft=None, temperature
     at ``temperature`` float32 [B] (None: 1; 0: greedy), or probabilities if ``probs``.  ``logp`` float32 [sum T] receives the log
     probabilities, ``new_len`` int32 [B] the own keys of ``self_len`` that stay."""
     import torch
-    shape, n, b = target.shape, tokens.shape[0], cu_qlens.shape[0] - 1
-    assert len(shape) == 2 and shape[0] == n and target.stride(1) == 1, "expected scores [sum T, V], V contiguous"
+    (rows, vocab), n, b = target.shape, tokens.numel(), cu_qlens.numel() - 1
+    assert rows == n and target.stride(1) == 1, "expected scores [sum T, V], V contiguous"
     assert b >= 1 and _ints(tokens, n) and _ints(cu_qlens, b + 1), "expected contiguous int32 tokens [sum T] and cu_qlens [B + 1]"
     for t, m in ((uniform, n), (temperature, b), (logp, n)):
-        assert t is None or (t.dtype == torch.float32 and t.shape == (m,) and t.is_contiguous()), "expected contiguous float32 numbers"
+        assert t is None or (t.shape == (m,) and t.dtype is torch.float32 and t.is_contiguous()), "expected contiguous float32 numbers"
     out = torch.empty_like(tokens) if out is None else out
     accepted = torch.empty_like(cu_qlens[1:]) if accepted is None else accepted
     assert _ints(out, n) and _ints(accepted, b)
     assert (self_len is None) == (new_len is None) and (self_len is None or (_ints(self_len, b) and _ints(new_len, b)))
     d = None
     if draft is not None and draft.shape[1] > 0:
-        s = draft.stride()
-        assert draft.dtype == target.dtype and draft.shape[0] == b and draft.shape[2] == shape[1] and s[2] == 1, "expected draft scores [B, steps, V]"
-        d = C.byref(Draft(draft.data_ptr(), s[0], s[1], draft.shape[1]))
+        s, (questions, steps, words) = draft.stride(), draft.shape
+        assert draft.dtype is target.dtype and questions == b and words == vocab and s[2] == 1, "expected draft scores [B, steps, V]"
+        d = C.byref(Draft(draft.data_ptr(), s[0], s[1], steps))
     if workspace is None:
-        workspace = torch.empty(max(16, dbsa_draft_verify_workspace_bytes(n, b, shape[1])), dtype=torch.uint8, device=target.device)
+        workspace = torch.empty(max(16, dbsa_draft_verify_workspace_bytes(n, b, vocab)), dtype=torch.uint8, device=target.device)
     stream = _here(target, tokens, cu_qlens, uniform, draft, temperature, out, accepted, logp, self_len, new_len, workspace)
-    rc = lib().dbsa_draft_verify(target.data_ptr(), target.stride(0), d, tokens.data_ptr(), cu_qlens.data_ptr(), n, b, shape[1],
+    rc = lib().dbsa_draft_verify(target.data_ptr(), target.stride(0), d, tokens.data_ptr(), cu_qlens.data_ptr(), n, b, vocab,
                                  _dtype_code(target), DBSA_PROBABILITIES if probs else DBSA_LOGITS, _at(temperature), uniform.data_ptr(),
                                  out.data_ptr(), accepted.data_ptr(), _at(logp), _at(self_len), _at(new_len), workspace.data_ptr(),
-                                 workspace.numel() * workspace.element_size(), stream)
+                                 workspace.nbytes, stream)
     _check(rc, "dbsa_draft_verify")
     return out, accepted
 
@@ -827,9 +833,10 @@ def dbsa_draft_verify(target, tokens, cu_qlens, uniform, draft=None, temperature
 def _book(page_table, refs, self_len, page_tokens: int):
     """The books of an arena: page_table int32 [B, pages of a question], refs int32 [pages], self_len int32 [B]."""
     b, columns = page_table.shape
-    assert _int32(page_table) and refs.dim() == 1 and _int32(refs), "expected a contiguous int32 page table and counts"
+    n = refs.numel()
+    assert _ints(page_table, b, columns) and _ints(refs, n), "expected a contiguous int32 page table and counts"
     assert self_len is None or _ints(self_len, b), "expected contiguous int32 lengths [B]"
-    return C.byref(PageBook(page_table.data_ptr(), refs.data_ptr(), _at(self_len), b, columns, int(page_tokens), refs.shape[0]))
+    return C.byref(PageBook(page_table.data_ptr(), refs.data_ptr(), _at(self_len), b, columns, page_tokens, n))
 
 
 def dbsa_pages_fork(page_table, refs, self_len, source, page_tokens: int) -> None:
@@ -849,10 +856,10 @@ def dbsa_pages_reserve(page_table, refs, self_len, add, page_tokens: int, got=No
     copies = torch.empty((b, 3), dtype=torch.int32, device=add.device) if copies is None else copies
     n_copies = torch.empty(1, dtype=torch.int32, device=add.device) if n_copies is None else n_copies
     workspace = torch.empty_like(refs) if workspace is None else workspace
-    assert _ints(add, b) and _ints(got, b) and _ints(n_copies, 1) and copies.shape == (b, 3) and _int32(copies)
+    assert _ints(add, b) and _ints(got, b) and _ints(n_copies, 1) and _ints(copies, b, 3)
     stream = _here(page_table, refs, self_len, add, got, copies, n_copies, workspace)
     rc = lib().dbsa_pages_reserve(book, add.data_ptr(), got.data_ptr(), copies.data_ptr(), n_copies.data_ptr(), workspace.data_ptr(),
-                                  workspace.numel() * workspace.element_size(), stream)
+                                  workspace.nbytes, stream)
     _check(rc, "dbsa_pages_reserve")
     return got, copies, n_copies
 
@@ -868,16 +875,16 @@ def dbsa_pages_compact(refs, page_table, page_tokens: int, copies=None, counts=N
     """-> (copies int32 [n, 3], counts int32 [2] = (copies, pages in use), new_place int32 [pages]): the pages in use move to the front of
     the arena; refs and page_table (None: the caller renames its tables) change in place, the caches by dbsa_pages_copy."""
     import torch
-    n = refs.shape[0]
+    n = refs.numel()
     if page_table is None:
-        assert refs.dim() == 1 and _int32(refs), "expected contiguous int32 counts"
-        book = C.byref(PageBook(None, refs.data_ptr(), None, 0, 0, int(page_tokens), n))
+        assert _ints(refs, n), "expected contiguous int32 counts"
+        book = C.byref(PageBook(None, refs.data_ptr(), None, 0, 0, page_tokens, n))
     else:
         book = _book(page_table, refs, None, page_tokens)
     copies = torch.empty((max(1, n // 2), 3), dtype=torch.int32, device=refs.device) if copies is None else copies
     counts = torch.empty(2, dtype=torch.int32, device=refs.device) if counts is None else counts
     new_place = torch.empty_like(refs) if new_place is None else new_place
-    assert copies.shape == (max(1, n // 2), 3) and _int32(copies) and _ints(counts, 2) and _ints(new_place, n)
+    assert _ints(copies, max(1, n // 2), 3) and _ints(counts, 2) and _ints(new_place, n)
     stream = _here(refs, page_table, copies, counts, new_place)
     _check(lib().dbsa_pages_compact(book, copies.data_ptr(), counts.data_ptr(), new_place.data_ptr(), stream), "dbsa_pages_compact")
     return copies, counts, new_place
@@ -888,7 +895,7 @@ def dbsa_pages_copy(k_pages, v_pages, copies, n_copies) -> None:
     D], or [layers, pages, page tokens, Hkv, D]; bf16, float32 or 8 bits."""
     s, shape = k_pages.stride(), k_pages.shape
     assert len(shape) in (4, 5) and s[-1] == 1 and v_pages.stride() == s and v_pages.shape == shape and v_pages.dtype == k_pages.dtype
-    assert copies.dim() == 2 and copies.shape[1] == 3 and _int32(copies) and _int32(n_copies) and n_copies.numel() >= 1
+    assert _ints(copies, copies.shape[0], 3) and _int32(n_copies) and n_copies.numel() >= 1
     layers, apart = (shape[0], s[0]) if len(shape) == 5 else (1, 0)
     pages = Pages(Tensor(k_pages.data_ptr(), s[-3], s[-2]), Tensor(v_pages.data_ptr(), s[-3], s[-2]), s[-4], None, 0, shape[-3], shape[-4])
     dtype = DBSA_E4M3 if k_pages.element_size() == 1 else _dtype_code(k_pages)

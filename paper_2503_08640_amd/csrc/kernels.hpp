@@ -187,7 +187,7 @@ struct BookParams {
   int32_t *table, *refs, *self_len;
   int32_t n_queries, table_stride, page_log2, n_pages;
 };
-constexpr int kBookQuestions = 8192;  // most rows of a table
+constexpr int kBookQuestions = 4096;  // most rows of a table
 hipError_t launch_pages_fork(const BookParams& p, const int32_t* source, hipStream_t stream);
 hipError_t launch_pages_reserve(const BookParams& p, const int32_t* add, int32_t* got, int32_t* copies, int32_t* n_copies, int32_t* spare,
                                 hipStream_t stream);

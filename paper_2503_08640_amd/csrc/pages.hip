@@ -8,6 +8,7 @@
 namespace {
 
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
 
 __device__ inline bool is_page(int entry, const BookParams& p) { return entry >= 0 && entry < p.n_pages; }
 
@@ -23,30 +24,55 @@ __device__ inline int pages_for(int64_t tokens, const BookParams& p) {
 
 // ---- fork ------------------------------------------------------------------------------------------------------
 
-// A workgroup takes a range of columns of all rows: what a row's copy reads of a column is in LDS before any row of that
-// column is written, so that rows may go round in a circle.  Counts: integer atomics, whose order does not matter.
-__global__ __launch_bounds__(256) void pages_fork_kernel(BookParams p, const int32_t* source, int columns) {
-  extern __shared__ int copy_sh[];
-  const int first = blockIdx.x * columns, here = min(columns, p.table_stride - first);
-  const int n = p.n_queries * here;
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const int u = i / here, c = first + i % here, s = source[u];
-    if (s < 0 || s >= p.n_queries || s == u) continue;
-    const int old = p.table[static_cast<int64_t>(u) * p.table_stride + c];
-    int now = c < pages_for(tokens_of(p, s), p) ? p.table[static_cast<int64_t>(s) * p.table_stride + c] : -1;
-    if (!is_page(now, p)) now = -1;
-    copy_sh[i] = now;
-    if (now != old) {
-      if (is_page(old, p)) atomicAdd(p.refs + old, -1);
-      if (now >= 0) atomicAdd(p.refs + now, 1);
-    }
+constexpr int kForkEach = 8;  // entries of a thread
+
+// A workgroup takes 2^columns_log2 columns of all rows: what the copies read of a column is in registers before any row of that
+// column is written, so that rows may go round in a circle.  The counts are what takes its time (device-wide integer atomics, 13e9 a
+// second; their order does not matter), so that an entry's whole change is one: the copies made of its row less the row's own loss
+// of it.  alone: the one workgroup of the launch, which sees to the lengths as well.
+__global__ __launch_bounds__(1024) void pages_fork_kernel(BookParams p, const int32_t* source, int columns_log2, bool alone) {
+  __shared__ int used_sh[kBookQuestions];         // pages of a row's tokens
+  __shared__ int copies_sh[kBookQuestions];       // copies made of the row
+  __shared__ uint16_t source_sh[kBookQuestions];  // kStays: the row stays as it is
+  constexpr uint16_t kStays = 0xffff;
+  const int tid = threadIdx.x;
+  for (int u = tid; u < p.n_queries; u += 1024) {
+    copies_sh[u] = 0;
+    used_sh[u] = pages_for(tokens_of(p, u), p);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const int u = i / here, c = first + i % here, s = source[u];
-    if (s < 0 || s >= p.n_queries || s == u) continue;
-    p.table[static_cast<int64_t>(u) * p.table_stride + c] = copy_sh[i];
+  int length = 0;
+  for (int u = tid; u < p.n_queries; u += 1024) {
+    const int s = source[u];
+    const bool forks = s >= 0 && s < p.n_queries && s != u;
+    source_sh[u] = forks ? static_cast<uint16_t>(s) : kStays;
+    if (forks) atomicAdd(&copies_sh[s], 1);
+    if (alone && forks) length = p.self_len[s];  // (alone: a thread has one row at most)
   }
+  __syncthreads();
+  const int c = (blockIdx.x << columns_log2) + (tid & ((1 << columns_log2) - 1)), first = tid >> columns_log2, step = 1024 >> columns_log2;
+  int old[kForkEach], now[kForkEach];
+#pragma unroll
+  for (int i = 0; i < kForkEach; ++i) {
+    const int u = first + i * step;
+    old[i] = now[i] = -1;
+    if (u >= p.n_queries || c >= p.table_stride) continue;
+    const int s = source_sh[u];
+    if (s != kStays || copies_sh[u] > 0) old[i] = p.table[static_cast<int64_t>(u) * p.table_stride + c];
+    if (s != kStays && c < used_sh[s]) now[i] = p.table[static_cast<int64_t>(s) * p.table_stride + c];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kForkEach; ++i) {
+    const int u = first + i * step;
+    if (u >= p.n_queries || c >= p.table_stride) continue;
+    const bool forks = source_sh[u] != kStays;
+    const int change = (c < used_sh[u] ? copies_sh[u] : 0) - forks;
+    if (is_page(old[i], p) && change != 0) atomicAdd(p.refs + old[i], change);
+    if (!is_page(now[i], p)) now[i] = -1;
+    if (forks && now[i] != old[i]) p.table[static_cast<int64_t>(u) * p.table_stride + c] = now[i];
+  }
+  if (alone && tid < p.n_queries && source_sh[tid] != kStays) p.self_len[tid] = length;
 }
 
 __global__ __launch_bounds__(1024) void pages_fork_lengths_kernel(BookParams p, const int32_t* source) {
@@ -59,9 +85,9 @@ __global__ __launch_bounds__(1024) void pages_fork_lengths_kernel(BookParams p, 
   }
 }
 
-// ---- reserve ---------------------------------------------------------------------------------------------------
+// ---- what one workgroup of 1024 threads shares -----------------------------------------------------------------
 
-// Exclusive prefix over the workgroup's 1024 threads, and the total.
+// Exclusive prefix over the workgroup, and the total.
 __device__ inline uint64_t scan1024(uint64_t v, uint64_t& total) {
   __shared__ uint64_t part[16];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -74,15 +100,41 @@ __device__ inline uint64_t scan1024(uint64_t v, uint64_t& total) {
   __syncthreads();
   if (lane == 63) part[wave] = up;
   __syncthreads();
-  uint64_t before = 0;
-  total = 0;
+  // (a wave adds the sixteen up by its lanes: kept apart in every thread they take its registers)
+  uint64_t sum = lane < 16 ? part[lane] : 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    if (i < wave) before += part[i];
-    total += part[i];
+  for (int s = 1; s < 16; s <<= 1) {
+    const uint64_t other = __shfl_up(sum, s);
+    if (lane >= s) sum += other;
   }
-  return before + up - v;
+  total = __shfl(sum, 15);
+  return (wave > 0 ? __shfl(sum, wave - 1) : 0) + up - v;
 }
+
+// Which of the kEach pages from the first-th on are in use; those behind the last count as used and, in `there`, as not there.
+template <int kEach>
+__device__ inline void refs_of(const BookParams& p, int64_t first, int (&r)[kEach]) {
+  if (first + kEach <= p.n_pages && reinterpret_cast<uintptr_t>(p.refs) % 16 == 0) {
+#pragma unroll
+    for (int e = 0; e < kEach; e += 4) {
+      const intx4 v = *reinterpret_cast<const intx4*>(p.refs + first + e);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) r[e + k] = v[k];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) r[e] = first + e < p.n_pages ? p.refs[first + e] : INT32_MAX;
+  }
+}
+template <int kEach>
+__device__ inline unsigned free_of(const int (&r)[kEach]) {
+  unsigned free = 0;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) free |= (r[e] <= 0 ? 1u : 0u) << e;
+  return free;
+}
+
+// ---- reserve ---------------------------------------------------------------------------------------------------
 
 // What question u asks for.
 struct Ask {
@@ -92,9 +144,9 @@ struct Ask {
   int first, behind;  // pages the new tokens reach into, behind the last one in use
   bool fits;
 };
-__device__ inline Ask ask_of(const BookParams& p, const int32_t* add, int u) {
+__device__ inline Ask ask_of(const BookParams& p, int length, int add, int u) {
   Ask a;
-  const int64_t n = p.self_len[u] < 0 ? 0 : p.self_len[u], more = add[u];
+  const int64_t n = length < 0 ? 0 : length, more = add;
   a.tokens = n;
   a.rows = static_cast<int>(n & ((int64_t{1} << p.page_log2) - 1));
   a.tail = -1;
@@ -115,135 +167,175 @@ __device__ inline Ask ask_of(const BookParams& p, const int32_t* add, int u) {
   return a;
 }
 
-// One workgroup, in the order of the questions: what each asks for, the pages it gets, the books.
+constexpr int kNarrow = 4;     // entries that the thread of a question looks at by itself; more: sixteen lanes
+constexpr int kSpareSh = 8192; // free pages that are kept in LDS
+
+// One workgroup, in the order of the questions, kQ of them to a thread: what each asks for, the pages it gets, the books.  A chain
+// of loads (lengths, entries, counts of the last pages); the first 8192 counts are asked for in front of it.
+template <int kQ>
 __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const int32_t* add, int32_t* got, int32_t* copies,
                                                             int32_t* n_copies, int32_t* spare) {
-  __shared__ int tail_sh[kBookQuestions];   // the last page that question u would write to, -1 if none
-  __shared__ int lacks_sh[kBookQuestions];  // entries that name no page yet; the lowest bit: the last page is to be replaced
-  __shared__ int copied_sh;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  if (tid == 0) copied_sh = 0;
-  // (a wave to a question where many entries are looked at, a thread to a question else)
-  for (int base = wave * 64; base < p.n_queries; base += 1024) {
-    const int u = base + lane;
-    Ask a{};
-    int lacks = 0;
+  constexpr int kEach = 8;
+  __shared__ __align__(16) int tail_sh[1024 * kQ];  // the last page that question u would write to, -1 if none
+  __shared__ int lacks_sh[1024 * kQ];               // wide questions: entries that name no page yet; then, where their pages begin
+  __shared__ uint16_t wide_sh[1024 * kQ];           // questions with many entries to look at, and which
+  __shared__ int wide_first_sh[1024 * kQ], wide_behind_sh[1024 * kQ];
+  __shared__ int spare_sh[kSpareSh];
+  __shared__ int wide_count_sh;
+  const int tid = threadIdx.x, lane = tid % 64;
+  int r[kEach];
+  refs_of<kEach>(p, static_cast<int64_t>(tid) * kEach, r);
+  if (tid == 0) wide_count_sh = 0;
+  Ask a[kQ];
+  int more[kQ], lacks[kQ];
+#pragma unroll
+  for (int i = 0; i < kQ; ++i) {
+    const int u = tid * kQ + i;
+    a[i] = Ask{};
+    a[i].tail = -1;
+    more[i] = lacks[i] = 0;
     if (u < p.n_queries) {
-      a = ask_of(p, add, u);
-      tail_sh[u] = a.tail;
-      if (a.behind - a.first <= 4)
-        for (int c = a.first; c < a.behind; ++c) lacks += !is_page(p.table[static_cast<int64_t>(u) * p.table_stride + c], p);
+      more[i] = add[u];
+      a[i] = ask_of(p, p.self_len[u], more[i], u);
     }
-    uint64_t many = __ballot(u < p.n_queries && a.behind - a.first > 4);
-    while (many) {
-      const int who = __ffsll(static_cast<unsigned long long>(many)) - 1;
-      many &= many - 1;
-      const int first = __shfl(a.first, who), behind = __shfl(a.behind, who);
-      int all = 0;
-      for (int c = first; c < behind; c += 64)
-        all += __popcll(__ballot(c + lane < behind && !is_page(p.table[static_cast<int64_t>(base + who) * p.table_stride + min(c + lane, behind - 1)], p)));
-      if (lane == who) lacks = all;
-    }
-    if (u < p.n_queries) lacks_sh[u] = 2 * lacks;
   }
   __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kQ; ++i) {
+    const int u = tid * kQ + i, wide = a[i].behind - a[i].first;
+    if (wide > 0 && wide <= kNarrow) {
+      const int32_t* const row = p.table + static_cast<int64_t>(u) * p.table_stride;
+#pragma unroll
+      for (int c = 0; c < kNarrow; ++c) lacks[i] += c < wide && !is_page(row[min(a[i].first + c, a[i].behind - 1)], p);
+    }
+    const uint64_t many = __ballot(wide > kNarrow);
+    if (many) {
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&wide_count_sh, __popcll(many));
+      at = __shfl(at, 0) + __popcll(many & ((uint64_t{1} << lane) - 1));
+      if (wide > kNarrow) {
+        wide_sh[at] = static_cast<uint16_t>(u);
+        wide_first_sh[at] = a[i].first;
+        wide_behind_sh[at] = a[i].behind;
+      }
+    }
+    tail_sh[u] = a[i].tail;
+  }
+  __syncthreads();
+  const int n_wide = wide_count_sh;
+  for (int i = tid / 16; i < n_wide; i += 64) {
+    const int u = wide_sh[i], behind = wide_behind_sh[i];
+    const int32_t* const row = p.table + static_cast<int64_t>(u) * p.table_stride;
+    int n = 0;
+#pragma unroll 2
+    for (int c = wide_first_sh[i] + tid % 16; c < behind; c += 16) n += !is_page(row[c], p);
+#pragma unroll
+    for (int s = 8; s > 0; s >>= 1) n += __shfl_xor(n, s);
+    if (tid % 16 == 0) lacks_sh[u] = n;
+  }
   // a page that several name is replaced while, behind the replacements of earlier questions, more than one still does
-  for (int u = tid; u < p.n_queries; u += 1024) {
-    const int tail = tail_sh[u];
-    if (tail < 0) continue;
-    const int count = p.refs[tail];
-    if (count <= 1) continue;
+  bool replaced[kQ];
+#pragma unroll
+  for (int i = 0; i < kQ; ++i) {
+    const int u = tid * kQ + i, tail = a[i].tail;
+    const int count = tail >= 0 ? p.refs[tail] : 0;
     int before = 0;
-    for (int v = 0; v < u; ++v) before += tail_sh[v] == tail;
-    if (count - before > 1) lacks_sh[u] |= 1;
+    if (count > 1) {
+      int v = 0;
+#pragma unroll 2
+      for (; v + 4 <= u; v += 4) {
+        const intx4 t = *reinterpret_cast<const intx4*>(tail_sh + v);
+        before += (t[0] == tail) + (t[1] == tail) + (t[2] == tail) + (t[3] == tail);
+      }
+#pragma unroll 1
+      for (; v < u; ++v) before += tail_sh[v] == tail;
+    }
+    replaced[i] = count - before > 1;
   }
-  __syncthreads();
-  uint64_t total = 0;  // pages asked for
-  for (int base = 0; base < p.n_queries; base += 1024) {
-    const int u = base + tid;
-    uint64_t all;
-    scan1024(u < p.n_queries ? (lacks_sh[u] >> 1) + (lacks_sh[u] & 1) : 0, all);
-    total += all;
+  __syncthreads();  // (lacks_sh of the wide questions)
+  constexpr uint64_t kOne = (uint64_t{1} << 48) + 1, low = (uint64_t{1} << 48) - 1;
+  uint64_t asks = 0;  // pages, and in the upper sixteen bits replacements, of this thread's questions
+#pragma unroll
+  for (int i = 0; i < kQ; ++i) {
+    if (a[i].behind - a[i].first > kNarrow) lacks[i] = lacks_sh[tid * kQ + i];
+    asks += lacks[i] + (replaced[i] ? kOne : 0);
   }
+  uint64_t all, mine = scan1024(asks, all);
+  const uint64_t total = all & low;
   // the lowest free pages
   uint64_t found = 0;
-  for (int64_t base = 0; base < p.n_pages && found < total; base += 4096) {
-    int free = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int64_t page = base + 4 * tid + e;
-      if (page < p.n_pages && p.refs[page] <= 0) free |= 1 << e;
+  for (int64_t base = 0; base < p.n_pages && found < total; base += 1024 * kEach) {
+    const unsigned free = free_of(r);
+    const int64_t first = base + static_cast<int64_t>(tid) * kEach;
+    if (base + 1024 * kEach < p.n_pages) refs_of<kEach>(p, first + 1024 * kEach, r);
+    uint64_t here, at = found + scan1024(__popc(free), here);
+#pragma unroll 1
+    for (unsigned left = free; left && at < total; left &= left - 1, ++at) {
+      const int page = static_cast<int>(first) + __builtin_ctz(left);
+      if (at < kSpareSh) spare_sh[at] = page;
+      else spare[at] = page;
     }
-    uint64_t here;
-    uint64_t at = found + scan1024(__popc(free), here);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (free >> e & 1) {
-        if (at < total) spare[at] = static_cast<int>(base + 4 * tid + e);
-        ++at;
-      }
     found += here;
   }
   __syncthreads();
+  auto spare_at = [&](uint64_t i) { return i < kSpareSh ? spare_sh[i] : spare[i]; };
   // in order, as long as they last
-  uint64_t before = 0;
-  for (int base = 0; base < p.n_queries; base += 1024) {
-    const int u = base + tid;
-    const bool there = u < p.n_queries;
-    const int word = there ? lacks_sh[u] : 0, ask = (word >> 1) + (word & 1);
-    uint64_t all;
-    const uint64_t mine = before + scan1024(static_cast<uint64_t>(ask) | static_cast<uint64_t>(word & 1) << 48, all);
-    before += all;
-    const uint64_t low = (uint64_t{1} << 48) - 1;
+  int copied = 0;
+#pragma unroll
+  for (int i = 0; i < kQ; ++i) {
+    const int u = tid * kQ + i, wide = a[i].behind - a[i].first;
     uint64_t at = mine & low;
-    Ask a{};
-    bool served = false;
-    if (there) {
-      a = ask_of(p, add, u);
-      served = at + ask <= found;
-      got[u] = a.fits && served ? add[u] : 0;
-      if (served && (word & 1)) {
-        const int page = spare[at++], number = static_cast<int>(mine >> 48);
-        copies[3 * number] = a.tail;
-        copies[3 * number + 1] = page;
-        copies[3 * number + 2] = a.rows;
-        atomicAdd(&copied_sh, 1);
-        atomicAdd(p.refs + a.tail, -1);
+    const bool served = at + lacks[i] + replaced[i] <= found;
+    if (u < p.n_queries) {
+      got[u] = a[i].fits && served ? more[i] : 0;
+      if (a[i].fits && served) p.self_len[u] = static_cast<int>(a[i].tokens + more[i]);
+    }
+    int32_t* const row = p.table + static_cast<int64_t>(u) * p.table_stride;
+    if (served && replaced[i]) {
+      const int page = spare_at(at++), number = static_cast<int>(mine >> 48);
+      copies[3 * number] = a[i].tail;
+      copies[3 * number + 1] = page;
+      copies[3 * number + 2] = a[i].rows;
+      ++copied;
+      atomicAdd(p.refs + a[i].tail, -1);
+      p.refs[page] = 1;
+      row[a[i].tokens >> p.page_log2] = page;
+    }
+    if (wide > kNarrow) {
+      lacks_sh[u] = served ? static_cast<int>(at) : -1;
+    } else if (served && lacks[i] > 0) {
+#pragma unroll 1
+      for (int c = a[i].first; c < a[i].behind; ++c) {
+        if (is_page(row[c], p)) continue;
+        const int page = spare_at(at++);
+        row[c] = page;
         p.refs[page] = 1;
-        p.table[static_cast<int64_t>(u) * p.table_stride + (a.tokens >> p.page_log2)] = page;
-      }
-      if (served && a.fits) p.self_len[u] = static_cast<int>(a.tokens + add[u]);
-      if (served && a.behind - a.first <= 4) {
-        for (int c = a.first; c < a.behind; ++c) {
-          int32_t* const entry = p.table + static_cast<int64_t>(u) * p.table_stride + c;
-          if (is_page(*entry, p)) continue;
-          const int page = spare[at++];
-          *entry = page;
-          p.refs[page] = 1;
-        }
       }
     }
-    uint64_t many = __ballot(there && served && a.behind - a.first > 4);
-    while (many) {
-      const int who = __ffsll(static_cast<unsigned long long>(many)) - 1;
-      many &= many - 1;
-      const int first = __shfl(a.first, who), behind = __shfl(a.behind, who);
-      uint64_t next = __shfl(at, who);
-      int32_t* const row = p.table + static_cast<int64_t>(base + wave * 64 + who) * p.table_stride;
-      for (int c = first; c < behind; c += 64) {
-        const bool lacks = c + lane < behind && !is_page(row[min(c + lane, behind - 1)], p);
-        const uint64_t which = __ballot(lacks);
-        if (lacks) {
-          const int page = spare[next + __popcll(which & ((uint64_t{1} << lane) - 1))];
-          row[c + lane] = page;
-          p.refs[page] = 1;
-        }
-        next += __popcll(which);
+    mine += lacks[i] + (replaced[i] ? kOne : 0);
+  }
+  uint64_t all_copied;
+  scan1024(static_cast<uint64_t>(copied), all_copied);  // (and a barrier)
+  if (tid == 0) *n_copies = static_cast<int>(all_copied);
+  for (int i = tid / 16; i < n_wide; i += 64) {
+    const int u = wide_sh[i], behind = wide_behind_sh[i], in = tid % 16, from = lane & 48;
+    if (lacks_sh[u] < 0) continue;
+    uint64_t at = static_cast<unsigned>(lacks_sh[u]);
+    int32_t* const row = p.table + static_cast<int64_t>(u) * p.table_stride;
+    int next = row[min(wide_first_sh[i] + in, behind - 1)];
+#pragma unroll 1
+    for (int c = wide_first_sh[i]; c < behind; c += 16) {
+      const bool lacking = c + in < behind && !is_page(next, p);
+      next = row[min(c + 16 + in, behind - 1)];
+      const unsigned which = static_cast<unsigned>(__ballot(lacking) >> from) & 0xffffu;
+      if (lacking) {
+        const int page = spare_at(at + __popc(which & ((1u << in) - 1)));
+        row[c + in] = page;
+        p.refs[page] = 1;
       }
+      at += __popc(which);
     }
   }
-  __syncthreads();
-  if (tid == 0) *n_copies = copied_sh;
 }
 
 // ---- trim ------------------------------------------------------------------------------------------------------
@@ -265,48 +357,67 @@ __global__ __launch_bounds__(256) void pages_trim_kernel(BookParams p) {
 
 // ---- compact ---------------------------------------------------------------------------------------------------
 
+constexpr int kMovesSh = 4096;    // moves that are kept in LDS
+constexpr int kChunksSh = 16;     // chunks of which the pages in use are kept there
+constexpr int kRenameHere = 32768;  // entries that the one workgroup renames itself
+
 // One workgroup: with L pages in use, those at L and behind go, in order, to the free ones before L.
-__global__ __launch_bounds__(1024) void pages_compact_kernel(BookParams p, int32_t* copies, int32_t* counts, int32_t* new_place) {
+template <int kEach>
+__global__ __launch_bounds__(1024) void pages_compact_kernel(BookParams p, int32_t* copies, int32_t* counts, int32_t* new_place, bool renames) {
+  constexpr int kChunk = 1024 * kEach;
+  __shared__ uint16_t free_sh[kChunksSh][1024];
+  __shared__ int from_sh[kMovesSh], to_sh[kMovesSh];
   const int tid = threadIdx.x;
-  uint64_t live = 0;
-  for (int64_t base = 0; base < p.n_pages; base += 4096) {
-    int here = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int64_t page = base + 4 * tid + e;
-      here += page < p.n_pages && p.refs[page] > 0;
-    }
-    uint64_t all;
-    scan1024(here, all);
-    live += all;
+  auto free_at = [&](int64_t base) {
+    int r[kEach];
+    refs_of<kEach>(p, base + static_cast<int64_t>(tid) * kEach, r);
+    return free_of(r);
+  };
+  uint64_t used = 0, live;
+#pragma unroll 2
+  for (int64_t base = 0; base < p.n_pages; base += kChunk) {
+    const unsigned free = free_at(base);
+    const int64_t left = p.n_pages - base - static_cast<int64_t>(tid) * kEach;
+    used += left <= 0 ? 0 : (left < kEach ? left : kEach) - __popc(free);
+    if (base / kChunk < kChunksSh) free_sh[base / kChunk][tid] = static_cast<uint16_t>(free);
   }
+  scan1024(used, live);
   uint64_t holes = 0, moves = 0;
-  for (int64_t base = 0; base < p.n_pages; base += 4096) {
-    int hole = 0, move = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int64_t page = base + 4 * tid + e;
-      if (page >= p.n_pages) continue;
-      const bool used = p.refs[page] > 0, front = static_cast<uint64_t>(page) < live;
-      if (front && !used) hole |= 1 << e;
-      if (!front && used) move |= 1 << e;
-      new_place[page] = used ? static_cast<int>(page) : -1;
-    }
+  for (int64_t base = 0; base < p.n_pages; base += kChunk) {
+    const int64_t first = base + static_cast<int64_t>(tid) * kEach;
+    const unsigned free = base / kChunk < kChunksSh ? free_sh[base / kChunk][tid] : free_at(base);
+    const int there = static_cast<int>(first >= p.n_pages ? 0 : p.n_pages - first < kEach ? p.n_pages - first : kEach);
+    const int front = static_cast<int>(static_cast<int64_t>(live) <= first ? 0 : static_cast<int64_t>(live) - first < there ? static_cast<int64_t>(live) - first : there);
+    const unsigned in_front = (1u << front) - 1, hole = free & in_front, move = ~free & ((1u << there) - 1) & ~in_front;
     uint64_t all;
     const uint64_t mine = scan1024(static_cast<uint64_t>(__popc(hole)) | static_cast<uint64_t>(__popc(move)) << 32, all);
     uint64_t h = holes + (mine & 0xffffffffu), m = moves + (mine >> 32);
+    int place[kEach];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int page = static_cast<int>(base + 4 * tid + e);
-      if (hole >> e & 1) copies[3 * h++ + 1] = page;
-      if (move >> e & 1) copies[3 * m++] = page;
+    for (int e = 0; e < kEach; ++e) {
+      const int page = static_cast<int>(first + e);
+      place[e] = free >> e & 1 ? -1 : page;
+      if (hole >> e & 1) {
+        if (h < kMovesSh) to_sh[h] = page;
+        copies[3 * h++ + 1] = page;
+      }
+      if (move >> e & 1) {
+        if (m < kMovesSh) from_sh[m] = page;
+        copies[3 * m++] = page;
+      }
+    }
+    if (there == kEach && reinterpret_cast<uintptr_t>(new_place) % 16 == 0) {
+#pragma unroll
+      for (int e = 0; e < kEach; e += 4) *reinterpret_cast<intx4*>(new_place + first + e) = intx4{place[e], place[e + 1], place[e + 2], place[e + 3]};
+    } else {
+      for (int e = 0; e < there; ++e) new_place[first + e] = free >> e & 1 ? -1 : static_cast<int>(first + e);
     }
     holes += all & 0xffffffffu;
     moves += all >> 32;
   }
   __syncthreads();
   for (uint64_t i = tid; i < moves; i += 1024) {
-    const int from = copies[3 * i], to = copies[3 * i + 1];
+    const int from = i < kMovesSh ? from_sh[i] : copies[3 * i], to = i < kMovesSh ? to_sh[i] : copies[3 * i + 1];
     copies[3 * i + 2] = 1 << p.page_log2;
     p.refs[to] = p.refs[from];
     p.refs[from] = 0;
@@ -315,6 +426,14 @@ __global__ __launch_bounds__(1024) void pages_compact_kernel(BookParams p, int32
   if (tid == 0) {
     counts[0] = static_cast<int>(moves);
     counts[1] = static_cast<int>(live);
+  }
+  if (!renames) return;
+  __syncthreads();
+  const int entries = p.n_queries * p.table_stride;
+#pragma unroll 4
+  for (int i = tid; i < entries; i += 1024) {
+    const int entry = p.table[i];
+    if (is_page(entry, p) && entry >= 0) p.table[i] = new_place[entry];
   }
 }
 
@@ -367,19 +486,23 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(PagesCopyParams p) {
 }  // namespace
 
 hipError_t launch_pages_fork(const BookParams& p, const int32_t* source, hipStream_t stream) {
-  // 64 KiB of LDS hold the columns of a workgroup
-  int columns = 16384 / p.n_queries;
-  columns = columns > 64 ? 64 : columns;
-  const int blocks = (p.table_stride + columns - 1) / columns;
-  pages_fork_kernel<<<dim3(blocks), dim3(256), static_cast<size_t>(p.n_queries) * columns * 4, stream>>>(p, source, columns);
-  if (const hipError_t e = hipGetLastError()) return e;
+  // as many columns as the workgroup's registers hold; a table that fits into one workgroup is one launch, others have 32 columns
+  // to a workgroup at most
+  int columns_log2 = 0;
+  while ((1 << columns_log2) < p.table_stride && (p.n_queries << (columns_log2 + 1)) <= 1024 * kForkEach && (1 << columns_log2) < 1024) ++columns_log2;
+  const bool alone = (1 << columns_log2) >= p.table_stride && p.n_queries <= 1024;
+  if (!alone && columns_log2 > 5) columns_log2 = 5;
+  const int blocks = (p.table_stride + (1 << columns_log2) - 1) >> columns_log2;
+  pages_fork_kernel<<<dim3(blocks), dim3(1024), 0, stream>>>(p, source, columns_log2, alone);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess || alone) return e;
   pages_fork_lengths_kernel<<<dim3(1), dim3(1024), 0, stream>>>(p, source);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_reserve(const BookParams& p, const int32_t* add, int32_t* got, int32_t* copies, int32_t* n_copies, int32_t* spare,
                                 hipStream_t stream) {
-  pages_reserve_kernel<<<dim3(1), dim3(1024), 0, stream>>>(p, add, got, copies, n_copies, spare);
+  if (p.n_queries <= 1024) pages_reserve_kernel<1><<<dim3(1), dim3(1024), 0, stream>>>(p, add, got, copies, n_copies, spare);
+  else pages_reserve_kernel<kBookQuestions / 1024><<<dim3(1), dim3(1024), 0, stream>>>(p, add, got, copies, n_copies, spare);
   return hipGetLastError();
 }
 
@@ -390,10 +513,12 @@ hipError_t launch_pages_trim(const BookParams& p, hipStream_t stream) {
 }
 
 hipError_t launch_pages_compact(const BookParams& p, int32_t* copies, int32_t* counts, int32_t* new_place, hipStream_t stream) {
-  pages_compact_kernel<<<dim3(1), dim3(1024), 0, stream>>>(p, copies, counts, new_place);
-  if (const hipError_t e = hipGetLastError()) return e;
   const int64_t entries = static_cast<int64_t>(p.n_queries) * p.table_stride;
-  if (entries > 0) pages_rename_kernel<<<dim3(static_cast<unsigned>((entries + 255) / 256)), dim3(256), 0, stream>>>(p, new_place);
+  const bool renames = entries <= kRenameHere;
+  if (p.n_pages <= 8192) pages_compact_kernel<4><<<dim3(1), dim3(1024), 0, stream>>>(p, copies, counts, new_place, renames);
+  else pages_compact_kernel<16><<<dim3(1), dim3(1024), 0, stream>>>(p, copies, counts, new_place, renames);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess || renames) return e;
+  pages_rename_kernel<<<dim3(static_cast<unsigned>((entries + 255) / 256)), dim3(256), 0, stream>>>(p, new_place);
   return hipGetLastError();
 }
 

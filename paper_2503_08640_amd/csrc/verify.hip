@@ -597,7 +597,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
     }
   }
   const T* const target = target_row<T>(p, d.row);
-  const T* const draft = d.refused == 1 ? draft_row<T>(p, u, d.step) : target;
+  const T* const draft = d.refused == 1 ? draft_row<T>(p, u, d.step) : nullptr;
   double* const sums = w.weight + static_cast<int64_t>(u) * w.shares;
   const Scale of_p = kLogits ? scale_of(d.top_p, heat.factor) : Scale{}, of_q = kLogits ? scale_of(d.top_q, heat.factor) : Scale{};
   // phase 0: the workgroup's shares; 1: the sums are there, and the share that the token lies in is gone through again (the same
@@ -614,7 +614,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
 #pragma unroll
       for (int k = 0; k < kLoads; ++k) {
         of_target[k] = load_wide(target, share * kShare + k * kStep + lane * kWide, p.vocab);
-        of_draft[k] = load_wide(draft, share * kShare + k * kStep + lane * kWide, p.vocab);
+        if (d.refused == 1) of_draft[k] = load_wide(draft, share * kShare + k * kStep + lane * kWide, p.vocab);
       }
     }
     while (share < end) {
@@ -630,14 +630,14 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
           values_of(of_target[k], target, first + k * kStep, p.vocab, kNone, x[k]);
-          values_of(of_draft[k], draft, first + k * kStep, p.vocab, kNone, y[k]);
+          if (d.refused == 1) values_of(of_draft[k], draft, first + k * kStep, p.vocab, kNone, y[k]);
         }
       }
       if (next < end) {
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
           of_target[k] = load_wide(target, next * kShare + k * kStep + lane * kWide, p.vocab);
-          of_draft[k] = load_wide(draft, next * kShare + k * kStep + lane * kWide, p.vocab);
+          if (d.refused == 1) of_draft[k] = load_wide(draft, next * kShare + k * kStep + lane * kWide, p.vocab);
         }
       }
       double sum = 0;

@@ -112,10 +112,10 @@ def test_rows_go_round_in_a_circle():
 
 
 def test_most_questions():
-    """8192 rows: the most a call takes."""
-    k = books(3, 8192, 3, 9000, 16, full=1.0)
-    k.fork(np.random.default_rng(0).integers(0, 8192, 8192))
-    k.reserve(np.ones(8192))
+    """4096 rows: the most a call takes."""
+    k = books(3, 4096, 3, 9000, 16, full=1.0)
+    k.fork(np.random.default_rng(0).integers(0, 4096, 4096))
+    k.reserve(np.ones(4096))
     k.trim()
     k.compact()
 

@@ -128,7 +128,7 @@ def book(**change):
 
 BAD_BOOKS = [(dict(refs=None), B.DBSA_ERR_INVALID_ARG), (dict(pages=0), B.DBSA_ERR_INVALID_ARG), (dict(table=None), B.DBSA_ERR_INVALID_ARG),
              (dict(columns=0), B.DBSA_ERR_INVALID_ARG), (dict(b=-1), B.DBSA_ERR_INVALID_ARG), (dict(page=8), B.DBSA_ERR_UNSUPPORTED),
-             (dict(page=48), B.DBSA_ERR_UNSUPPORTED), (dict(page=0), B.DBSA_ERR_UNSUPPORTED), (dict(b=8193), B.DBSA_ERR_UNSUPPORTED),
+             (dict(page=48), B.DBSA_ERR_UNSUPPORTED), (dict(page=0), B.DBSA_ERR_UNSUPPORTED), (dict(b=4097), B.DBSA_ERR_UNSUPPORTED),
              (dict(columns=(1 << 24) + 1), B.DBSA_ERR_UNSUPPORTED)]
 
 
