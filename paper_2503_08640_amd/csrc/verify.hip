@@ -567,21 +567,69 @@ __device__ inline int passing_thread(double mine, double front, double want) {
   return it;
 }
 
-// One workgroup: shares part * each .. of the row that decides for question u, a wave a share at a time and the next one on its way.
+// The piece of the row that decides in which the running sum passes `number` of the whole, from the sums that the statistics left:
+// where w is p (or p without the proposal) nothing has to be weighed for it.  -1 without weights.
+struct Place {
+  int piece;
+  double before, want;  // running sum in front of it
+};
+__device__ inline Place place_of(const VerifyParams& p, const Work& w, Decision& d, const Scale& of_p, float proposed, int piece) {
+  __shared__ Place place_sh;
+  const int tid = threadIdx.x, run = (w.pieces + kThreads - 1) / kThreads;
+  const int64_t base = static_cast<int64_t>(d.row) * w.pieces;
+  auto sum_of = [&](int i) {
+    const double sum = w.sum[base + i];
+    if (!(sum > 0)) return 0.0;
+    const double all = sum * rescale(scale_of(w.top[base + i], of_p.factor), of_p) * d.inv_p;
+    return d.refused == 2 && i == d.proposal / piece ? fmax(all - weight_of(proposed, of_p) * d.inv_p, 0.0) : all;
+  };
+  for (;;) {
+    double mine = 0, all;
+#pragma unroll 1
+    for (int i = tid * run; i < min(tid * run + run, w.pieces); ++i) mine += sum_of(i);
+    const double front = scan(mine, all);
+    if (!(all > 0)) {
+      if (d.refused == 0) return {-1, 0.0, 0.0};
+      d.refused = 0;  // the proposal has all there is
+      continue;
+    }
+    const double want = static_cast<double>(d.number) * all;
+    if (tid == passing_thread(mine, front, want)) {
+      double before = front, in_front = front;
+      int chosen = tid * run;
+#pragma unroll 1
+      for (int i = tid * run; i < min(tid * run + run, w.pieces); ++i) {
+        const double here = run == 1 ? mine : sum_of(i);
+        if (!(here > 0)) continue;
+        chosen = i;
+        in_front = before;
+        before += here;
+        if (before > want) break;
+      }
+      place_sh = {chosen, in_front, want};
+    }
+    __syncthreads();
+    return place_sh;
+  }
+}
+
+// One workgroup: shares part * each .. of the row that decides for question u, a wave a share at a time and the next one on its way;
+// where the statistics have the sums already, one workgroup alone and the piece that the token lies in.
 template <typename T, bool kLogits, bool kDecided>
 __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, int piece, int parts, int each) {
   constexpr int kWide = 16 / sizeof(T), kStep = 64 * kWide, kLoads = kShare / kStep;
   constexpr float kNone = kLogits ? -INFINITY : 0.f;
   const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
-  const int part = blockIdx.x % parts, u = blockIdx.x / parts, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  // (workgroup i runs on the chip's part i % 8: the first parts, which have more to do, are not to lie on one of them)
+  const int u = blockIdx.x / parts, part = (blockIdx.x + u) % parts, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   __shared__ bool last_sh;
   __shared__ int chosen_sh;
-  __shared__ double before_sh, weight_sh[kShare];
+  __shared__ double before_sh, weight_sh[kPieceLeast];
   const Heat heat = heat_of(p, u);
   Decision d;
   if constexpr (kDecided) {
     d = w.decision[u];
-    if (d.row < 0) return;
+    if (d.row < 0 || (kLogits && d.refused != 1 && part > 0)) return;
   } else {
     const Span s = span_of(p, u);
     const bool greedy = kLogits && heat.greedy;
@@ -591,6 +639,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
       return;
     }
     d = decide<T, kLogits>(p, w, u, s, heat, part == 0);
+    if (kLogits && d.refused != 1 && part > 0) return;
     if (greedy) {
       if (tid == 0) tell_token<T, kLogits>(p, d, d.place, heat.factor);
       return;
@@ -600,24 +649,39 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
   const T* const draft = d.refused == 1 ? draft_row<T>(p, u, d.step) : nullptr;
   double* const sums = w.weight + static_cast<int64_t>(u) * w.shares;
   const Scale of_p = kLogits ? scale_of(d.top_p, heat.factor) : Scale{}, of_q = kLogits ? scale_of(d.top_q, heat.factor) : Scale{};
-  // phase 0: the workgroup's shares; 1: the sums are there, and the share that the token lies in is gone through again (the same
-  // instructions: what runs for the first time waits for them); 2: the target lies nowhere above what proposed, the last workgroup
-  // goes through all of the target alone
-  int share_begin = part * each, share_end = min(share_begin + each, w.shares), phase = 0;
-  double want = 0;
+  int share_begin = part * each, share_end = min(share_begin + each, w.shares);
+  // keep: the weights stay in LDS for the draw, those of a short piece, or of the share that the token lies in, which is gone through
+  // once more when its sum is there (the same instructions: what runs for the first time waits for them)
+  bool alone = false, keep = false;
+  double base = 0, want = 0;
+  if constexpr (kLogits) {
+    if (d.refused != 1) {
+      const Place place = place_of(p, w, d, of_p, d.refused == 2 ? at(target, d.proposal) : 0.f, piece);
+      if (place.piece < 0) {
+        if (tid == 0) tell_token<T, kLogits>(p, d, -1, heat.factor);
+        return;
+      }
+      base = place.before;
+      want = place.want;
+      share_begin = place.piece * (piece / kShare);
+      share_end = min(share_begin + piece / kShare, w.shares);
+      alone = true;
+      keep = piece <= kPieceLeast;
+      before_sh = base;
+    }
+  }
+  const bool known = alone;  // `want` is
   for (;;) {
-    const bool again = phase == 1;
-    const int end = again ? share_begin + 1 : share_end;
     int share = share_begin + wave;
     uintx4 of_target[kLoads], of_draft[kLoads];
-    if (share < end) {
+    if (share < share_end) {
 #pragma unroll
       for (int k = 0; k < kLoads; ++k) {
         of_target[k] = load_wide(target, share * kShare + k * kStep + lane * kWide, p.vocab);
         if (d.refused == 1) of_draft[k] = load_wide(draft, share * kShare + k * kStep + lane * kWide, p.vocab);
       }
     }
-    while (share < end) {
+    while (share < share_end) {
       const int first = share * kShare + lane * kWide, next = share + kWaves;
       float x[kLoads][kWide], y[kLoads][kWide];
       if ((share + 1) * kShare <= p.vocab) {
@@ -633,7 +697,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
           if (d.refused == 1) values_of(of_draft[k], draft, first + k * kStep, p.vocab, kNone, y[k]);
         }
       }
-      if (next < end) {
+      if (next < share_end) {
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
           of_target[k] = load_wide(target, next * kShare + k * kStep + lane * kWide, p.vocab);
@@ -647,70 +711,74 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
         for (int e = 0; e < kWide; ++e) {
           const double here = weight_at<kLogits>(d, x[k][e], y[k][e], first + k * kStep + e, of_p, of_q);
           sum += here;
-          if (again) weight_sh[k * kStep + lane * kWide + e] = here;
+          if (keep) weight_sh[(share - share_begin) * kShare + k * kStep + lane * kWide + e] = here;
         }
-      if (!again) {
+      if (!keep) {
         sum = wave_sum(sum);
         if (lane == 0) leave(sums + share, sum);
       }
       share = next;
     }
-    if (again) break;
+    if (keep) break;
     wait_for_stores();
     __syncthreads();
-    if (phase == 0) {
+    if (!alone) {
       if (tid == 0)
         last_sh = __hip_atomic_fetch_add(w.done + static_cast<int64_t>(u) * kApart, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == static_cast<unsigned>(parts - 1);
       __syncthreads();
       if (!last_sh) return;
-    }
-    const int run = (w.shares + kThreads - 1) / kThreads;
-    double mine = 0, all;
-    for (int i = tid * run; i < min(tid * run + run, w.shares); ++i) mine += left(sums + i);
-    const double front = scan(mine, all);
-    if (!(all > 0)) {
-      if (phase == 2 || d.refused == 0) {
-        if (tid == 0) tell_token<T, kLogits>(p, d, -1, heat.factor);
-        return;
-      }
-      d.refused = 0;
       share_begin = 0;
       share_end = w.shares;
-      phase = 2;
-      continue;
     }
-    want = static_cast<double>(d.number) * all;
+    const int run = (share_end - share_begin + kThreads - 1) / kThreads, first = share_begin + tid * run, end = min(first + run, share_end);
+    double mine = 0, all;
+    for (int i = first; i < end; ++i) mine += left(sums + i);
+    const double front = base + scan(mine, all);
+    if (!known) {
+      if (!(all > 0)) {
+        if (d.refused == 0) {
+          if (tid == 0) tell_token<T, kLogits>(p, d, -1, heat.factor);
+          return;
+        }
+        d.refused = 0;  // the target lies nowhere above what proposed: this workgroup goes through all of the target
+        alone = true;
+        continue;
+      }
+      want = static_cast<double>(d.number) * all;
+    }
     if (tid == passing_thread(mine, front, want)) {
-      double before = front, at_last = front;
-      int chosen = 0;
-      for (int i = tid * run; i < min(tid * run + run, w.shares); ++i) {
+      double before = front, in_front = front;
+      int chosen = first;
+      for (int i = first; i < end; ++i) {
         const double here = run == 1 ? mine : left(sums + i);
         if (!(here > 0)) continue;
         chosen = i;
-        at_last = before;
+        in_front = before;
         before += here;
         if (before > want) break;
       }
       chosen_sh = chosen;
-      before_sh = at_last;
+      before_sh = in_front;
     }
     __syncthreads();
     share_begin = chosen_sh;
-    phase = 1;
+    share_end = share_begin + 1;
+    keep = true;
   }
   __syncthreads();
-  constexpr int kMine = kShare / kThreads;
+  const int run = (share_end - share_begin) * (kShare / kThreads);
   double mine = 0, all;
-#pragma unroll
-  for (int e = 0; e < kMine; ++e) mine += weight_sh[tid * kMine + e];
+#pragma unroll 2
+  for (int e = 0; e < run; ++e) mine += weight_sh[tid * run + e];
   const double front = before_sh + scan(mine, all);
   if (tid != passing_thread(mine, front, want)) return;
   double before = front;
   int token = 0;
-  for (int e = 0; e < kMine; ++e) {
-    const double here = weight_sh[tid * kMine + e];
+#pragma unroll 1
+  for (int e = 0; e < run; ++e) {
+    const double here = weight_sh[tid * run + e];
     if (!(here > 0)) continue;
-    token = share_begin * kShare + tid * kMine + e;
+    token = share_begin * kShare + tid * run + e;
     before += here;
     if (before > want) break;
   }
@@ -723,8 +791,9 @@ void launch(const VerifyParams& p, hipStream_t stream) {
   const int piece = rows * p.vocab >= int64_t{1} << 25 ? 4 * kPieceLeast : kPieceLeast;
   const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
   const dim3 threads(kThreads);
-  // shares of a workgroup, a multiple of its waves
-  const int64_t most = pieces_of(w.shares, kWaves), per = (p.n_queries * most + 2047) / 2048;
+  constexpr int64_t kFull = kLogits ? 2048 : 4096;  // workgroups that fill the chip a few times (half and twice as many: 3 to 9 % slower)
+  // shares of a workgroup, a multiple of its waves; nothing is weighed by more than one where no distribution is taken off
+  const int64_t most = pieces_of(w.shares, kWaves), per = kLogits && !p.draft ? most : (p.n_queries * most + kFull - 1) / kFull;
   const int each = static_cast<int>(per * kWaves), parts = static_cast<int>(pieces_of(w.shares, each));
   const bool apart = static_cast<int64_t>(p.n_queries) * parts > 512;
   if (kLogits && rows > 0) {
