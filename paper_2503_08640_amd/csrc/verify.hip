@@ -42,6 +42,7 @@ struct Decision {
 // pieces of the workspace
 struct Work {
   double* sum;   // [2 n_tokens][pieces]: target rows, then the rows of what proposed
+  double* rest;  // [n_tokens][pieces], where no distribution proposed: the same without the proposal
   float* top;    // what its weights are counted from
   float* peak;   // greedy: largest value and its place
   int32_t* place;
@@ -63,6 +64,8 @@ __host__ __device__ inline Work work_of(void* base, int64_t n_tokens, int64_t n_
   const int64_t cells = 2 * n_tokens * w.pieces;
   w.sum = reinterpret_cast<double*>(at);
   at += cells * 8;
+  w.rest = reinterpret_cast<double*>(at);
+  at += cells * 4;
   w.top = reinterpret_cast<float*>(at);
   at += cells * 4;
   w.peak = reinterpret_cast<float*>(at);
@@ -258,6 +261,10 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
     for (int i = 0; i < kLoads; ++i) raw[i] = load_wide(from, mine + i * kStep, p.vocab);
   }
   const bool sums = !heat.greedy || p.logp;
+  // where no distribution proposed, the sum without the proposal is kept, too (a difference would leave what it was rounded by)
+  int proposal = -1;
+  if (!p.draft && !heat.greedy && row + 1 < s.end) proposal = p.tokens[row + 1];
+  if (proposal < begin || proposal >= end) proposal = -1;
   float peak = -INFINITY;
   double sum = 0;
   int place = INT32_MAX;
@@ -297,6 +304,12 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
             place = first + i * kStep + e;
           }
     }
+    if (proposal >= chunk && proposal < chunk + kChunk) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int e = 0; e < kWide; ++e) x[i][e] = first + i * kStep + e == proposal ? -INFINITY : x[i][e];
+    }
     if (sums) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
@@ -306,13 +319,15 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
   }
   float top = scale.top;
   sum = wave_sum(sum);
-  if (sums && top > -INFINITY && !(scale.plain && sum < 0x1p1000)) {
+  double proposed = proposal >= 0 ? weight_of(at(from, proposal), scale) : 0.0;
+  if (sums && top > -INFINITY && !(scale.plain && sum + proposed < 0x1p1000)) {
     for (int i = begin + lane; i < end; i += 64) top = fmaxf(top, at(from, i));
     top = wave_max(top);
     scale = scale_of(top, heat.factor);
     sum = 0;
-    for (int i = begin + lane; i < end; i += 64) sum += weight_of(at(from, i), scale);
+    for (int i = begin + lane; i < end; i += 64) sum += i == proposal ? 0.0 : weight_of(at(from, i), scale);
     sum = wave_sum(sum);
+    if (proposal >= 0) proposed = weight_of(at(from, proposal), scale);
   }
   if (heat.greedy) {
     const float all = wave_max(peak);
@@ -320,7 +335,8 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
     peak = all;
   }
   if (lane == 0) {
-    w.sum[cell] = sum;
+    if (!p.draft) w.rest[cell] = sum;
+    w.sum[cell] = sum + proposed;
     w.top[cell] = top;
     w.peak[cell] = peak;
     w.place[cell] = place;
@@ -548,7 +564,7 @@ __device__ inline void leave(double* p, double v) { __hip_atomic_store(p, v, __A
 __device__ inline void wait_for_stores() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Threads hold runs of items one after the other, of sums `mine` with `front` in front of them.  The thread in whose run the
-// running sum passes `want`; where none does, the last that has any.  (By ballots: an atomic of many lanes becomes a loop over
+// running sum passes `want`; where none does, the last that has any; 0 if none has.  (By ballots: an atomic of many lanes becomes a loop over
 // them, 1.5 us each.)
 __device__ inline int passing_thread(double mine, double front, double want) {
   __shared__ int found_sh[kWaves], last_sh[kWaves];
@@ -559,7 +575,7 @@ __device__ inline int passing_thread(double mine, double front, double want) {
     last_sh[wave] = any ? wave * 64 + 63 - __builtin_clzll(any) : -1;
   }
   __syncthreads();
-  int it = -1;
+  int it = 0;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) it = max(it, last_sh[i]);
 #pragma unroll
@@ -573,15 +589,13 @@ struct Place {
   int piece;
   double before, want;  // running sum in front of it
 };
-__device__ inline Place place_of(const VerifyParams& p, const Work& w, Decision& d, const Scale& of_p, float proposed, int piece) {
+__device__ inline Place place_of(const Work& w, Decision& d, const Scale& of_p) {
   __shared__ Place place_sh;
   const int tid = threadIdx.x, run = (w.pieces + kThreads - 1) / kThreads;
   const int64_t base = static_cast<int64_t>(d.row) * w.pieces;
   auto sum_of = [&](int i) {
-    const double sum = w.sum[base + i];
-    if (!(sum > 0)) return 0.0;
-    const double all = sum * rescale(scale_of(w.top[base + i], of_p.factor), of_p) * d.inv_p;
-    return d.refused == 2 && i == d.proposal / piece ? fmax(all - weight_of(proposed, of_p) * d.inv_p, 0.0) : all;
+    const double sum = (d.refused == 2 ? w.rest : w.sum)[base + i];
+    return sum > 0 ? sum * rescale(scale_of(w.top[base + i], of_p.factor), of_p) * d.inv_p : 0.0;
   };
   for (;;) {
     double mine = 0, all;
@@ -656,7 +670,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
   double base = 0, want = 0;
   if constexpr (kLogits) {
     if (d.refused != 1) {
-      const Place place = place_of(p, w, d, of_p, d.refused == 2 ? at(target, d.proposal) : 0.f, piece);
+      const Place place = place_of(w, d, of_p);
       if (place.piece < 0) {
         if (tid == 0) tell_token<T, kLogits>(p, d, -1, heat.factor);
         return;
@@ -773,7 +787,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
   const double front = before_sh + scan(mine, all);
   if (tid != passing_thread(mine, front, want)) return;
   double before = front;
-  int token = 0;
+  int token = -1;
 #pragma unroll 1
   for (int e = 0; e < run; ++e) {
     const double here = weight_sh[tid * run + e];

@@ -193,6 +193,26 @@ def test_equal_distributions():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("over", [5.0, 12.0, 25.0, 60.0, 400.0])
+def test_proposals_that_have_nearly_everything(dtype, over):
+    """Looked-up proposals whose probability leaves little, or nothing, to the others: what is left is drawn from exactly."""
+    for vocab in (700, 9000, 70000):
+        c = make(85 + vocab, [3, 4, 2], vocab, dtype, draft=False, spread=1.0)
+        for row in (0, 3, 7):
+            c["x"][row, int(c["tokens"][row + 1])] = over
+        c["uniform"][:] = 1.0 - 2.0 ** -24
+        c["uniform"][[2, 6, 8]] = [0.3, 0.9, 0.6]
+        same(call(c), wanted(c), c, f"{over} above {vocab} {dtype}")
+        only = torch.full_like(c["x"][0], -float("inf"))
+        for row in (0, 3, 7):
+            c["x"][row] = only
+            c["x"][row, int(c["tokens"][row + 1])] = over
+        same(call(c), wanted(c), c, f"nothing but {over} {vocab} {dtype}")
+        c["uniform"][:] = 1.0
+        same(call(c), wanted(c), c, f"nothing but {over}, refused, {vocab} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("form", ["logits", "probs"])
 def test_strides_and_alignments(dtype, form):
     """Rows off 16-byte addresses, wider than the vocabulary, every one at an offset of its own; the proposer's rows step by step
