@@ -633,7 +633,7 @@ int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, co
  *   w = p_n if there was none: the first i with  sum_{j <= i} w_j > uniform_last * sum_j w_j.
  * What comes out is distributed as if the target had drawn every token.  T_u = 1 draws a token without proposals.
  *
- *   target     : device [n_tokens, vocab] of dtype, rows target_stride elements apart (any alignment), packed by cu_qlens.
+ *   target     : device [n_tokens, vocab] of dtype (n_tokens may be 0: every question is without rows), rows target_stride elements apart (any alignment), packed by cu_qlens.
  *   draft      : rows of the same form and dtype that the proposals were drawn from: that of proposal a of question u begins at
  *                element u * stride_query + a * stride_step, a < n_steps.  NULL, or ptr NULL: the proposals were not drawn at
  *                random (q = 1 at the proposal).
@@ -689,7 +689,7 @@ typedef struct {
   int32_t* refs;       /* device [n_pages]                                                   */
   int32_t* self_len;   /* device [n_queries], counted from 0 to what a row of the table holds */
   int32_t n_queries;   /* at most 4096                                                       */
-  int32_t table_stride;/* at most 2^24                                                       */
+  int32_t table_stride;/* at most 2^20                                                       */
   int32_t page_tokens; /* a power of two, at least 16                                        */
   int32_t n_pages;
 } dbsa_page_book;

@@ -21,7 +21,7 @@ def distribution(scores, temperature, probabilities: bool):
         if top == np.inf:
             free = np.where(x == np.inf, 0.0, -np.inf)
         else:
-            free = (x - top) / (1.0 if greedy else min(np.float64(temperature), 1e30))
+            free = (x - top) / (1.0 if greedy else min(np.float64(temperature), float(np.float32(1e30))))
             free = np.where(x == -np.inf, -np.inf, free)
         free = free - np.log(np.exp(free).sum())
         if not greedy:

@@ -1329,9 +1329,8 @@ int dbsa_draft_verify(const void* target, int64_t target_stride, const dbsa_draf
                       const int32_t* self_len, int32_t* new_len, void* workspace, size_t workspace_bytes, void* stream) {
   if (dtype != DBSA_BF16 && dtype != DBSA_F32) return DBSA_ERR_UNSUPPORTED;
   if (form != DBSA_LOGITS && form != DBSA_PROBABILITIES) return DBSA_ERR_UNSUPPORTED;
-  if (!target || !tokens || !cu_qlens || !uniform || !out_tokens || !accepted || n_tokens < 0 || n_queries < 1 || vocab < 1)
-    return DBSA_ERR_INVALID_ARG;
-  if (out_tokens == tokens || !self_len != !new_len) return DBSA_ERR_INVALID_ARG;
+  if (!cu_qlens || !accepted || n_tokens < 0 || n_queries < 1 || vocab < 1 || !self_len != !new_len) return DBSA_ERR_INVALID_ARG;
+  if (n_tokens > 0 && (!target || !tokens || !uniform || !out_tokens || out_tokens == tokens)) return DBSA_ERR_INVALID_ARG;
   if (form == DBSA_PROBABILITIES && temperature) return DBSA_ERR_INVALID_ARG;
   const uintptr_t size = dtype == DBSA_BF16 ? 2 : 4;
   if (reinterpret_cast<uintptr_t>(target) % size != 0 || target_stride < 0) return DBSA_ERR_INVALID_ARG;
@@ -1374,7 +1373,7 @@ int book_common(BookParams& p, const dbsa_page_book* book, bool rows) {
   if (book->n_queries > 0 && (!book->table || book->table_stride < 1)) return DBSA_ERR_INVALID_ARG;
   if (rows && !book->self_len) return DBSA_ERR_INVALID_ARG;
   if (book->page_tokens < 16 || (book->page_tokens & (book->page_tokens - 1)) != 0) return DBSA_ERR_UNSUPPORTED;
-  if (book->n_queries > kBookQuestions || book->table_stride > 1 << 24) return DBSA_ERR_UNSUPPORTED;
+  if (book->n_queries > kBookQuestions || book->table_stride > 1 << 20) return DBSA_ERR_UNSUPPORTED;
   p.table = book->table;
   p.refs = book->refs;
   p.self_len = book->self_len;
@@ -1430,7 +1429,8 @@ int dbsa_pages_copy(const dbsa_pages* pages, int32_t n_layers, int64_t stride_la
     return DBSA_ERR_INVALID_ARG;
   if (pages->page_tokens < 16 || (pages->page_tokens & (pages->page_tokens - 1)) != 0) return DBSA_ERR_UNSUPPORTED;
   const int64_t units = int64_t{pages->page_tokens} * n_kv_heads * (head_dim * bytes / 16);
-  if (units > 1 << 30) return DBSA_ERR_UNSUPPORTED;  // 16 GB a page
+  // (a page has at most 2^34 bytes; pieces of 2^15 are counted in 32 bits within a copy)
+  if (units > 1 << 30 || (units / 2048 + 1) * 2 * n_layers > INT32_MAX) return DBSA_ERR_UNSUPPORTED;
   PagesCopyParams p{};
   p.k = view(pages->k);
   p.v = view(pages->v);

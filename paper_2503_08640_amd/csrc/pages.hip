@@ -111,7 +111,7 @@ __device__ inline uint64_t scan1024(uint64_t v, uint64_t& total) {
   return (wave > 0 ? __shfl(sum, wave - 1) : 0) + up - v;
 }
 
-// Which of the kEach pages from the first-th on are in use; those behind the last count as used and, in `there`, as not there.
+// Counts of the kEach pages from the first-th on; those behind the last count as used.
 template <int kEach>
 __device__ inline void refs_of(const BookParams& p, int64_t first, int (&r)[kEach]) {
   if (first + kEach <= p.n_pages && reinterpret_cast<uintptr_t>(p.refs) % 16 == 0) {
@@ -433,15 +433,16 @@ __global__ __launch_bounds__(1024) void pages_compact_kernel(BookParams p, int32
 #pragma unroll 4
   for (int i = tid; i < entries; i += 1024) {
     const int entry = p.table[i];
-    if (is_page(entry, p) && entry >= 0) p.table[i] = new_place[entry];
+    if (is_page(entry, p)) p.table[i] = new_place[entry];
   }
 }
 
 __global__ __launch_bounds__(256) void pages_rename_kernel(BookParams p, const int32_t* new_place) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= static_cast<int64_t>(p.n_queries) * p.table_stride) return;
-  const int entry = p.table[i];
-  if (is_page(entry, p)) p.table[i] = new_place[entry];
+  const int64_t entries = static_cast<int64_t>(p.n_queries) * p.table_stride, step = static_cast<int64_t>(gridDim.x) * 256;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < entries; i += step) {
+    const int entry = p.table[i];
+    if (is_page(entry, p)) p.table[i] = new_place[entry];
+  }
 }
 
 // ---- copy ------------------------------------------------------------------------------------------------------
@@ -518,7 +519,8 @@ hipError_t launch_pages_compact(const BookParams& p, int32_t* copies, int32_t* c
   if (p.n_pages <= 8192) pages_compact_kernel<4><<<dim3(1), dim3(1024), 0, stream>>>(p, copies, counts, new_place, renames);
   else pages_compact_kernel<16><<<dim3(1), dim3(1024), 0, stream>>>(p, copies, counts, new_place, renames);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || renames) return e;
-  pages_rename_kernel<<<dim3(static_cast<unsigned>((entries + 255) / 256)), dim3(256), 0, stream>>>(p, new_place);
+  const int64_t blocks = (entries + 255) / 256;
+  pages_rename_kernel<<<dim3(static_cast<unsigned>(blocks < 65536 ? blocks : 65536)), dim3(256), 0, stream>>>(p, new_place);
   return hipGetLastError();
 }
 

@@ -461,7 +461,21 @@ __device__ Decision decide(const VerifyParams& p, const Work& w, int u, const Sp
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) falls |= falls_sh[i];
     const int stop = falls ? __ffs(falls) - 1 : kRows;
-    if (group == stop && speaks) decision_sh = d;
+    if (group == stop && speaks) {  // (field by field: copied as a whole it goes through scratch memory)
+      decision_sh.row = d.row;
+      decision_sh.step = d.step;
+      decision_sh.refused = d.refused;
+      decision_sh.proposal = d.proposal;
+      decision_sh.number = d.number;
+      if constexpr (kLogits) {
+        decision_sh.place = d.place;
+        decision_sh.top_p = d.top_p;
+        decision_sh.top_q = d.top_q;
+        decision_sh.log_p = d.log_p;
+        decision_sh.inv_p = d.inv_p;
+        decision_sh.inv_q = d.inv_q;
+      }
+    }
     if (tells && speaks && row < s.end && group != stop) {
       p.out[row] = group < stop ? x : -1;
       if (p.logp) p.logp[row] = group < stop ? static_cast<float>(log_of<kLogits>(v, d.top_p, d.log_p, heat.factor)) : 0.f;
@@ -497,12 +511,11 @@ __device__ inline void tell_token(const VerifyParams& p, const Decision& d, int 
     p.logp[d.row] = token < 0 ? 0.f : static_cast<float>(log_of<kLogits>(at(target_row<T>(p, d.row), token), d.top_p, d.log_p, factor));
 }
 
-// One workgroup: question u.
-template <typename T, bool kLogits>
+// One workgroup: question u, from logits.
+template <typename T>
 __global__ __launch_bounds__(kThreads) void verify_decide_kernel(VerifyParams p, int piece) {
   const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
   const int u = blockIdx.x;
-  if (threadIdx.x == 0) w.done[static_cast<int64_t>(u) * kApart] = 0;
   const Span s = span_of(p, u);
   if (s.begin == s.end) {
     if (threadIdx.x == 0) w.decision[u].row = -1;
@@ -510,10 +523,10 @@ __global__ __launch_bounds__(kThreads) void verify_decide_kernel(VerifyParams p,
     return;
   }
   const Heat heat = heat_of(p, u);
-  Decision d = decide<T, kLogits>(p, w, u, s, heat, true);
+  Decision d = decide<T, true>(p, w, u, s, heat, true);
   if (threadIdx.x > 0) return;
-  if (kLogits && heat.greedy) {
-    tell_token<T, kLogits>(p, d, d.place, heat.factor);
+  if (heat.greedy) {
+    tell_token<T, true>(p, d, d.place, heat.factor);
     d.row = -1;
   }
   w.decision[u] = d;
@@ -805,24 +818,30 @@ void launch(const VerifyParams& p, hipStream_t stream) {
   const int piece = rows * p.vocab >= int64_t{1} << 25 ? 4 * kPieceLeast : kPieceLeast;
   const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
   const dim3 threads(kThreads);
-  constexpr int64_t kFull = kLogits ? 2048 : 4096;  // workgroups that fill the chip a few times (half and twice as many: 3 to 9 % slower)
+  // workgroups that fill the chip (logits: half as many 123 us instead of 114 for 128 x 4 in bf16; probabilities of 128 questions in
+  // fp32 37 us, twice as many 41, four times 39)
+  constexpr int64_t kFull = kLogits ? 2048 : 1024;
   // shares of a workgroup, a multiple of its waves; nothing is weighed by more than one where no distribution is taken off
   const int64_t most = pieces_of(w.shares, kWaves), per = kLogits && !p.draft ? most : (p.n_queries * most + kFull - 1) / kFull;
   const int each = static_cast<int>(per * kWaves), parts = static_cast<int>(pieces_of(w.shares, each));
-  const bool apart = static_cast<int64_t>(p.n_queries) * parts > 512;
+  const dim3 grid(static_cast<unsigned>(p.n_queries) * parts);
   if (kLogits && rows > 0) {
     const int64_t cells = rows * w.pieces;
     verify_stats_kernel<T><<<dim3(static_cast<unsigned>((cells + kWaves - 1) / kWaves)), threads, 0, stream>>>(p, piece);
-  } else if (!apart) {
+  } else {
     verify_clear_kernel<<<dim3((p.n_queries + kThreads - 1) / kThreads), threads, 0, stream>>>(p, piece);
   }
-  const dim3 grid(static_cast<unsigned>(p.n_queries) * parts);
-  if (apart) {
-    verify_decide_kernel<T, kLogits><<<dim3(p.n_queries), threads, 0, stream>>>(p, piece);
-    verify_draw_kernel<T, kLogits, true><<<grid, threads, 0, stream>>>(p, piece, parts, each);
-  } else {
-    verify_draw_kernel<T, kLogits, false><<<grid, threads, 0, stream>>>(p, piece, parts, each);
+  if constexpr (kLogits) {
+    // Each workgroup of a question decides for itself, which takes 3 us, while they all run at once; for more of them one does, 6.5 us
+    // before the others begin: 128 x 4 in bf16 114 us against 119, 128 x 3 over 20000 words (1280 workgroups) 36 against 35.  (From
+    // probabilities it takes less: never apart, 45 against 43 and 25 against 24 us.)
+    if (static_cast<int64_t>(p.n_queries) * parts > 1536) {
+      verify_decide_kernel<T><<<dim3(p.n_queries), threads, 0, stream>>>(p, piece);
+      verify_draw_kernel<T, true, true><<<grid, threads, 0, stream>>>(p, piece, parts, each);
+      return;
+    }
   }
+  verify_draw_kernel<T, kLogits, false><<<grid, threads, 0, stream>>>(p, piece, parts, each);
 }
 
 }  // namespace

@@ -155,6 +155,38 @@ def test_values_that_are_no_numbers(dtype, heat):
     same(call(c), wanted(c), c, f"no probabilities {dtype}")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_masks_of_the_lowest_value(dtype):
+    """What is masked with the type's lowest value weighs nothing beside what is not, and as much as the rest where all is; values far
+    beyond what the exponent's whole numbers hold are counted from the largest."""
+    low = float(torch.finfo(TYPES[dtype]).min)
+    for heat in (None, [1.0, 0.0, 0.4, 1e30, 3.0, 1.0], [1e-3] * 6):
+        for draft in (True, False):
+            c = make(45, [3, 3, 3, 2, 2, 2], 9001, dtype, draft=draft, heat=heat)
+            hide = torch.from_numpy(np.random.default_rng(1).random(c["x"].shape) < 0.99)
+            c["x"][hide] = low
+            c["x"][4] = low                       # everything is
+            c["x"][6, :5000] = -float("inf")      # either kind
+            c["x"][7], c["x"][7, 8000] = low, -1e30
+            c["x"][9] = c["x"][9].clamp_min(-10) * 1e30
+            c["x"][11] = c["x"][11].clamp_min(-10) + 3e6
+            c["x"][13, 100], c["x"][13, 8900] = 3e5, 3e5 + 2048
+            if draft:
+                c["y"][1, 1] = low
+                c["y"][3, 0] = c["y"][3, 0] * 1e30
+                c["y"][4, 0] = c["y"][4, 0] + 3e6
+            same(call(c), wanted(c), c, f"lowest {dtype} {heat} {draft}")
+
+
+def test_no_tokens_at_all():
+    for probs in (False, True):
+        n = torch.tensor([7, 9], dtype=torch.int32, device="cuda")
+        x, empty = torch.zeros((0, 50), device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+        out, accepted = B.dbsa_draft_verify(x, empty, torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(0, device="cuda"), probs=probs,
+                                            self_len=n, new_len=n, accepted=torch.full((2,), 5, dtype=torch.int32, device="cuda"))
+        assert out.numel() == 0 and accepted.tolist() == [0, 0] and n.tolist() == [7, 9]
+
+
 def test_proposals_that_are_none():
     """-1, words outside the vocabulary, more tokens than what proposed has rows for: the chain ends, the target is drawn from."""
     for dtype in ("bf16", "f32"):

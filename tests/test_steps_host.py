@@ -129,7 +129,7 @@ def book(**change):
 BAD_BOOKS = [(dict(refs=None), B.DBSA_ERR_INVALID_ARG), (dict(pages=0), B.DBSA_ERR_INVALID_ARG), (dict(table=None), B.DBSA_ERR_INVALID_ARG),
              (dict(columns=0), B.DBSA_ERR_INVALID_ARG), (dict(b=-1), B.DBSA_ERR_INVALID_ARG), (dict(page=8), B.DBSA_ERR_UNSUPPORTED),
              (dict(page=48), B.DBSA_ERR_UNSUPPORTED), (dict(page=0), B.DBSA_ERR_UNSUPPORTED), (dict(b=4097), B.DBSA_ERR_UNSUPPORTED),
-             (dict(columns=(1 << 24) + 1), B.DBSA_ERR_UNSUPPORTED)]
+             (dict(columns=(1 << 20) + 1), B.DBSA_ERR_UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("change,code", BAD_BOOKS + [(dict(self_len=None), B.DBSA_ERR_INVALID_ARG), (dict(b=0), B.DBSA_ERR_INVALID_ARG)])
@@ -179,7 +179,7 @@ def copy(**change):
     (dict(stride_layer=0), B.DBSA_ERR_INVALID_ARG), (dict(copies=None), B.DBSA_ERR_INVALID_ARG), (dict(n=None), B.DBSA_ERR_INVALID_ARG),
     (dict(most=-1), B.DBSA_ERR_INVALID_ARG), (dict(heads=0), B.DBSA_ERR_INVALID_ARG), (dict(pages=0), B.DBSA_ERR_INVALID_ARG),
     (dict(dim=96), B.DBSA_ERR_UNSUPPORTED), (dict(dtype=3), B.DBSA_ERR_UNSUPPORTED), (dict(page=24), B.DBSA_ERR_UNSUPPORTED),
-    (dict(page=1 << 29), B.DBSA_ERR_UNSUPPORTED),
+    (dict(page=1 << 29), B.DBSA_ERR_UNSUPPORTED), (dict(page=1 << 20, layers=1 << 22), B.DBSA_ERR_UNSUPPORTED),
 ])
 def test_copy_refuses(change, code):
     assert copy(**change) == code
