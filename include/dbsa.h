@@ -650,9 +650,9 @@ int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, co
  *                draws.  (Where it is outside, the draw takes the last token with a weight.)
  *   out_tokens : device int32 [n_tokens]: the tokens that stand, the drawn one, then -1, from the question's first row on; rows
  *                of no question are left alone.  A row without any probability draws -1; where w is 0 throughout (p nowhere above
- *                q) the draw is from p_n.  Not the same array as tokens.
+ *                q) the draw is from p_n.  Not to overlap tokens.
  *   accepted   : device int32 [n_queries]: how many stand.
- *   logp       : optional device float [n_tokens]: log p of each token of out_tokens (where T is not above 0: of T = 1), 0 in
+ *   logp       : optional device float [n_tokens], not to overlap uniform: log p of each token of out_tokens (where T is not above 0: of T = 1), 0 in
  *                rows without one.
  *   self_len, new_len : optional device int32 [n_queries], both or none: the own keys at the chunk's attention call, and those
  *                of the tokens that stand: self_len - (T_u - 1 - accepted).  May be the same array.

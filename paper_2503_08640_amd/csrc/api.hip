@@ -1330,7 +1330,13 @@ int dbsa_draft_verify(const void* target, int64_t target_stride, const dbsa_draf
   if (dtype != DBSA_BF16 && dtype != DBSA_F32) return DBSA_ERR_UNSUPPORTED;
   if (form != DBSA_LOGITS && form != DBSA_PROBABILITIES) return DBSA_ERR_UNSUPPORTED;
   if (!cu_qlens || !accepted || n_tokens < 0 || n_queries < 1 || vocab < 1 || !self_len != !new_len) return DBSA_ERR_INVALID_ARG;
-  if (n_tokens > 0 && (!target || !tokens || !uniform || !out_tokens || out_tokens == tokens)) return DBSA_ERR_INVALID_ARG;
+  if (n_tokens > 0 && (!target || !tokens || !uniform || !out_tokens)) return DBSA_ERR_INVALID_ARG;
+  // (every workgroup of a question reads what one of them writes beside)
+  auto meet = [n_tokens](const void* a, const void* b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b), bytes = static_cast<uintptr_t>(n_tokens) * 4;
+    return x < y + bytes && y < x + bytes;
+  };
+  if (n_tokens > 0 && (meet(out_tokens, tokens) || (logp && meet(logp, uniform)))) return DBSA_ERR_INVALID_ARG;
   if (form == DBSA_PROBABILITIES && temperature) return DBSA_ERR_INVALID_ARG;
   const uintptr_t size = dtype == DBSA_BF16 ? 2 : 4;
   if (reinterpret_cast<uintptr_t>(target) % size != 0 || target_stride < 0) return DBSA_ERR_INVALID_ARG;

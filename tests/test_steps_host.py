@@ -87,7 +87,7 @@ def test_books_stay_consistent():
 
 def verify(**change):
     a = dict(target=A, stride=1000, draft=None, tokens=A, cu=A, n=5, b=1, vocab=1000, dtype=B.DBSA_BF16, form=B.DBSA_LOGITS, heat=None,
-             uniform=A, out=2 * A, accepted=A, logp=None, self_len=None, new_len=None, ws=A, ws_bytes=None)
+             uniform=A, out=1 << 40, accepted=A, logp=None, self_len=None, new_len=None, ws=A, ws_bytes=None)
     a.update(change)
     d = None if a["draft"] is None else C.byref(B.Draft(*a["draft"]))
     need = B.dbsa_draft_verify_workspace_bytes(a["n"], a["b"], a["vocab"]) if a["ws_bytes"] is None else a["ws_bytes"]
@@ -100,7 +100,8 @@ def verify(**change):
     (dict(target=None), B.DBSA_ERR_INVALID_ARG), (dict(tokens=None), B.DBSA_ERR_INVALID_ARG), (dict(cu=None), B.DBSA_ERR_INVALID_ARG),
     (dict(uniform=None), B.DBSA_ERR_INVALID_ARG), (dict(out=None), B.DBSA_ERR_INVALID_ARG), (dict(accepted=None), B.DBSA_ERR_INVALID_ARG),
     (dict(n=-1), B.DBSA_ERR_INVALID_ARG), (dict(b=0), B.DBSA_ERR_INVALID_ARG), (dict(vocab=0), B.DBSA_ERR_INVALID_ARG),
-    (dict(out=A), B.DBSA_ERR_INVALID_ARG), (dict(self_len=A), B.DBSA_ERR_INVALID_ARG), (dict(new_len=A), B.DBSA_ERR_INVALID_ARG),
+    (dict(out=A), B.DBSA_ERR_INVALID_ARG), (dict(out=A + 4), B.DBSA_ERR_INVALID_ARG), (dict(out=A - 16), B.DBSA_ERR_INVALID_ARG),
+    (dict(logp=A + 8), B.DBSA_ERR_INVALID_ARG), (dict(self_len=A), B.DBSA_ERR_INVALID_ARG), (dict(new_len=A), B.DBSA_ERR_INVALID_ARG),
     (dict(target=A + 1), B.DBSA_ERR_INVALID_ARG), (dict(target=A + 2, dtype=B.DBSA_F32), B.DBSA_ERR_INVALID_ARG),
     (dict(stride=-1), B.DBSA_ERR_INVALID_ARG), (dict(draft=(A + 1, 1, 1, 1)), B.DBSA_ERR_INVALID_ARG),
     (dict(draft=(A, -1, 1, 1)), B.DBSA_ERR_INVALID_ARG), (dict(draft=(A, 1, -1, 1)), B.DBSA_ERR_INVALID_ARG),
