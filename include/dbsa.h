@@ -635,8 +635,8 @@ int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, co
  *
  *   target     : device [n_tokens, vocab] of dtype (n_tokens may be 0: every question is without rows), rows target_stride elements apart (any alignment), packed by cu_qlens.
  *   draft      : rows of the same form and dtype that the proposals were drawn from: that of proposal a of question u begins at
- *                element u * stride_query + a * stride_step, a < n_steps.  NULL, or ptr NULL: the proposals were not drawn at
- *                random (q = 1 at the proposal).
+ *                element u * stride_query + a * stride_step, a < n_steps (0: no proposal has a row; ptr is
+ *                then any address but NULL).  NULL, or ptr NULL: the proposals were not drawn at random (q = 1 at the proposal).
  *   tokens     : device int32 [n_tokens], the chunk's tokens.  One that is no token of the vocabulary (-1), or has no row
  *                in draft, ends the proposals: nothing is taken from p_n there.
  *   cu_qlens   : device int32 [n_queries + 1], ascending from 0, each at most n_tokens; a question may have no rows.

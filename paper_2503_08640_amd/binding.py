@@ -815,10 +815,10 @@ def dbsa_draft_verify(target, tokens, cu_qlens, uniform, draft=None, temperature
     assert _ints(out, n) and _ints(accepted, b)
     assert (self_len is None) == (new_len is None) and (self_len is None or (_ints(self_len, b) and _ints(new_len, b)))
     d = None
-    if draft is not None and draft.shape[1] > 0:
+    if draft is not None:
         s, (questions, steps, words) = draft.stride(), draft.shape
         assert draft.dtype is target.dtype and questions == b and words == vocab and s[2] == 1, "expected draft scores [B, steps, V]"
-        d = C.byref(Draft(draft.data_ptr(), s[0], s[1], steps))
+        d = C.byref(Draft(draft.data_ptr() if steps > 0 else cu_qlens.data_ptr(), s[0], s[1], steps))  # (no rows: no address)
     if workspace is None:
         workspace = torch.empty(max(16, dbsa_draft_verify_workspace_bytes(n, b, vocab)), dtype=torch.uint8, device=target.device)
     stream = _here(target, tokens, cu_qlens, uniform, draft, temperature, out, accepted, logp, self_len, new_len, workspace)

@@ -1341,7 +1341,7 @@ int dbsa_draft_verify(const void* target, int64_t target_stride, const dbsa_draf
   const uintptr_t size = dtype == DBSA_BF16 ? 2 : 4;
   if (reinterpret_cast<uintptr_t>(target) % size != 0 || target_stride < 0) return DBSA_ERR_INVALID_ARG;
   const bool drawn = draft && draft->ptr;
-  if (drawn && (reinterpret_cast<uintptr_t>(draft->ptr) % size != 0 || draft->stride_query < 0 || draft->stride_step < 0 || draft->n_steps < 1))
+  if (drawn && (reinterpret_cast<uintptr_t>(draft->ptr) % size != 0 || draft->stride_query < 0 || draft->stride_step < 0 || draft->n_steps < 0))
     return DBSA_ERR_INVALID_ARG;
   const int64_t pieces = (int64_t{vocab} + 8 + 4095) / 4096;  // (a grid counts its threads in 32 bits)
   if (vocab > 1 << 30 || std::max<int64_t>(n_tokens, n_queries) * pieces > 1 << 23) return DBSA_ERR_UNSUPPORTED;
@@ -1350,11 +1350,11 @@ int dbsa_draft_verify(const void* target, int64_t target_stride, const dbsa_draf
   VerifyParams p{};
   p.target = target;
   p.target_stride = target_stride;
-  if (drawn) {
+  p.draft_steps = drawn ? draft->n_steps : INT32_MAX;
+  if (drawn && draft->n_steps > 0) {
     p.draft = draft->ptr;
     p.draft_query = draft->stride_query;
     p.draft_step = draft->stride_step;
-    p.draft_steps = draft->n_steps;
   }
   p.tokens = tokens;
   p.cu = cu_qlens;

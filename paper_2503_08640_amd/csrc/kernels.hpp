@@ -170,7 +170,7 @@ struct VerifyParams {
   int64_t target_stride;
   const void* draft;    // null, or step a of question u at u * draft_query + a * draft_step
   int64_t draft_query, draft_step;
-  int32_t draft_steps;
+  int32_t draft_steps;  // rows that check a proposal (no draft: any number, or none)
   const int32_t *tokens, *cu;   // device [n_tokens], [n_queries + 1]
   const float *uniform, *heat;  // device [n_tokens]; [n_queries] or null
   const int32_t* self_len;      // device [n_queries] or null

@@ -200,7 +200,7 @@ __device__ inline const T* draft_row(const VerifyParams& p, int64_t u, int64_t s
 }
 // whether row t checks proposal x: a token of the vocabulary that a row of probabilities belongs to
 __device__ inline bool proposes(const VerifyParams& p, const Span& s, int row, int x) {
-  return row + 1 < s.end && x >= 0 && x < p.vocab && (!p.draft || row - s.begin < p.draft_steps);
+  return row + 1 < s.end && x >= 0 && x < p.vocab && row - s.begin < p.draft_steps;
 }
 
 // 16 / sizeof(T) values from the first-th on, in two steps, so that several loads are in flight before one is waited for: the

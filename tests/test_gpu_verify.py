@@ -202,6 +202,22 @@ def test_proposals_that_are_none():
                     same(call(c), wanted(c), c, f"two rows of five {dtype} {form}")
 
 
+@pytest.mark.parametrize("form", ["logits", "probs"])
+@pytest.mark.parametrize("heat", [None, [0.0, 0.7, 1.0]])
+def test_what_proposed_has_no_rows(form, heat):
+    """[B, 0, V]: no proposal of these can be checked, which is not the same as proposals that were not drawn."""
+    if form == "probs" and heat:
+        heat = None
+    c = make(62, [5, 1, 3], 2500, "f32", form, heat=heat)
+    c["y"] = c["y"][:, :0]
+    want = wanted(c)
+    assert want["accepted"].tolist() == [0, 0, 0]
+    same(call(c), want, c, f"no rows {form} {heat}")
+    c["y"] = None
+    assert (wanted(c)["accepted"] > 0).any()
+    same(call(c), wanted(c), c, f"looked up {form} {heat}")
+
+
 def test_random_numbers_at_their_ends():
     for form in ("logits", "probs"):
         for u in (0.0, 1.0 - 2.0 ** -24, 1.0, 7.0, -1.0):

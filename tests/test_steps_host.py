@@ -105,7 +105,7 @@ def verify(**change):
     (dict(target=A + 1), B.DBSA_ERR_INVALID_ARG), (dict(target=A + 2, dtype=B.DBSA_F32), B.DBSA_ERR_INVALID_ARG),
     (dict(stride=-1), B.DBSA_ERR_INVALID_ARG), (dict(draft=(A + 1, 1, 1, 1)), B.DBSA_ERR_INVALID_ARG),
     (dict(draft=(A, -1, 1, 1)), B.DBSA_ERR_INVALID_ARG), (dict(draft=(A, 1, -1, 1)), B.DBSA_ERR_INVALID_ARG),
-    (dict(draft=(A, 1, 1, 0)), B.DBSA_ERR_INVALID_ARG), (dict(form=B.DBSA_PROBABILITIES, heat=A), B.DBSA_ERR_INVALID_ARG),
+    (dict(draft=(A, 1, 1, -1)), B.DBSA_ERR_INVALID_ARG), (dict(form=B.DBSA_PROBABILITIES, heat=A), B.DBSA_ERR_INVALID_ARG),
     (dict(dtype=B.DBSA_E4M3), B.DBSA_ERR_UNSUPPORTED), (dict(form=2), B.DBSA_ERR_UNSUPPORTED),
     (dict(vocab=(1 << 30) + 1, ws_bytes=1 << 60), B.DBSA_ERR_UNSUPPORTED), (dict(n=1 << 20, vocab=200000), B.DBSA_ERR_UNSUPPORTED),
     (dict(ws=None), B.DBSA_ERR_WORKSPACE), (dict(ws=A + 8), B.DBSA_ERR_WORKSPACE), (dict(ws_bytes=64), B.DBSA_ERR_WORKSPACE),
