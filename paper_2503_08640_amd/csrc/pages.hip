@@ -14,14 +14,12 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 
 __device__ inline bool is_page(int entry, const BookParams& p) { return entry >= 0 && entry < p.n_pages; }
 
-// Tokens of row u, as far as the row reaches.
-__device__ inline int64_t tokens_of(const BookParams& p, int u) {
-  const int64_t most = static_cast<int64_t>(p.table_stride) << p.page_log2;
-  const int64_t n = p.self_len[u];
-  return n < 0 ? 0 : n < most ? n : most;
-}
 __device__ inline int pages_for(int64_t tokens, const BookParams& p) {
   return static_cast<int>((tokens + (int64_t{1} << p.page_log2) - 1) >> p.page_log2);
+}
+// Pages of a row with so many tokens, as far as the row reaches.
+__device__ inline int pages_used(int length, const BookParams& p) {
+  return length < 0 ? 0 : min(pages_for(length, p), p.table_stride);
 }
 
 // ---- fork ------------------------------------------------------------------------------------------------------
@@ -29,29 +27,27 @@ __device__ inline int pages_for(int64_t tokens, const BookParams& p) {
 constexpr int kForkEach = 8;  // entries of a thread
 
 // A workgroup takes 2^columns_log2 columns of all rows: what the copies read of a column is in registers before any row of that
-// column is written, so that rows may go round in a circle.  The counts are what takes its time (device-wide integer atomics, 13e9 a
-// second; their order does not matter), so that an entry's whole change is one: the copies made of its row less the row's own loss
-// of it.  alone: the one workgroup of the launch, which sees to the lengths as well.  512 rows of 375 pages, half of them forked: 12.5
-// us (18 with a change for the loss and one for the copy, 71 with the loads one after the other), 8 rows of 57 pages 2.4.
+// column is written, so that rows may go round in a circle.  The counts are nearly half of its time (device-wide integer atomics; their
+// order does not matter), so that an entry's whole change is one: the copies made of its row less the row's own loss of it.
+// alone: the one workgroup of the launch, which sees to the lengths as well.  512 rows of 375 pages, half of them forked: 9.0 us with 8
+// columns to a workgroup (12.5 with 16; before that 18 with a change for the loss and one for the copy, 71 with the loads one after the
+// other), 8 rows of 57 pages 2.4.  One change for neighbours that name the same page, a thread having eight rows in a column, gained
+// 1 us of 13 in beams that share most pages and lost as much in rows that share none and in small tables.
 __global__ __launch_bounds__(1024) void pages_fork_kernel(BookParams p, const int32_t* source, int columns_log2, bool alone) {
-  __shared__ int used_sh[kBookQuestions];         // pages of a row's tokens
+  __shared__ int length_sh[kBookQuestions];
   __shared__ int copies_sh[kBookQuestions];       // copies made of the row
   __shared__ uint16_t source_sh[kBookQuestions];  // kStays: the row stays as it is
   constexpr uint16_t kStays = 0xffff;
   const int tid = threadIdx.x;
   for (int u = tid; u < p.n_queries; u += 1024) {
+    const int s = source[u];
     copies_sh[u] = 0;
-    used_sh[u] = pages_for(tokens_of(p, u), p);
+    length_sh[u] = p.self_len[u];
+    source_sh[u] = s >= 0 && s < p.n_queries && s != u ? static_cast<uint16_t>(s) : kStays;
   }
   __syncthreads();
-  int length = 0;
-  for (int u = tid; u < p.n_queries; u += 1024) {
-    const int s = source[u];
-    const bool forks = s >= 0 && s < p.n_queries && s != u;
-    source_sh[u] = forks ? static_cast<uint16_t>(s) : kStays;
-    if (forks) atomicAdd(&copies_sh[s], 1);
-    if (alone && forks) length = p.self_len[s];  // (alone: a thread has one row at most)
-  }
+  for (int u = tid; u < p.n_queries; u += 1024)
+    if (source_sh[u] != kStays) atomicAdd(&copies_sh[source_sh[u]], 1);
   __syncthreads();
   const int c = (blockIdx.x << columns_log2) + (tid & ((1 << columns_log2) - 1)), first = tid >> columns_log2, step = 1024 >> columns_log2;
   int old[kForkEach], now[kForkEach];
@@ -62,7 +58,7 @@ __global__ __launch_bounds__(1024) void pages_fork_kernel(BookParams p, const in
     if (u >= p.n_queries || c >= p.table_stride) continue;
     const int s = source_sh[u];
     if (s != kStays || copies_sh[u] > 0) old[i] = p.table[static_cast<int64_t>(u) * p.table_stride + c];
-    if (s != kStays && c < used_sh[s]) now[i] = p.table[static_cast<int64_t>(s) * p.table_stride + c];
+    if (s != kStays && c < pages_used(length_sh[s], p)) now[i] = p.table[static_cast<int64_t>(s) * p.table_stride + c];
   }
   __syncthreads();
 #pragma unroll
@@ -70,12 +66,12 @@ __global__ __launch_bounds__(1024) void pages_fork_kernel(BookParams p, const in
     const int u = first + i * step;
     if (u >= p.n_queries || c >= p.table_stride) continue;
     const bool forks = source_sh[u] != kStays;
-    const int change = (c < used_sh[u] ? copies_sh[u] : 0) - forks;
+    const int change = (c < pages_used(length_sh[u], p) ? copies_sh[u] : 0) - forks;
     if (is_page(old[i], p) && change != 0) atomicAdd(p.refs + old[i], change);
     if (!is_page(now[i], p)) now[i] = -1;
     if (forks && now[i] != old[i]) p.table[static_cast<int64_t>(u) * p.table_stride + c] = now[i];
   }
-  if (alone && tid < p.n_queries && source_sh[tid] != kStays) p.self_len[tid] = length;
+  if (alone && tid < p.n_queries && source_sh[tid] != kStays) p.self_len[tid] = length_sh[source_sh[tid]];
 }
 
 __global__ __launch_bounds__(1024) void pages_fork_lengths_kernel(BookParams p, const int32_t* source) {
@@ -348,7 +344,7 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const
 __global__ __launch_bounds__(256) void pages_trim_kernel(BookParams p) {
   const int per_row = (p.table_stride + 1023) / 1024;
   const int u = blockIdx.x / per_row, first = (blockIdx.x % per_row) * 1024 + threadIdx.x;
-  const int keep = pages_for(tokens_of(p, u), p);
+  const int keep = pages_used(p.self_len[u], p);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int c = first + 256 * e;
@@ -493,12 +489,12 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(PagesCopyParams p) {
 }  // namespace
 
 hipError_t launch_pages_fork(const BookParams& p, const int32_t* source, hipStream_t stream) {
-  // as many columns as the workgroup's registers hold; a table that fits into one workgroup is one launch, others have 32 columns
-  // to a workgroup at most
+  // as many columns as the workgroup's registers hold; a table that fits into one workgroup is one launch, others have 8 columns
+  // to a workgroup at most (512 rows 11.5 us with the lengths, 16 columns 15.2, 4 columns 12.4)
   int columns_log2 = 0;
   while ((1 << columns_log2) < p.table_stride && (p.n_queries << (columns_log2 + 1)) <= 1024 * kForkEach && (1 << columns_log2) < 1024) ++columns_log2;
   const bool alone = (1 << columns_log2) >= p.table_stride && p.n_queries <= 1024;
-  if (!alone && columns_log2 > 5) columns_log2 = 5;
+  if (!alone && columns_log2 > 3) columns_log2 = 3;
   const int blocks = (p.table_stride + (1 << columns_log2) - 1) >> columns_log2;
   pages_fork_kernel<<<dim3(blocks), dim3(1024), 0, stream>>>(p, source, columns_log2, alone);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || alone) return e;
