@@ -389,7 +389,8 @@ __device__ inline RowSum row_sum(const Work& w, int64_t which, Piece first, doub
   for (int s = kGroup / 2; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
   return {scale, sum};
 }
-__device__ inline int row_place(const Work& w, int64_t which) {
+// (an index into the row, whatever the pieces hold: those of rows that belong to no question, or to one of other bounds, are not written)
+__device__ inline int row_place(const Work& w, int64_t which, int vocab) {
   const int lane = threadIdx.x % kGroup;
   const int64_t base = which * w.pieces;
   float peak = -INFINITY;
@@ -405,7 +406,7 @@ __device__ inline int row_place(const Work& w, int64_t which) {
   place = peak == all ? place : INT32_MAX;
 #pragma unroll
   for (int s = kGroup / 2; s > 0; s >>= 1) place = min(place, __shfl_xor(place, s));
-  return place == INT32_MAX ? -1 : place;
+  return place >= 0 && place < vocab ? place : -1;
 }
 __device__ inline double inverse(double sum) { return sum > 0 ? 1.0 / sum : 0.0; }
 
@@ -442,7 +443,7 @@ __device__ Decision decide(const VerifyParams& p, const Work& w, int u, const Sp
       double mine;  // p(x), in the other half of the lanes q(x)
       if constexpr (kLogits) {
         mine = 0.0;
-        if (heat.greedy) d.place = row_place(w, row);
+        if (heat.greedy) d.place = row_place(w, row, p.vocab);
         if (sums) {
           const RowSum sum = row_sum(w, which, piece, heat.factor);
           d.top_p = sum.scale.top;

@@ -342,3 +342,20 @@ def test_bounds_that_do_not_ascend_stay_inside():
                             draft=dev(c["y"]), out=full[2:8], logp=torch.zeros(6, device="cuda"))
         torch.cuda.synchronize()
         assert (full[:2] == -77).all() and (full[8:] == -77).all()
+
+
+@pytest.mark.parametrize("byte", [0x7e, 0x80])
+def test_rows_that_two_questions_claim_stay_inside(byte):
+    """The second row lies in front of the bound behind it and belongs to no question's statistics, while two questions decide by it: what
+    the workspace held there (a large value at a word far outside, or a negative one) is not taken for a word."""
+    vocab = 600
+    for heat, logits in (([0.0] * 3, True), ([0.7, 0.0, 1.0], True), (None, True), (None, False)):
+        c = make(320, [1, 1, 1], vocab, "f32", "logits" if logits else "probs", draft=False, heat=heat)
+        need = B.dbsa_draft_verify_workspace_bytes(3, 3, vocab)
+        full, logp = torch.full((7,), -77, dtype=torch.int32, device="cuda"), torch.zeros(3, device="cuda")
+        B.dbsa_draft_verify(dev(c["x"]), dev(c["tokens"]), torch.tensor([0, 2, 1, 3], dtype=torch.int32, device="cuda"), dev(c["uniform"]),
+                            temperature=dev(c["heat"]), probs=not logits, out=full[2:5], logp=logp,
+                            workspace=torch.full((need,), byte, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        assert (full[:2] == -77).all() and (full[5:] == -77).all()
+        assert (full[2:5] >= -1).all() and (full[2:5] < vocab).all(), full.tolist()
