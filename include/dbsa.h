@@ -704,13 +704,17 @@ typedef struct {
 int dbsa_pages_fork(const dbsa_page_book* book, const int32_t* source, void* stream);
 
 /*
- * Room for add[u] (device int32) more tokens of each question, which self_len then counts.  In the order of the questions:
+ * Room for add[u] (device int32) more tokens of each question, which self_len then counts: what they are written to, no other entry
+ * names.  First, entries behind a question's last page in use that its new tokens reach into, and whose page more than one entry
+ * names as the call begins, are given back as by dbsa_pages_trim (a question that was cut shares them still; they hold none of its
+ * tokens).  Then, in the order of the questions:
  *   - a last page that is partly used and that, after the questions before, more than one entry names is replaced by a free
  *     one, and (old page, new page, rows in use) is added to the copies: the caller passes them to dbsa_pages_copy for its caches
  *     before it writes the new tokens' keys;
  *   - entries the new tokens reach into that name no page get free ones.
  * Free pages are taken from the lowest up.  From the first question on that they do not suffice for, questions are left as they
- * are.  A question whose row of the table is too short, or whose partly used last page is not there, is left as it is.
+ * are (but for what was given back).  A question whose row of the table is too short, or whose partly used last page is not there,
+ * is left as it is.
  *   got      : device int32 [n_queries], written: add[u], or 0 for a question that is left as it is.
  *   copies   : device int32 [n_queries][3]; n_copies: device int32, how many were written (the rest is left alone).
  *   workspace: device memory of >= 4 * n_pages bytes, 4-byte aligned.

@@ -102,21 +102,35 @@ class Books:
                 self.table[u, c] = now
             self.self_len[u] = length[s]
 
+    def _asks(self, u, more):
+        """Whether question u can be served at all, and the columns its new tokens reach into behind its last page in use."""
+        n = max(int(self.self_len[u]), 0)
+        if more <= 0 or n + more > self.table.shape[1] * self.page:
+            return False, range(0)
+        if n % self.page and not self._is_page(int(self.table[u, n // self.page])):
+            return False, range(0)
+        return True, range(self._used(n), self._used(n + more))
+
     def reserve(self, add):
         """-> (got, copies)"""
+        # what lies behind the tokens holds nothing: entries that share their page go back before anything is handed out
+        before = self.refs.copy()
+        for u, more in enumerate(int(x) for x in add):
+            for c in self._asks(u, more)[1]:
+                if self._is_page(self.table[u, c]) and before[self.table[u, c]] > 1:
+                    self.refs[self.table[u, c]] -= 1
+                    self.table[u, c] = -1
         free = [p for p in range(len(self.refs)) if self.refs[p] <= 0]
         got, copies, stopped = np.zeros(len(add), np.int64), [], False
         for u, more in enumerate(int(x) for x in add):
             n = max(int(self.self_len[u]), 0)
-            if stopped or more <= 0 or n + more > self.table.shape[1] * self.page:
+            asks, reached = self._asks(u, more)
+            if stopped or not asks:
                 continue
-            rows, tail = n % self.page, -1
-            if rows:
-                tail = int(self.table[u, n // self.page])
-                if not self._is_page(tail):
-                    continue
+            rows = n % self.page
+            tail = int(self.table[u, n // self.page]) if rows else -1
             replace = tail >= 0 and self.refs[tail] > 1
-            lacks = [c for c in range(self._used(n), self._used(n + more)) if not self._is_page(self.table[u, c])]
+            lacks = [c for c in reached if not self._is_page(self.table[u, c])]
             if replace + len(lacks) > len(free):
                 stopped = True
                 continue

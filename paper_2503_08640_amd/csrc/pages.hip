@@ -182,10 +182,23 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const
   __shared__ int wide_first_sh[1024 * kQ], wide_behind_sh[1024 * kQ];
   __shared__ int spare_sh[kSpareSh];
   __shared__ int wide_count_sh;
+  __shared__ bool shared_sh;
   const int tid = threadIdx.x, lane = tid % 64;
   int r[kEach];
   refs_of<kEach>(p, static_cast<int64_t>(tid) * kEach, r);
-  if (tid == 0) wide_count_sh = 0;
+  if (tid == 0) {
+    wide_count_sh = 0;
+    shared_sh = false;
+  }
+  // An entry behind the tokens lacks a page of the question's own if it names none, or one that others name too.  Those are given back
+  // below, all that were shared as the call began, so that the order does not matter: until then the workspace keeps which pages are.
+  auto lacks_page = [&](int entry) {
+    if (!is_page(entry, p)) return true;
+    const bool several = p.refs[entry] > 1;
+    spare[entry] = several;
+    if (several) shared_sh = true;
+    return several;
+  };
   Ask a[kQ];
   int more[kQ], lacks[kQ];
 #pragma unroll
@@ -205,8 +218,11 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const
     const int u = tid * kQ + i, wide = a[i].behind - a[i].first;
     if (wide > 0 && wide <= kNarrow) {
       const int32_t* const row = p.table + static_cast<int64_t>(u) * p.table_stride;
+      int entry[kNarrow];
 #pragma unroll
-      for (int c = 0; c < kNarrow; ++c) lacks[i] += c < wide && !is_page(row[min(a[i].first + c, a[i].behind - 1)], p);
+      for (int c = 0; c < kNarrow; ++c) entry[c] = row[min(a[i].first + c, a[i].behind - 1)];
+#pragma unroll
+      for (int c = 0; c < kNarrow; ++c) lacks[i] += c < wide && lacks_page(entry[c]);
     }
     const uint64_t many = __ballot(wide > kNarrow);
     if (many) {
@@ -228,10 +244,36 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const
     const int32_t* const row = p.table + static_cast<int64_t>(u) * p.table_stride;
     int n = 0;
 #pragma unroll 2
-    for (int c = wide_first_sh[i] + tid % 16; c < behind; c += 16) n += !is_page(row[c], p);
+    for (int c = wide_first_sh[i] + tid % 16; c < behind; c += 16) n += lacks_page(row[c]);
 #pragma unroll
     for (int s = 8; s > 0; s >>= 1) n += __shfl_xor(n, s);
     if (tid % 16 == 0) lacks_sh[u] = n;
+  }
+  __syncthreads();
+  if (shared_sh) {
+    auto give_back = [&](int32_t* entry) {
+      const int page = *entry;
+      if (!is_page(page, p) || !spare[page]) return;
+      atomicAdd(p.refs + page, -1);
+      *entry = -1;
+    };
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) {
+      const int wide = a[i].behind - a[i].first;
+      int32_t* const row = p.table + static_cast<int64_t>(tid * kQ + i) * p.table_stride;
+      if (wide <= kNarrow)
+#pragma unroll 1
+        for (int c = a[i].first; c < a[i].behind; ++c) give_back(row + c);
+    }
+    for (int i = tid / 16; i < n_wide; i += 64) {
+      int32_t* const row = p.table + static_cast<int64_t>(wide_sh[i]) * p.table_stride;
+      for (int c = wide_first_sh[i] + tid % 16; c < wide_behind_sh[i]; c += 16) give_back(row + c);
+    }
+    // (the counts changed behind the first cache: done before the barrier, and nothing of before is kept behind it)
+    __threadfence();
+    __syncthreads();
+    __threadfence();
+    refs_of<kEach>(p, static_cast<int64_t>(tid) * kEach, r);
   }
   // a page that several name is replaced while, behind the replacements of earlier questions, more than one still does
   bool replaced[kQ];
@@ -252,7 +294,6 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const
     }
     replaced[i] = count - before > 1;
   }
-  __syncthreads();  // (lacks_sh of the wide questions)
   constexpr uint64_t kOne = (uint64_t{1} << 48) + 1, low = (uint64_t{1} << 48) - 1;
   uint64_t asks = 0;  // pages, and in the upper sixteen bits replacements, of this thread's questions
 #pragma unroll

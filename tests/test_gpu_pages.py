@@ -103,6 +103,48 @@ def test_random_runs(b, columns, pages, page):
                 k.compact()
 
 
+@pytest.mark.parametrize("b,columns,pages,page", SHAPES + [(1100, 6, 9000, 16)])
+def test_random_runs_without_trims(b, columns, pages, page):
+    """Rows go on naming what lies behind their tokens: what others name too is not written to."""
+    rng = np.random.default_rng(7 * b + columns)
+    for seed in range(3):
+        k = books(50 + seed, b, columns, pages, page)
+        for step in range(8):
+            print(f"[pages] {b} {columns} {pages} {page}: without trims, seed {seed} step {step}", flush=True)
+            k.fork(np.where(rng.random(b) < 0.4, rng.integers(-2, b + 2, b), np.arange(b)))
+            k.set_len(np.maximum(k.want.self_len - rng.integers(0, [12, 5 * page, columns * page][step % 3], b), 0))
+            k.reserve(rng.integers(-1, [2, 9, 3 * page, columns * page // 2 + 2][step % 4], b))
+            if step % 3 == 2:
+                k.compact()
+
+
+def test_pages_that_are_shared_behind_the_tokens():
+    """A fork that was cut: entries that are reached and shared go back and others stand in their place, be they few or many, is the page
+    another's last one or named by another table, or is there no free one."""
+    page = 16
+    for columns, add in ((4, 20), (30, 300)):
+        table, refs = np.full((3, columns), -1), np.zeros(90)
+        n = 3 if columns == 4 else 25
+        table[0, :n], refs[:n] = np.arange(n), 1
+        refs[1] += 1  # another table names it
+        k = Pair(table, refs, [n * page - 8, 0, 0], page)
+        k.fork([0, 0, 0])
+        k.set_len([n * page - 8, 20, 0])
+        k.reserve([4, add, 0])
+        end = -(-(20 + add) // page)
+        assert k.refs[k.table[1, 1:end].long()].tolist() == [1] * (end - 1)
+        k.fork([0, 1, 0])
+        k.set_len([3, 0, 16])
+        k.reserve([1, 17, add])
+        k.set_len([0, 0, 0])
+        k.reserve([add, add, add])
+    k = Pair([[0, 1], [0, 1]], [2, 2], [16, 0], page)  # none is free
+    k.reserve([0, 32])
+    assert k.table.tolist() == [[0, 1], [-1, -1]]
+    k = Pair([[0, 0, 0], [1, 2, 1]], [3, 2, 1], [5, 5], page)  # a row that names a page several times
+    k.reserve([30, 30])
+
+
 def test_rows_go_round_in_a_circle():
     for b in (2, 3, 300, 1500):
         k = books(b, b, 6, 8 * b, 16, full=0.8)

@@ -83,6 +83,48 @@ def test_books_stay_consistent():
             assert (k.table[u, :k._used(k.self_len[u])] >= 0).all()
 
 
+def test_what_is_written_to_is_not_shared():
+    """A question that was cut without a trim still names pages behind its tokens.  Those of them that others name too are not handed to
+    it for its new tokens: they are given back, and pages of its own stand in their place."""
+    table, refs = np.full((2, 4), -1), np.zeros(8)
+    table[0, :3], refs[:3] = [0, 1, 2], 1
+    k = orc.Books(table, refs, [40, 0], 16)
+    k.fork([0, 0])
+    k.self_len[1] = 20
+    got, copies = k.reserve([0, 20])
+    assert list(got) == [0, 20] and copies == [(1, 3, 4)]
+    # (page 2 is not question 0's alone until question 1 has given it back: then page 4 takes its place)
+    assert k.table.tolist() == [[0, 1, 2, -1], [0, 3, 4, -1]] and k.refs.tolist() == [2, 1, 1, 1, 1, 0, 0, 0]
+    # both are cut to nothing: page 0 goes back twice and is the lowest free one
+    k.self_len[:] = 0
+    got, copies = k.reserve([16, 16])
+    assert copies == [] and k.table.tolist() == [[0, 1, 2, -1], [5, 3, 4, -1]] and k.refs.tolist() == [1, 1, 1, 1, 1, 1, 0, 0]
+    # there are too few free ones: what was shared is given back all the same, the rest stays
+    k = orc.Books(np.array([[0, 1], [0, 1]]), [2, 2], [16, 0], 16)
+    got, copies = k.reserve([0, 32])
+    assert list(got) == [0, 0] and copies == [] and k.table.tolist() == [[0, 1], [-1, -1]] and k.refs.tolist() == [1, 1]
+    assert k.self_len.tolist() == [16, 0]
+
+
+def test_books_without_trims():
+    """Random runs in which rows keep naming what lies behind their tokens: nobody is handed a page that another entry names, and what a
+    copy reads is still named."""
+    rng = np.random.default_rng(6)
+    b, c, pages, page = 9, 6, 70, 16
+    for _ in range(40):
+        k = orc.Books(np.full((b, c), -1), np.zeros(pages), np.zeros(b), page)
+        for _ in range(12):
+            k.fork([int(x) for x in np.where(rng.random(b) < 0.3, rng.integers(0, b, b), np.arange(b))])
+            k.self_len = np.maximum(k.self_len - rng.integers(0, 50, b), 0)
+            got, copies = k.reserve(rng.integers(-2, 40, b))
+            for u in np.nonzero(got)[0]:
+                for i in range((k.self_len[u] - got[u]) // page, -(-k.self_len[u] // page)):
+                    assert k.refs[k.table[u, i]] == 1
+            assert not set(x[0] for x in copies) & set(x[1] for x in copies) and all(k.refs[x[0]] > 0 for x in copies)
+            named = k.table[k.table >= 0]
+            assert (np.bincount(named, minlength=pages) == k.refs).all()
+
+
 # ---- refusals of the library -----------------------------------------------------------------------------------
 
 def verify(**change):
