@@ -650,12 +650,13 @@ int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, co
  *                draws.  (Where it is outside, the draw takes the last token with a weight.)
  *   out_tokens : device int32 [n_tokens]: the tokens that stand, the drawn one, then -1, from the question's first row on; rows
  *                of no question are left alone.  A row without any probability draws -1; where w is 0 throughout (p nowhere above
- *                q) the draw is from p_n.  Not to overlap tokens.
+ *                q) the draw is from p_n.
  *   accepted   : device int32 [n_queries]: how many stand.
- *   logp       : optional device float [n_tokens], not to overlap uniform: log p of each token of out_tokens (where T is not above 0: of T = 1), 0 in
+ *   logp       : optional device float [n_tokens]: log p of each token of out_tokens (where T is not above 0: of T = 1), 0 in
  *                rows without one.
  *   self_len, new_len : optional device int32 [n_queries], both or none: the own keys at the chunk's attention call, and those
- *                of the tokens that stand: self_len - (T_u - 1 - accepted).  May be the same array.
+ *                of the tokens that stand: self_len - (T_u - 1 - accepted).  May be the same array.  No other array that is
+ *                written may overlap one that is read, or another (INVALID_ARG where both are among tokens to new_len).
  *   workspace  : device memory of >= dbsa_draft_verify_workspace_bytes() bytes, 16-byte aligned; calls that overlap need one
  *                each.  Its contents need not be set.
  * Distributions, sums and prefixes are held in 64 bits.  The call only launches kernels and may be recorded into a HIP graph;

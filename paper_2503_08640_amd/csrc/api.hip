@@ -1331,12 +1331,6 @@ int dbsa_draft_verify(const void* target, int64_t target_stride, const dbsa_draf
   if (form != DBSA_LOGITS && form != DBSA_PROBABILITIES) return DBSA_ERR_UNSUPPORTED;
   if (!cu_qlens || !accepted || n_tokens < 0 || n_queries < 1 || vocab < 1 || !self_len != !new_len) return DBSA_ERR_INVALID_ARG;
   if (n_tokens > 0 && (!target || !tokens || !uniform || !out_tokens)) return DBSA_ERR_INVALID_ARG;
-  // (every workgroup of a question reads what one of them writes beside)
-  auto meet = [n_tokens](const void* a, const void* b) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b), bytes = static_cast<uintptr_t>(n_tokens) * 4;
-    return x < y + bytes && y < x + bytes;
-  };
-  if (n_tokens > 0 && (meet(out_tokens, tokens) || (logp && meet(logp, uniform)))) return DBSA_ERR_INVALID_ARG;
   if (form == DBSA_PROBABILITIES && temperature) return DBSA_ERR_INVALID_ARG;
   const uintptr_t size = dtype == DBSA_BF16 ? 2 : 4;
   if (reinterpret_cast<uintptr_t>(target) % size != 0 || target_stride < 0) return DBSA_ERR_INVALID_ARG;
@@ -1347,6 +1341,23 @@ int dbsa_draft_verify(const void* target, int64_t target_stride, const dbsa_draf
   if (vocab > 1 << 30 || std::max<int64_t>(n_tokens, n_queries) * pieces > 1 << 23) return DBSA_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < verify_workspace_bytes(n_tokens, n_queries, vocab) || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
     return DBSA_ERR_WORKSPACE;
+  // Every workgroup of a question reads what one of them writes beside.
+  struct Words {
+    const void* at;
+    int64_t n;
+  };
+  const Words written[] = {{out_tokens, n_tokens}, {logp, n_tokens}, {accepted, n_queries}, {new_len, n_queries}};
+  const Words read[] = {{tokens, n_tokens}, {uniform, n_tokens}, {cu_qlens, int64_t{n_queries} + 1}, {temperature, n_queries}, {self_len, n_queries}};
+  auto meet = [](const Words& a, const Words& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return x && y && a.n > 0 && b.n > 0 && x < y + b.n * 4 && y < x + a.n * 4;
+  };
+  for (int i = 0; i < 4; ++i) {
+    for (const Words& r : read)
+      if (meet(written[i], r) && !(new_len == self_len && written[i].at == new_len && r.at == self_len)) return DBSA_ERR_INVALID_ARG;
+    for (int k = 0; k < i; ++k)
+      if (meet(written[i], written[k])) return DBSA_ERR_INVALID_ARG;
+  }
   VerifyParams p{};
   p.target = target;
   p.target_stride = target_stride;

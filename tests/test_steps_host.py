@@ -156,6 +156,26 @@ def test_verify_refuses(change, code):
     assert verify(**change) == code
 
 
+@pytest.mark.parametrize("written", ["out", "logp", "accepted", "new_len"])
+@pytest.mark.parametrize("read", ["tokens", "uniform", "cu", "heat", "self_len"])
+def test_outputs_over_what_is_read_are_refused(written, read):
+    """Every workgroup of a question reads what one of them writes beside: only the lengths may be one array."""
+    at = dict(tokens=1 << 20, uniform=2 << 20, cu=3 << 20, heat=4 << 20, self_len=5 << 20, out=6 << 20, logp=7 << 20, accepted=8 << 20,
+              new_len=9 << 20, target=10 << 20, ws=11 << 20, n=40, b=30)
+    last = 4 * (dict(tokens=40, uniform=40, cu=31, heat=30, self_len=30)[read] - 1)
+    first = 4 * (dict(out=40, logp=40, accepted=30, new_len=30)[written] - 1)
+    for off in (last, -first) + ((0,) if (written, read) != ("new_len", "self_len") else (4, -4)):
+        assert verify(**dict(at, **{written: at[read] + off})) == B.DBSA_ERR_INVALID_ARG, off
+
+
+@pytest.mark.parametrize("one,other", itertools.combinations(["out", "logp", "accepted", "new_len"], 2))
+def test_outputs_over_each_other_are_refused(one, other):
+    at = dict(tokens=1 << 20, uniform=2 << 20, cu=3 << 20, self_len=5 << 20, out=6 << 20, logp=7 << 20, accepted=8 << 20, new_len=9 << 20,
+              target=10 << 20, ws=11 << 20, n=40, b=30)
+    for off in (0, 4 * 29, -4 * 29):
+        assert verify(**dict(at, **{one: at[other] + off})) == B.DBSA_ERR_INVALID_ARG, off
+
+
 def test_workspace_grows_with_what_is_checked():
     size = B.dbsa_draft_verify_workspace_bytes
     assert size(-1, 1, 9) == size(1, 0, 9) == size(1, 1, 0) == size(1, 1, (1 << 30) + 1) == 0
