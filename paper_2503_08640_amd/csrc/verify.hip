@@ -453,12 +453,12 @@ __device__ Decision decide(const VerifyParams& p, const Work& w, int u, const Sp
           d.top_q = __shfl_xor(d.top_p, kGroup);
           d.inv_q = __shfl_xor(d.inv_p, kGroup);
         }
-        if (heat.greedy) mine = of_draft ? 0.0 : x == d.place ? 1.0 : 0.0;
       } else {
         mine = clean(v);
       }
-      const double other = __shfl_xor(mine, kGroup), qx = drawn || (kLogits && heat.greedy) ? other : 1.0;
+      const double other = __shfl_xor(mine, kGroup), qx = drawn ? other : 1.0;
       stands = asks && static_cast<double>(number_of_row) * qx < mine;  // (counts in the lanes that speak)
+      if (kLogits && heat.greedy) stands = asks && x == d.place;        // (whatever the number is)
     }
     const uint64_t mask = __ballot(!stands);
     if (threadIdx.x % 64 == 0) falls_sh[threadIdx.x / 64] = static_cast<unsigned>((mask & 1) | (mask >> 2 * kGroup & 1) << 1) << group;

@@ -359,3 +359,16 @@ def test_rows_that_two_questions_claim_stay_inside(byte):
         torch.cuda.synchronize()
         assert (full[:2] == -77).all() and (full[5:] == -77).all()
         assert (full[2:5] >= -1).all() and (full[2:5] < vocab).all(), full.tolist()
+
+
+@pytest.mark.parametrize("number", [float("nan"), float("inf"), -float("inf"), -1.0, 7.0])
+def test_greedy_needs_no_random_numbers(number):
+    """Where a question is greedy its numbers may be anything; the others' are not touched by that."""
+    for draft in (True, False):
+        c = make(330, [4, 3, 4, 1], 2500, "f32", draft=draft, heat=[0.0, 0.7, -1.0, 0.0])
+        likely = c["x"].argmax(1).numpy()
+        c["tokens"][[1, 2, 3, 8, 9]] = likely[[0, 1, 2, 7, 8]]
+        c["uniform"][[0, 1, 2, 3, 7, 8, 9, 10, 11]] = number
+        want = wanted(c)
+        assert want["accepted"][0] == 3 and want["accepted"][2] >= 2
+        same(call(c), want, c, f"greedy, numbers {number} draft {draft}")
