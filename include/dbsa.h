@@ -647,7 +647,8 @@ int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, co
  *                number count as 0, and a row need not sum to 1.
  *   temperature: device float [n_queries], or NULL for 1.
  *   uniform    : device float [n_tokens] in [0, 1): that of row a decides on proposal a, that of the question's last row
- *                draws.  (Where it is outside, the draw takes the last token with a weight.)
+ *                draws.  (Outside, as the formulas say: below 0 every proposal with q > 0 stands, be p 0 and its log p
+ *                -infinity, and the draw takes the first token with a weight; at 1 and above, and where it is no number, the last.)
  *   out_tokens : device int32 [n_tokens]: the tokens that stand, the drawn one, then -1, from the question's first row on; rows
  *                of no question are left alone.  A row without any probability draws -1; where w is 0 throughout (p nowhere above
  *                q) the draw is from p_n.

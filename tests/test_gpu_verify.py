@@ -372,3 +372,28 @@ def test_greedy_needs_no_random_numbers(number):
         want = wanted(c)
         assert want["accepted"][0] == 3 and want["accepted"][2] >= 2
         same(call(c), want, c, f"greedy, numbers {number} draft {draft}")
+
+
+def test_random_numbers_outside_their_range():
+    """What the formulas make of them, where the outcome can be said without an oracle."""
+    for form in ("logits", "probs"):
+        for draft in (True, False):
+            for u, place in ((-0.5, 0), (1.0, 1), (7.0, 1), (float("nan"), 1), (float("inf"), 1), (-float("inf"), 0)):
+                c = make(340, [2, 1], 900, "f32", form, draft)
+                low = -float("inf") if form == "logits" else 0.0
+                c["x"][:, :30], c["x"][:, 800:] = low, low
+                c["x"][:, 500], c["x"][:, 799], c["x"][:, 30] = 0.25, 0.25, 0.25
+                if draft:  # proposed from where the target has nothing
+                    c["y"][0, 0] = low
+                    c["y"][0, 0, [7, 500]] = 0.5
+                c["tokens"][1] = 7
+                c["uniform"][:] = u
+                want = wanted(c)
+                first = [30, 799][place]
+                # below 0 what was drawn with q > 0 stands, and what is looked up, q = 1, too; -infinity times q is no less
+                stands = u < 0
+                assert want["accepted"].tolist() == [int(stands), 0]
+                assert want["out"].tolist() == ([7, first, first] if stands else [first, -1, first])
+                got = call(c)
+                assert got["out"].tolist() == want["out"].tolist() and got["accepted"].tolist() == want["accepted"].tolist()
+                assert got["logp"][0] == (-np.inf if stands else got["logp"][0])
