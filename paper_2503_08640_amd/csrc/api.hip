@@ -1337,7 +1337,8 @@ int dbsa_draft_verify(const void* target, int64_t target_stride, const dbsa_draf
   const bool drawn = draft && draft->ptr;
   if (drawn && (reinterpret_cast<uintptr_t>(draft->ptr) % size != 0 || draft->stride_query < 0 || draft->stride_step < 0 || draft->n_steps < 0))
     return DBSA_ERR_INVALID_ARG;
-  const int64_t pieces = (int64_t{vocab} + 8 + 4095) / 4096;  // (a grid counts its threads in 32 bits)
+  // (a grid counts its threads in 32 bits: with this the statistics have 2^30 at most, the draws 2^31)
+  const int64_t pieces = (int64_t{vocab} + 4095) / 4096;
   if (vocab > 1 << 30 || std::max<int64_t>(n_tokens, n_queries) * pieces > 1 << 23) return DBSA_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < verify_workspace_bytes(n_tokens, n_queries, vocab) || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
     return DBSA_ERR_WORKSPACE;

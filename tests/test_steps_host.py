@@ -176,6 +176,15 @@ def test_outputs_over_each_other_are_refused(one, other):
         assert verify(**dict(at, **{one: at[other] + off})) == B.DBSA_ERR_INVALID_ARG, off
 
 
+def test_the_most_that_is_checked():
+    """Rows, or questions, times pieces of 4096 words: 2^23, and not one more (seen by which argument is refused)."""
+    for n, b, vocab, code in ((1 << 23, 1, 4096, B.DBSA_ERR_WORKSPACE), (1 << 23, 1, 4097, B.DBSA_ERR_UNSUPPORTED),
+                              (1, 1 << 23, 4096, B.DBSA_ERR_WORKSPACE), ((1 << 23) + 1, 1, 1, B.DBSA_ERR_UNSUPPORTED),
+                              (1 << 22, 1, 8192, B.DBSA_ERR_WORKSPACE), (1 << 22, 1, 8193, B.DBSA_ERR_UNSUPPORTED),
+                              (32, 1, 1 << 30, B.DBSA_ERR_WORKSPACE), (33, 1, 1 << 30, B.DBSA_ERR_UNSUPPORTED)):
+        assert verify(n=n, b=b, vocab=vocab, ws=None) == code, (n, b, vocab)
+
+
 def test_workspace_grows_with_what_is_checked():
     size = B.dbsa_draft_verify_workspace_bytes
     assert size(-1, 1, 9) == size(1, 0, 9) == size(1, 1, 0) == size(1, 1, (1 << 30) + 1) == 0
