@@ -192,10 +192,9 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const
   }
   // An entry behind the tokens lacks a page of the question's own if it names none, or one that others name too.  Those are given back
   // below, all that were shared as the call began, so that the order does not matter: until then the workspace keeps which pages are.
-  auto lacks_page = [&](int entry) {
-    if (!is_page(entry, p)) return true;
-    const bool several = p.refs[entry] > 1;
-    spare[entry] = several;
+  auto shared = [&](int page) {
+    const bool several = p.refs[page] > 1;
+    spare[page] = several;
     if (several) shared_sh = true;
     return several;
   };
@@ -218,11 +217,17 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const
     const int u = tid * kQ + i, wide = a[i].behind - a[i].first;
     if (wide > 0 && wide <= kNarrow) {
       const int32_t* const row = p.table + static_cast<int64_t>(u) * p.table_stride;
-      int entry[kNarrow];
+      int entry[kNarrow], named = 0;
 #pragma unroll
-      for (int c = 0; c < kNarrow; ++c) entry[c] = row[min(a[i].first + c, a[i].behind - 1)];
+      for (int c = 0; c < kNarrow; ++c) {
+        entry[c] = row[min(a[i].first + c, a[i].behind - 1)];
+        named += c < wide && is_page(entry[c], p);
+      }
+      lacks[i] = wide - named;
+      if (named) {
 #pragma unroll
-      for (int c = 0; c < kNarrow; ++c) lacks[i] += c < wide && lacks_page(entry[c]);
+        for (int c = 0; c < kNarrow; ++c) lacks[i] += c < wide && is_page(entry[c], p) && shared(entry[c]);
+      }
     }
     const uint64_t many = __ballot(wide > kNarrow);
     if (many) {
@@ -243,8 +248,15 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const
     const int u = wide_sh[i], behind = wide_behind_sh[i];
     const int32_t* const row = p.table + static_cast<int64_t>(u) * p.table_stride;
     int n = 0;
+    bool named = false;
 #pragma unroll 2
-    for (int c = wide_first_sh[i] + tid % 16; c < behind; c += 16) n += lacks_page(row[c]);
+    for (int c = wide_first_sh[i] + tid % 16; c < behind; c += 16) {
+      const int lacking = !is_page(row[c], p);
+      n += lacking;
+      named |= !lacking;
+    }
+    if (named)
+      for (int c = wide_first_sh[i] + tid % 16; c < behind; c += 16) n += is_page(row[c], p) && shared(row[c]);
 #pragma unroll
     for (int s = 8; s > 0; s >>= 1) n += __shfl_xor(n, s);
     if (tid % 16 == 0) lacks_sh[u] = n;
