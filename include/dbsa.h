@@ -641,7 +641,8 @@ int dbsa_kv8_read(dbsa_tensor k_cache8, dbsa_tensor v_cache8, int64_t n_rows, co
  *                in draft, ends the proposals: nothing is taken from p_n there.
  *   cu_qlens   : device int32 [n_queries + 1], ascending from 0, each at most n_tokens; a question may have no rows.
  *   form       : DBSA_LOGITS: p = softmax(row / T), T = temperature[u]; a value that is no number counts as -infinity, values of
- *                +infinity share everything; T counts as at most 1e30.  T that is not above 0: p is 1 at the largest value, the lowest index of equal
+ *                +infinity share everything (what is masked is best -infinity: stretches of finite low values take longer);
+ *                T counts as at most 1e30.  T that is not above 0: p is 1 at the largest value, the lowest index of equal
  *                ones, draft is not read, and the random numbers do not matter.
  *                DBSA_PROBABILITIES: rows hold p and q themselves (temperature NULL); values that are negative, infinite or no
  *                number count as 0, and a row need not sum to 1.

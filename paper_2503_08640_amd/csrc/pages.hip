@@ -1,8 +1,8 @@
 // Pages of the caches that the chunk attention reads: sharing, making room, giving back, tidying up, copying.  The books (page
 // table, counts of the entries that name a page, lengths) are the caller's arrays; a page is free while its count is not above 0.
 // These calls move little and are bound by the launch and by chains of loads, the copies by memory: 1.07 GB moved by a compaction in 8
-// layers 215 us with its plan (5.0 TB/s, what a large copy reaches), 48 shared last pages in 16 layers 29 us (196 MB, partly from the
-// last-level cache).
+// layers 215 us with its plan (5.0 TB/s, what a large copy reaches), 48 shared last pages in 16 layers 40 us (196 MB, three caches in
+// turn; 32 with one, partly from the last-level cache).
 #include <cstdint>
 
 #include "kernels.hpp"
@@ -171,7 +171,9 @@ constexpr int kSpareSh = 8192; // free pages that are kept in LDS
 
 // One workgroup, in the order of the questions, kQ of them to a thread: what each asks for, the pages it gets, the books.  A chain
 // of loads (lengths, entries, counts of the last pages); the first 8192 counts are asked for in front of it.  64 questions with 48
-// replacements 7.8 us, 128 prompts of 450 to 900 tokens in pages of 16 (5500 pages out of 32768) 10.4 (64 with a question after the other).
+// replacements 8 us, 128 prompts of 450 to 900 tokens in pages of 16 (5500 pages out of 32768) 11.4 (64 with a question after the other).
+// Counts are looked through from page 0 on, 8192 with a scan: a page for each of 128 questions 6.9 us in an arena of 8192 pages, 10.8 of
+// 32768 and 42 of 262144 with the first four fifths in use.
 template <int kQ>
 __global__ __launch_bounds__(1024) void pages_reserve_kernel(BookParams p, const int32_t* add, int32_t* got, int32_t* copies,
                                                             int32_t* n_copies, int32_t* spare) {
@@ -543,7 +545,9 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(PagesCopyParams p) {
 
 hipError_t launch_pages_fork(const BookParams& p, const int32_t* source, hipStream_t stream) {
   // as many columns as the workgroup's registers hold; a table that fits into one workgroup is one launch, others have 8 columns
-  // to a workgroup at most (512 rows 11.5 us with the lengths, 16 columns 15.2, 4 columns 12.4)
+  // to a workgroup at most, however few rows there are: the loads and atomics of a workgroup are the time.  With the lengths, of 4, 8, 16,
+  // 64 and any columns: 512 rows of 1024 entries, 375 in use, 11.0 10.7 14.3 14.3 14.3 us; 128 rows 5.6 5.8 6.7 13.0 13.0; 16 rows 4.3 4.3 4.5
+  // 5.0 12.4; 16 rows of 4096, 2000 in use, 6.3 4.9 4.8 5.2 14.4
   int columns_log2 = 0;
   while ((1 << columns_log2) < p.table_stride && (p.n_queries << (columns_log2 + 1)) <= 1024 * kForkEach && (1 << columns_log2) < 1024) ++columns_log2;
   const bool alone = (1 << columns_log2) >= p.table_stride && p.n_queries <= 1024;

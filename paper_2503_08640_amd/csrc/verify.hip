@@ -228,7 +228,10 @@ __device__ inline void values_of(uintx4 v, const T* row, int first, int vocab, f
 
 // One wave: a piece of a row, in chunks of kLoads times 16 bytes a lane, the next chunk on its way while one is summed up.  The
 // exponents are counted from the largest value of the first chunk that has one: 64 bits leave 2^1000 on either side, so that the
-// maximum need not be followed.  A piece that holds more than that (or +infinity) is gone through again with its own.
+// maximum need not be followed.  A piece that holds more than that (or +infinity) is gone through again with its own, twice and a value
+// at a time: also one whose first chunk with a value above -infinity holds finite masks alone (-1e9, the type's lowest value), which
+// -infinity does not cost.  512 rows of 128256 values, the front half masked: 232 us in bf16 and 176 in fp32 with -1e9, 60 and 68 with
+// -infinity; 1 in 100 left anywhere, with the lowest value: 78 and 112, 60 and 66.
 // 800 rows of 128256 values: 92 us in fp32, memory (4.5 TB/s; a copy on this card reaches 5.0), 82 in bf16, operations (20.7 of a wave
 // for 64 values, 82 % of the rate that such operations reach).  With a maximum and barriers per workgroup 100 and 95 us; pieces of half
 // the size 3 to 5 % more, four loads on their way instead of two no less.
@@ -252,7 +255,8 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) raw[i] = load_wide(from, mine + i * kStep, p.vocab);
   }
-  // the question: as many as end at or before this row
+  // the question: as many as end at or before this row, 64 bounds a step (2048 rows of 32000 values in bf16: 57 us for 2048 questions, 48
+  // for 512; 4096 rows of 8000 in fp32: 69 us for 4096, 39 for 1024)
   int u = 0;
   for (int i = 0; i < p.n_queries; i += 64) u += __popcll(__ballot(i + lane < p.n_queries && p.cu[min(i + lane, p.n_queries - 1) + 1] <= row));
   if (u >= p.n_queries) return;
@@ -648,7 +652,8 @@ __device__ inline Place place_of(const Work& w, Decision& d, const Scale& of_p) 
 
 // One workgroup: shares part * each .. of the row that decides for question u, a wave a share at a time and the next one on its way;
 // where the statistics have the sums already, one workgroup alone and the piece that the token lies in (a draw for each of 128 rows
-// without proposals: 54 us with every row weighed, so 29, statistics included).  Two kernels, the sums first and then the draws, were
+// without proposals: 54 us with every row weighed, so 27, statistics included; this kernel 11 of it, a chain: the pieces summed up,
+// weighed, the token's piece read).  Two kernels, the sums first and then the draws, were
 // 24 us instead of 19 for probabilities of 64 questions over 102400 words (2.8 TB/s of the rows that decide, the launch and the draw
 // included) and 25 instead of 16 for one question.
 template <typename T, bool kLogits, bool kDecided>
@@ -824,6 +829,10 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyParams p, i
 template <typename T, bool kLogits>
 void launch(const VerifyParams& p, hipStream_t stream) {
   const int64_t rows = (p.draft ? 2 : 1) * static_cast<int64_t>(p.n_tokens);
+  // A wave's piece: short ones fill the chip, long ones pay less often for the search, the scale and the reductions.  Calls with pieces
+  // of 2048 and of 8192, in bf16: 16 x 8 looked up over 50257 words (2^22.6 values) 19.4 and 26.7 us, 128 rows of 128256 (2^24) 26.6 and
+  // 30.7, 256 (2^25) 39.7 and 40.2, 512 (2^26) 67.0 and 59.4; with proposals' logits 32 x 4 (2^25) 51.2 and 45.7, 48 x 4 68.0 and 58.8,
+  // 128 x 4 (2^27) 133 and 119; fp32 84 and 79 for 64 x 4, 157 and 145 for 128 x 4.
   const int piece = rows * p.vocab >= int64_t{1} << 25 ? 4 * kPieceLeast : kPieceLeast;
   const Work w = work_of(p.workspace, p.n_tokens, p.n_queries, p.vocab, piece);
   const dim3 threads(kThreads);
